@@ -270,6 +270,169 @@ typedef struct tl_gemm_gs_job {
 tl_status tl_ternary_gemm_gs_grouped(const tl_gemm_gs_job* jobs, int64_t count, void* stream);
 
 /*
+ * ---- The attention of a block: positions, an 8-bit cache in pages, attention over it and over whole prompts ----
+ *
+ * What stands between the QKV and the O projection of a transformer block whose linears are the products above.  All
+ * activations are fp16; softmax, sums and scales are fp32.
+ *
+ * A tensor of heads: element (token t, head h, dimension d) is the fp16 at ptr + t * token_stride + h * head_stride + d,
+ * strides in elements, multiples of 8 and not negative, ptr 16-byte aligned.  So query, key and value may lie side by
+ * side in the rows that one QKV product writes.
+ */
+typedef struct tl_heads {
+    void* ptr;                /* device, fp16 */
+    int64_t token_stride;
+    int64_t head_stride;
+} tl_heads;
+
+/*
+ * The tokens of a call: those of sequence s are rows seq_start[s] .. seq_start[s+1] - 1, and cached[s] tokens of the
+ * sequence came before them, so that its token i stands at position cached[s] + i.  Both arrays are device memory and read
+ * by the kernels, so a captured call serves every step.  seq_start does not decrease and lies in [0, tokens]; rows that no sequence has are neither read
+ * nor written, and a sequence may have none.  cached[s] < 0 marks a sequence that is not in use: nothing of it
+ * goes into the cache and its output rows are written as 0.
+ */
+typedef struct tl_batch {
+    const int32_t* seq_start; /* device, [seqs + 1]; NULL: every sequence has one token (tokens == seqs)   */
+    const int32_t* cached;    /* device, [seqs]; NULL: 0 for each                                          */
+    int64_t seqs, tokens;     /* 1 <= seqs < 2^20; 0 <= tokens < 2^30 (0: the call does nothing)           */
+} tl_batch;
+
+/*
+ * A cache of keys and values in 8 bits.  Pages of page_tokens tokens (16, 32, 64, ... 1024) hold all key heads; position p of
+ * sequence s is in page page_table[s][p / page_tokens].  Sixteen tokens (positions 16 b .. 16 b + 15) and one head are a
+ * block, which has one fp32 scale: a code stands for scale * code.  Codes are whole numbers in -127 .. 127
+ * (TL_KV_INT8) or 8-bit floats with 4 exponent and 3 mantissa bits, largest 448 (TL_KV_FP8); the former are the nearer to
+ * values of one size, the latter to values of many.
+ *   k, v              device, [pages][kv_heads][page_tokens / 16][16 * head_dim] bytes, 16-byte aligned.  In a block, a
+ *                     key's dimension d of token t is byte ((t / 4) * (head_dim / 16) + d / 16) * 64 + (t % 4) * 16 + d % 16, a value's
+ *                     (d / 16) * 256 + (d % 16) * 16 + t: the orders in which the matrix instructions take them
+ *   k_scale, v_scale  device, fp32 [pages][kv_heads][page_tokens / 16]
+ *   page_table        device, int32 [seqs][pages_per_seq].  An entry outside [0, pages) stands for no page: what would
+ *                     go there is dropped, and attention does not see it
+ * Memory of pages need not be set to anything before they are used.  The cache belongs to the caller, and two calls
+ * that write or read and write the same page have to be on one stream or ordered by the caller.
+ */
+typedef enum tl_kv_type {
+    TL_KV_INT8 = 0,
+    TL_KV_FP8 = 1,
+    TL_KV_INT_RANGE_ = 0x7fffffff /* not a type (see TL_FMT_INT_RANGE_) */
+} tl_kv_type;
+
+typedef struct tl_kv_cache {
+    void* k;
+    void* v;
+    float* k_scale;
+    float* v_scale;
+    const int32_t* page_table;
+    int64_t pages, page_tokens, pages_per_seq;
+    int64_t kv_heads, head_dim;
+    tl_kv_type type;
+} tl_kv_cache;
+
+/*
+ * Rotary positions.  Of each head the first rot_dim dimensions (even, at most head_dim) are turned in pairs,
+ * (a, b) -> (a c - b s, a s + b c) with c = table[p][j] and s = table[p][rot_dim / 2 + j] for pair j at position p; the pair is
+ * dimensions (j, rot_dim / 2 + j), or with `pairs` not 0 the neighbours (2 j, 2 j + 1).  Products and sums are fp32, each rounded by itself.
+ *   table   device, fp32 [positions][rot_dim], 4-byte aligned (tl_rope_table fills one on the host).  A position that it does not
+ *           reach gives NaN
+ */
+typedef struct tl_rope {
+    const float* table;
+    int64_t positions, rot_dim;
+    int32_t pairs;
+} tl_rope;
+
+/*
+ * Fills a host table for tl_rope: pair j turns by p * f_j with f_j = base^(-2 j / rot_dim), computed in fp64.  For contexts longer
+ * than a model was trained on, `scaling` (NULL: none) changes the frequencies:
+ *   TL_ROPE_LINEAR    f_j / factor
+ *   TL_ROPE_BY_PARTS  a pair that turns t = trained * f_j / (2 pi) times over the trained length keeps f_j if t >= high, gets
+ *                     f_j / factor if t <= low, and between them the mean of both weighted by (t - low) / (high - low)
+ * and cosines and sines are multiplied by `magnitude`.  TL_ERR_SHAPE for positions or rot_dim < 1 or an odd rot_dim,
+ * TL_ERR_VALUE for a base, factor or magnitude that is not positive and finite, or a range that is none, TL_ERR_UNSUPPORTED for an unknown kind.
+ */
+typedef enum tl_rope_kind {
+    TL_ROPE_PLAIN = 0,
+    TL_ROPE_LINEAR = 1,
+    TL_ROPE_BY_PARTS = 2,
+    TL_ROPE_INT_RANGE_ = 0x7fffffff /* not a kind (see TL_FMT_INT_RANGE_) */
+} tl_rope_kind;
+
+typedef struct tl_rope_scaling {
+    tl_rope_kind kind;
+    double factor;            /* TL_ROPE_LINEAR, TL_ROPE_BY_PARTS                  */
+    double trained, low, high;/* TL_ROPE_BY_PARTS: 0 <= low < high, trained > 0     */
+    double magnitude;
+} tl_rope_scaling;
+
+tl_status tl_rope_table(float* table, int64_t positions, int64_t rot_dim, double base, const tl_rope_scaling* scaling);
+
+/*
+ * Rotates the queries and keys of a call's tokens and puts keys and values into the cache.
+ *   q, k, v        in; q_out, k_out: rotated and rounded to fp16 (ptr NULL: not wanted; they may be q and k themselves, with
+ *                  the same strides, and may not overlap them otherwise).  q may have ptr NULL and q_heads 0, k and v ptr NULL where kv_heads is 0
+ *   rope           NULL: no rotation
+ *   cache          NULL: rotation alone (v is then not read); else kv_heads and head_dim as the cache has them
+ *   head_dim       a multiple of 16 up to 128
+ * What goes into the cache is coded from the fp32 rotated key and from the fp16 value.  A block's scale is that of the
+ * tokens it holds before the call (0 if it holds none) or, if larger, the call's largest magnitude in it divided by 127 (448); where it grows, the
+ * earlier codes are coded anew, round(code * (old scale / new scale)).  Places behind the last token keep what they hold.
+ * A block that takes a NaN or an infinity gets the scale NaN, and stands for NaN until its first token is written again.
+ * Two sequences may not share a page that the call writes.
+ */
+typedef struct tl_append_job {
+    tl_heads q, k, v, q_out, k_out;
+    tl_batch batch;
+    const tl_kv_cache* cache;
+    const tl_rope* rope;
+    int64_t q_heads, kv_heads, head_dim;
+} tl_append_job;
+
+tl_status tl_kv_append(const tl_append_job* job, void* stream);
+
+/*
+ * Attention of a call's tokens over the cache, which holds them already (tl_kv_append first): the query of token i of sequence s sees
+ * positions 0 .. cached[s] + i, and
+ *     out[t][h] = sum_p softmax_p(scale * q[t][h] . k[p][g]) v[p][g],   g = h / (q_heads / kv_heads).
+ * A query that sees no position (all its pages missing) gives 0.  A block whose scale is NaN makes NaN of every query that sees a token of it, and of no other.
+ *   q, out      q_heads heads of cache->head_dim dimensions; out may be q itself with the same strides, and may not overlap it otherwise
+ *   longest     an upper bound of cached[s] + the tokens of s over all sequences, 0 if not known: it spares the second
+ *               launch that joins the parts of long sequences where none can be cut in parts.  Results are right also where it is exceeded
+ *   workspace   device, 16-byte aligned, tl_attn_cached_workspace bytes at least; written and read within the call alone
+ * Deterministic: no atomics, and the cuts depend on lengths and sizes alone.
+ */
+typedef struct tl_cached_job {
+    tl_heads q, out;
+    tl_batch batch;
+    const tl_kv_cache* cache;
+    int64_t q_heads;
+    float scale;
+    int64_t longest;
+    void* workspace;
+    size_t workspace_bytes;
+} tl_cached_job;
+
+size_t tl_attn_cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim);
+tl_status tl_attn_cached(const tl_cached_job* job, void* stream);
+
+/*
+ * Attention of whole prompts, causal: token i of a sequence sees tokens 0 .. i of the same sequence among this call's rows
+ * (batch.cached is not read), with fp16 keys and values:
+ *     out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j][g]) v[j][g],   g = h / (q_heads / kv_heads).
+ * head_dim is a multiple of 16 up to 128.  An infinity or a NaN in a key or value shows in the tokens that see it and in no others.  out may be
+ * q itself with the same strides, and may not overlap q, k or v otherwise.  Deterministic.
+ */
+typedef struct tl_prompt_job {
+    tl_heads q, k, v, out;
+    tl_batch batch;
+    int64_t q_heads, kv_heads, head_dim;
+    float scale;
+} tl_prompt_job;
+
+tl_status tl_attn_prompt(const tl_prompt_job* job, void* stream);
+
+/*
  * Bandwidth calibration: a plain streaming copy dst[i] = src[i] of `bytes` bytes
  * (multiple of 16, both device pointers 16-byte aligned).  Not part of the
  * method; it gives the HBM counters and timers a kernel of known traffic.

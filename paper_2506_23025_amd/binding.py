@@ -17,6 +17,8 @@ LIB_PATH = os.environ.get("TL_LIB_PATH") or os.path.join(_HERE, "libtl.so")
 TL_OK = 0
 TL_ERR_NULL, TL_ERR_SHAPE, TL_ERR_VALUE, TL_ERR_ALIGN, TL_ERR_UNSUPPORTED, TL_ERR_HIP = 1, 2, 3, 4, 5, 6
 TL_FMT_2BIT, TL_FMT_1P6BIT, TL_FMT_1P6BIT_FX = 0, 1, 2
+TL_KV_INT8, TL_KV_FP8 = 0, 1
+TL_ROPE_PLAIN, TL_ROPE_LINEAR, TL_ROPE_BY_PARTS = 0, 1, 2
 TL_PATH_AUTO, TL_PATH_GENERIC, TL_PATH_GEMV, TL_PATH_MFMA = 0, 1, 2, 3
 
 EXPORTS = (
@@ -26,6 +28,11 @@ EXPORTS = (
     "tl_ternary_gemm_gs", "tl_ternary_gemm_1p6_grouped", "tl_ternary_gemm_gs_grouped",
     "tl_ternary_gemm_which",
     "tl_init",
+    "tl_rope_table",
+    "tl_kv_append",
+    "tl_attn_cached_workspace",
+    "tl_attn_cached",
+    "tl_attn_prompt",
     "tl_probe_copy",
     "tl_probe_read",
     "tl_probe_mfma",
@@ -44,6 +51,54 @@ class tl_gemm_gs_job(ctypes.Structure):
     _fields_ = [("x", ctypes.c_void_p), ("Wpacked", ctypes.c_void_p), ("scales", ctypes.c_void_p),
                 ("y", ctypes.c_void_p),
                 ("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64), ("group", ctypes.c_int64)]
+
+
+class tl_heads(ctypes.Structure):
+    """Mirror of struct tl_heads in include/tl.h."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class tl_batch(ctypes.Structure):
+    """Mirror of struct tl_batch in include/tl.h."""
+    _fields_ = [("seq_start", ctypes.c_void_p), ("cached", ctypes.c_void_p), ("seqs", ctypes.c_int64), ("tokens", ctypes.c_int64)]
+
+
+class tl_kv_cache(ctypes.Structure):
+    """Mirror of struct tl_kv_cache in include/tl.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_table", ctypes.c_void_p), ("pages", ctypes.c_int64), ("page_tokens", ctypes.c_int64),
+                ("pages_per_seq", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("type", ctypes.c_int)]
+
+
+class tl_rope(ctypes.Structure):
+    """Mirror of struct tl_rope in include/tl.h."""
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int64), ("rot_dim", ctypes.c_int64), ("pairs", ctypes.c_int32)]
+
+
+class tl_rope_scaling(ctypes.Structure):
+    """Mirror of struct tl_rope_scaling in include/tl.h."""
+    _fields_ = [("kind", ctypes.c_int), ("factor", ctypes.c_double), ("trained", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("magnitude", ctypes.c_double)]
+
+
+class tl_append_job(ctypes.Structure):
+    """Mirror of struct tl_append_job in include/tl.h."""
+    _fields_ = [(n, tl_heads) for n in ("q", "k", "v", "q_out", "k_out")] + [
+        ("batch", tl_batch), ("cache", ctypes.POINTER(tl_kv_cache)), ("rope", ctypes.POINTER(tl_rope)),
+        ("q_heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64)]
+
+
+class tl_cached_job(ctypes.Structure):
+    """Mirror of struct tl_cached_job in include/tl.h."""
+    _fields_ = [("q", tl_heads), ("out", tl_heads), ("batch", tl_batch), ("cache", ctypes.POINTER(tl_kv_cache)),
+                ("q_heads", ctypes.c_int64), ("scale", ctypes.c_float), ("longest", ctypes.c_int64), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
+
+
+class tl_prompt_job(ctypes.Structure):
+    """Mirror of struct tl_prompt_job in include/tl.h."""
+    _fields_ = [(n, tl_heads) for n in ("q", "k", "v", "out")] + [
+        ("batch", tl_batch), ("q_heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
 class TlError(RuntimeError):
@@ -102,6 +157,13 @@ def _load():
     L.tl_ternary_gemm_which.restype = ci
     L.tl_init.argtypes = []
     L.tl_init.restype = ci
+    L.tl_rope_table.argtypes = [vp, i64, i64, ctypes.c_double, ctypes.POINTER(tl_rope_scaling)]
+    L.tl_rope_table.restype = ci
+    L.tl_attn_cached_workspace.argtypes = [i64, i64, i64, i64, i64]
+    L.tl_attn_cached_workspace.restype = sz
+    for name, job in (("tl_kv_append", tl_append_job), ("tl_attn_cached", tl_cached_job), ("tl_attn_prompt", tl_prompt_job)):
+        getattr(L, name).argtypes = [ctypes.POINTER(job), vp]
+        getattr(L, name).restype = ci
     L.tl_probe_copy.argtypes = [vp, vp, sz, vp]
     L.tl_probe_copy.restype = ci
     L.tl_probe_read.argtypes = [vp, sz, vp, vp]
@@ -316,6 +378,152 @@ def tl_ternary_gemm_gs_grouped(jobs, stream=None):
     """jobs: list of (x, Wpacked, scales, group, y, M, N, K), or an array made by make_gs_jobs."""
     arr = jobs if isinstance(jobs, ctypes.Array) else make_gs_jobs(jobs)
     _check(_lib.tl_ternary_gemm_gs_grouped(arr, len(arr), _stream(stream)), "tl_ternary_gemm_gs_grouped")
+
+
+# ---- attention of a block --------------------------------------------------------------
+#
+# A job is made once of the buffers that a program keeps and handed over at every step; it holds the tensors that it points to.
+
+def tl_rope_table(positions, rot_dim, base=10000.0, kind=TL_ROPE_PLAIN, factor=1.0, trained=1.0, low=0.0, high=1.0, magnitude=1.0):
+    """float32 [positions][rot_dim]: cosines, then sines."""
+    if positions < 1 or rot_dim < 1:
+        raise TlError(TL_ERR_SHAPE, "tl_rope_table")
+    out = np.empty((positions, rot_dim), dtype=np.float32)
+    scaling = tl_rope_scaling(kind, factor, trained, low, high, magnitude)
+    _check(_lib.tl_rope_table(out.ctypes.data, positions, rot_dim, float(base), ctypes.byref(scaling)), "tl_rope_table")
+    return out
+
+
+def _wants(t, what, dtype, dims, dense=True):
+    """A tensor's type and number of dimensions, before its address is all that is left of it."""
+    if str(t.dtype).replace("torch.", "") not in dtype or t.dim() != dims or not t.is_cuda:
+        raise ValueError(f"{what}: a device tensor of {' or '.join(dtype)} with {dims} dimensions is wanted, not {t.dtype} {tuple(t.shape)} on {t.device}")
+    if dense and not t.is_contiguous():
+        raise ValueError(f"{what} has to be contiguous")
+    return t.data_ptr()
+
+
+def _heads(t, what, like=None):
+    """fp16 [tokens][heads][dim], strides as they are along the first two."""
+    if t is None:
+        return tl_heads(None, 0, 0)
+    p = _wants(t, what, ("float16",), 3, False)
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"{what}: the dimensions of a head have to stand side by side")
+    if like is not None and t.shape != like:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(like)}")
+    return tl_heads(p, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
+
+
+def make_batch(seq_start, cached, seqs, tokens):
+    """seq_start: int32 [seqs + 1] or None (one token per sequence); cached: int32 [seqs] or None (0 for each)."""
+    b = tl_batch(None, None, seqs, tokens)
+    if seq_start is not None:
+        b.seq_start = _wants(seq_start, "seq_start", ("int32",), 1)
+        if seq_start.numel() != seqs + 1:
+            raise ValueError(f"seq_start has {seq_start.numel()} entries, not {seqs + 1}")
+    if cached is not None:
+        b.cached = _wants(cached, "cached", ("int32",), 1)
+        if cached.numel() != seqs:
+            raise ValueError(f"cached has {cached.numel()} entries, not {seqs}")
+    b.kept = (seq_start, cached)
+    return b
+
+
+def make_kv_cache(k, v, k_scale, v_scale, page_table, page_tokens, head_dim, kind=TL_KV_INT8):
+    """k, v: [pages][kv_heads][page_tokens * head_dim] of one byte each; k_scale, v_scale: float32 [pages][kv_heads][page_tokens / 16];
+    page_table: int32 [seqs][pages_per_seq]."""
+    types = ("int8", "uint8") if kind == TL_KV_INT8 else ("float8_e4m3fn", "uint8")
+    c = tl_kv_cache(_wants(k, "k", types, 3), _wants(v, "v", types, 3), _wants(k_scale, "k_scale", ("float32",), 3),
+                    _wants(v_scale, "v_scale", ("float32",), 3), _wants(page_table, "page_table", ("int32",), 2), k.shape[0], page_tokens,
+                    page_table.shape[1], k.shape[1], head_dim, kind)
+    if k.shape != v.shape or k.shape[2] != page_tokens * head_dim:
+        raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)}: [pages][kv_heads][{page_tokens} * {head_dim}] is wanted")
+    if k_scale.shape != v_scale.shape or tuple(k_scale.shape) != (k.shape[0], k.shape[1], page_tokens // 16):
+        raise ValueError(f"k_scale {tuple(k_scale.shape)} and v_scale {tuple(v_scale.shape)}: {(k.shape[0], k.shape[1], page_tokens // 16)} is wanted")
+    c.kept = (k, v, k_scale, v_scale, page_table)
+    return c
+
+
+def make_rope(table, rot_dim, pairs=False):
+    """table: float32 [positions][rot_dim] on the device, as tl_rope_table fills it."""
+    r = tl_rope(_wants(table, "table", ("float32",), 2), table.shape[0], rot_dim, int(bool(pairs)))
+    if table.shape[1] != rot_dim:
+        raise ValueError(f"table has rows of {table.shape[1]}, not {rot_dim}")
+    r.kept = table
+    return r
+
+
+def _tokens(t, batch, what):
+    if t.shape[0] != batch.tokens:
+        raise ValueError(f"{what} has {t.shape[0]} tokens, the batch {batch.tokens}")
+
+
+def _table_rows(cache, batch):
+    if cache.kept[4].shape[0] != batch.seqs:
+        raise ValueError(f"page_table has {cache.kept[4].shape[0]} sequences, the batch {batch.seqs}")
+
+
+def make_append_job(q, k, v, q_out, k_out, batch, cache=None, rope=None):
+    """q [tokens][q_heads][dim], k, v [tokens][kv_heads][dim]; any of q, k, v, q_out, k_out may be None where the call does without."""
+    some = q if q is not None else k
+    if some is None:
+        raise ValueError("neither q nor k")
+    j = tl_append_job(_heads(q, "q"), _heads(k, "k"), _heads(v, "v", None if k is None else k.shape), _heads(q_out, "q_out", None if q is None else q.shape),
+                      _heads(k_out, "k_out", None if k is None else k.shape), batch)
+    j.q_heads, j.kv_heads, j.head_dim = 0 if q is None else q.shape[1], 0 if k is None else k.shape[1], some.shape[2]
+    for t, what in ((q, "q"), (k, "k")):
+        if t is not None:
+            _tokens(t, batch, what)
+            if t.shape[2] != some.shape[2]:
+                raise ValueError("q and k have heads of different sizes")
+    if cache is not None:
+        _table_rows(cache, batch)
+        j.cache = ctypes.pointer(cache)
+    if rope is not None:
+        j.rope = ctypes.pointer(rope)
+    j.kept = (q, k, v, q_out, k_out, batch, cache, rope)
+    return j
+
+
+def tl_kv_append(job, stream=None):
+    _check(_lib.tl_kv_append(job, _stream(stream)), "tl_kv_append")
+
+
+def tl_attn_cached_workspace(seqs, tokens, q_heads, kv_heads, head_dim):
+    return int(_lib.tl_attn_cached_workspace(seqs, tokens, q_heads, kv_heads, head_dim))
+
+
+def make_cached_job(q, out, batch, cache, scale, longest, workspace):
+    """q, out [tokens][q_heads][dim]; workspace: uint8, tl_attn_cached_workspace bytes; longest: 0 if not known."""
+    _tokens(q, batch, "q")
+    _table_rows(cache, batch)
+    if q.shape[2] != cache.head_dim:
+        raise ValueError(f"q has heads of {q.shape[2]}, the cache of {cache.head_dim}")
+    j = tl_cached_job(_heads(q, "q"), _heads(out, "out", q.shape), batch, ctypes.pointer(cache), q.shape[1], scale, longest,
+                      _wants(workspace, "workspace", ("uint8",), 1), workspace.numel())
+    j.kept = (q, out, batch, cache, workspace)
+    return j
+
+
+def tl_attn_cached(job, stream=None):
+    _check(_lib.tl_attn_cached(job, _stream(stream)), "tl_attn_cached")
+
+
+def make_prompt_job(q, k, v, out, batch, scale):
+    """q, out [tokens][q_heads][dim], k, v [tokens][kv_heads][dim]."""
+    _tokens(q, batch, "q")
+    _tokens(k, batch, "k")
+    if q.shape[2] != k.shape[2]:
+        raise ValueError("q and k have heads of different sizes")
+    j = tl_prompt_job(_heads(q, "q"), _heads(k, "k"), _heads(v, "v", k.shape), _heads(out, "out", q.shape), batch, q.shape[1], k.shape[1],
+                      q.shape[2], scale)
+    j.kept = (q, k, v, out, batch)
+    return j
+
+
+def tl_attn_prompt(job, stream=None):
+    _check(_lib.tl_attn_prompt(job, _stream(stream)), "tl_attn_prompt")
 
 
 def tl_probe_copy(dst, src, nbytes, stream=None):
