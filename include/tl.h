@@ -276,7 +276,7 @@ tl_status tl_ternary_gemm_gs_grouped(const tl_gemm_gs_job* jobs, int64_t count, 
  * activations are fp16; softmax, sums and scales are fp32.
  *
  * A tensor of heads: element (token t, head h, dimension d) is the fp16 at ptr + t * token_stride + h * head_stride + d,
- * strides in elements, multiples of 8 and not negative, ptr 16-byte aligned.  So query, key and value may lie side by
+ * strides in elements, multiples of 8, not negative, below 2^24 from token to token and 2^40 from head to head; ptr 16-byte aligned.  So query, key and value may lie side by
  * side in the rows that one QKV product writes.
  */
 typedef struct tl_heads {
@@ -295,7 +295,7 @@ typedef struct tl_heads {
 typedef struct tl_batch {
     const int32_t* seq_start; /* device, [seqs + 1]; NULL: every sequence has one token (tokens == seqs)   */
     const int32_t* cached;    /* device, [seqs]; NULL: 0 for each                                          */
-    int64_t seqs, tokens;     /* 1 <= seqs < 2^20; 0 <= tokens < 2^30 (0: the call does nothing)           */
+    int64_t seqs, tokens;     /* 1 <= seqs < 2^20; 0 <= tokens < 2^23 (0: the call does nothing)           */
 } tl_batch;
 
 /*
@@ -420,7 +420,7 @@ tl_status tl_attn_cached(const tl_cached_job* job, void* stream);
  * Attention of whole prompts, causal: token i of a sequence sees tokens 0 .. i of the same sequence among this call's rows
  * (batch.cached is not read), with fp16 keys and values:
  *     out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j][g]) v[j][g],   g = h / (q_heads / kv_heads).
- * head_dim is a multiple of 16 up to 128.  An infinity or a NaN in a key or value shows in the tokens that see it and in no others.  out may be
+ * head_dim is a multiple of 16 up to 128; (seqs + tokens / 32) * q_heads is below 2^24.  An infinity or a NaN in a key or value shows in the tokens that see it and in no others.  out may be
  * q itself with the same strides, and may not overlap q, k or v otherwise.  Deterministic.
  */
 typedef struct tl_prompt_job {

@@ -8,12 +8,12 @@ namespace {
 
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// Strides up to 2^31 and 2^30 tokens: addresses stay within 62 bits.
+// 64 tokens of 2^24 elements each lie within the 32-bit offsets of the kernels.
 inline tl_status heads_status(const tl_heads& h, int64_t heads)
 {
     if (heads == 0) return TL_OK;
     if (!h.ptr) return TL_ERR_NULL;
-    const int64_t lim = int64_t(1) << 31;
+    const int64_t lim = int64_t(1) << 24;
     if (h.token_stride < 0 || h.head_stride < 0 || h.token_stride >= lim || h.head_stride >= (int64_t(1) << 40)) return TL_ERR_SHAPE;
     if (!aligned(h.ptr, 16) || h.token_stride % 8 != 0 || h.head_stride % 8 != 0) return TL_ERR_ALIGN;
     return TL_OK;
@@ -21,9 +21,12 @@ inline tl_status heads_status(const tl_heads& h, int64_t heads)
 
 inline Heads heads_of(const tl_heads& h) { return {static_cast<_Float16*>(h.ptr), h.token_stride, h.head_stride}; }
 
+// A grid holds fewer than 2^32 threads in a direction: 2^24 workgroups of 256.
+constexpr int64_t kMaxSeqs = int64_t(1) << 20, kMaxTokens = int64_t(1) << 23, kMaxGroups = int64_t(1) << 24;
+
 inline tl_status batch_status(const tl_batch& b)
 {
-    if (b.seqs < 1 || b.seqs >= (int64_t(1) << 20) || b.tokens < 0 || b.tokens >= (int64_t(1) << 30)) return TL_ERR_SHAPE;
+    if (b.seqs < 1 || b.seqs >= kMaxSeqs || b.tokens < 0 || b.tokens >= kMaxTokens) return TL_ERR_SHAPE;
     if (!b.seq_start && b.tokens != b.seqs) return TL_ERR_SHAPE;
     if (!aligned(b.seq_start, 4) || !aligned(b.cached, 4)) return TL_ERR_ALIGN;
     return TL_OK;
@@ -139,7 +142,7 @@ tl_status tl_kv_append(const tl_append_job* job, void* stream)
 
 size_t tl_attn_cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t head_dim)
 {
-    if (seqs < 1 || seqs >= (int64_t(1) << 20) || tokens < 0 || tokens >= (int64_t(1) << 30)) return 0;
+    if (seqs < 1 || seqs >= tl::kMaxSeqs || tokens < 0 || tokens >= tl::kMaxTokens) return 0;
     if (tl::heads_number_status(q_heads, kv_heads) != TL_OK || !tl::dim_ok(head_dim)) return 0;
     return tl::cached_workspace(seqs, tokens, q_heads, kv_heads, head_dim);
 }
@@ -173,6 +176,7 @@ tl_status tl_attn_prompt(const tl_prompt_job* job, void* stream)
     tl_status e = batch_status(j.batch);
     if (e != TL_OK || (e = heads_number_status(j.q_heads, j.kv_heads)) != TL_OK) return e;
     if (!dim_ok(j.head_dim)) return TL_ERR_SHAPE;
+    if ((j.batch.seqs + j.batch.tokens / 32) * j.q_heads >= kMaxGroups) return TL_ERR_SHAPE;
     if (!std::isfinite(j.scale)) return TL_ERR_VALUE;
     if ((e = heads_status(j.q, j.q_heads)) != TL_OK || (e = heads_status(j.k, j.kv_heads)) != TL_OK || (e = heads_status(j.v, j.kv_heads)) != TL_OK ||
         (e = heads_status(j.out, j.q_heads)) != TL_OK) return e;

@@ -293,11 +293,15 @@ __global__ __launch_bounds__(64 * kWaves, 2) void cached_kernel(CachedArgs a, Sh
                 }
             const float top = mx == -kInf ? -kInf : mx + lv;
             if (__any(mx > m[n] + kSlack || top > R[n] + kSlack)) {
-                float a1 = fmaxf(m[n], mx), a2 = fmaxf(R[n], top);
+                // each row by itself: what one row sees does not change how another is rounded
+                float a1 = mx, a2 = top;
                 a1 = fmaxf(a1, __shfl_xor(a1, 16));
                 a2 = fmaxf(a2, __shfl_xor(a2, 16));
                 a1 = fmaxf(a1, __shfl_xor(a1, 32));
                 a2 = fmaxf(a2, __shfl_xor(a2, 32));
+                const bool moves = a1 > m[n] + kSlack || a2 > R[n] + kSlack;
+                a1 = moves ? fmaxf(a1, m[n]) : m[n];
+                a2 = moves ? fmaxf(a2, R[n]) : R[n];
                 l[n] *= power(m[n] - finite(a1));
                 const float f = power(R[n] - finite(a2));
 #pragma unroll

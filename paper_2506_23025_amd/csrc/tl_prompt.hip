@@ -1,69 +1,257 @@
-// Causal attention over packed prompts: the plain kernel.  One wave per query row and head, 64 keys at a time.
+// Causal attention over packed prompts.
+//
+// A workgroup takes 32 * NW query rows of one head, a wave 32 of them, and walks the keys 64 at a time.  Keys and values go to LDS
+// by LDS-DMA (no registers), the next tile's while this one is worked on.  Products are v_mfma_f32_32x32x16_f16:
+//   scores  S^T = K Q^T: A = keys from LDS, B = queries, which stay in registers.  Lane (column q, half h) receives the scores of its query
+//           with keys 8 i + 4 h .. + 3, which packed to fp16 are the B operand of the second product as they stand
+//   output  O^T = V^T P^T: A = values by the transposing LDS read, in the same order of keys
+// so weights never leave the lane.  A row of LDS is a token's head; its 16-byte pieces are permuted by the token's number, so that both kinds of
+// reads (16 tokens at one piece, 4 tokens at 4 pieces) touch all banks evenly.
+// Softmax: powers of 2 relative to a row's reference, which moves only when a score is more than 2^8 beyond it (fp16 holds the weights all the same), so most tiles need
+// no exchange between lanes and no scaling of the sums.
+// Bound: the matrix pipes and, beside them, the softmax's vector instructions; two workgroups on a CU, so that one's products run beside the other's softmax.
 #include "tl_attn.hpp"
 
 namespace tl {
 namespace {
 
-__global__ __launch_bounds__(64) void prompt_kernel(PromptArgs a)
+constexpr float kInf = __builtin_inff();
+constexpr float kSlack = 8.0f;
+constexpr int kTile = 64;                 // keys
+
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+
+__device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
+__device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
+
+__device__ inline uint32_t lds_address(const void* p)
 {
-    const int lane = threadIdx.x, row = blockIdx.x, h = blockIdx.y, g = h / a.group, dim = a.dim;
-    int s = row;
-    if (a.b.start) {
-        int lo = 0, hi = a.b.seqs;
-        while (hi - lo > 1) {
-            const int mid = (lo + hi) >> 1;
-            if (a.b.start[mid] <= row) lo = mid; else hi = mid;
+    return uint32_t(reinterpret_cast<uintptr_t>((const __attribute__((address_space(3))) void*)p));
+}
+
+// 16 bytes a lane from base + off to LDS, the lanes' side by side.
+__device__ inline void transfer(const void* base, uint32_t off, uint32_t lds)
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+}
+
+// Where piece c (16 bytes) of token r stands in its row.
+template <int DP>
+__device__ inline int piece(int r, int c)
+{
+    if constexpr (DP == 128) return c ^ (((r & 3) << 2) | ((r >> 2) & 3));
+    else return c ^ ((((r >> 1) & 1) << 2) | ((r >> 2) & 3));
+}
+
+template <int DP, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
+{
+    constexpr int kRow = DP * 2, kPieces = DP / 8, kBytes = kTile * kRow;
+    constexpr int kSteps = kBytes / (NW * 1024);             // transfers of a wave for keys, and as many for values
+    constexpr int kRows1 = 1024 / kRow;                      // tokens of a transfer
+    constexpr int KK = DP / 16, DT = DP / 32;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kBytes];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5;
+
+    // heads that share keys go to one chiplet (workgroups are dealt to the 8 of them in turn); the rows with most keys first
+    int h = int(blockIdx.x) % a.q_heads;
+    const int item = int(gridDim.x) / a.q_heads - 1 - int(blockIdx.x) / a.q_heads;
+    if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads >> 3) + (h >> 3);
+    Item it{item, 0};
+    if (a.b.start) it = find_item(a.b, item, 32 * NW, 1);
+    const int seq = __builtin_amdgcn_readfirstlane(it.seq);
+    if (seq < 0) return;
+    const Span sp = span(a.b, seq);
+    const int n = __builtin_amdgcn_readfirstlane(sp.n), first = __builtin_amdgcn_readfirstlane(sp.first);
+    const int q0 = __builtin_amdgcn_readfirstlane(it.i) * (32 * NW);
+    if (q0 >= n) return;
+    const int g = h / a.group;
+    const int row0 = q0 + wave * 32, row = row0 + l32;       // this lane's query in the sequence
+    const int pieces = a.dim >> 3;
+    const bool flip = a.scale < 0.0f;
+    const float scale = fabsf(a.scale);
+
+    f16x8 q[KK];
+    {
+        const _Float16* from = a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head;
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+            const int c = 2 * k + half;
+            f16x8 x = *reinterpret_cast<const f16x8*>(from + (c < pieces ? c : 0) * 8);
+            if (c >= pieces) x = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+            if (flip) x = -x;
+            q[k] = x;
         }
-        s = lo;
     }
-    const Span sp = span(a.b, s);
-    if (row < sp.first || row >= sp.first + sp.n) return;
-    __shared__ float q[128], p[64];
-    for (int d = lane; d < dim; d += 64) q[d] = float(a.q.p[int64_t(row) * a.q.token + int64_t(h) * a.q.head + d]);
+
+    if (pieces < kPieces) {                                  // dimensions beyond the head are never transferred
+        for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 64 * NW) reinterpret_cast<u32x4*>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    const int most = q0 + 32 * NW < n ? q0 + 32 * NW : n;    // keys that the workgroup sees
+    const int tiles = (most + kTile - 1) / kTile;
+    const char* const kbase = reinterpret_cast<const char*>(a.k.p + int64_t(first) * a.k.token + int64_t(g) * a.k.head);
+    const char* const vbase = reinterpret_cast<const char*>(a.v.p + int64_t(first) * a.v.token + int64_t(g) * a.v.head);
+    const uint32_t kstride = uint32_t(a.k.token) * 2u, vstride = uint32_t(a.v.token) * 2u;
+    const uint32_t lds0 = lds_address(&lds[0][0][0]) + wave * kSteps * 1024;
+    auto fetch = [&](int t, int buf) {
+        const char* const kb = kbase + int64_t(t) * kTile * kstride;
+        const char* const vb = vbase + int64_t(t) * kTile * vstride;
+        const int last = n - 1 - t * kTile;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            int r = (wave * kSteps + i) * kRows1 + lane / kPieces;
+            const int c = piece<DP>(r, lane % kPieces);
+            if (r > last) r = last;                          // tokens behind the sequence: masked, but no NaN that is not there
+            if (c < pieces) {
+                transfer(kb, uint32_t(r) * kstride + c * 16, lds0 + buf * 2 * kBytes + i * 1024);
+                transfer(vb, uint32_t(r) * vstride + c * 16, lds0 + (buf * 2 + 1) * kBytes + i * 1024);
+            }
+        }
+    };
+
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = -kInf, l = 0.0f;
+
+    fetch(0, 0);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
-    const _Float16* k = a.k.p + int64_t(sp.first) * a.k.token + int64_t(g) * a.k.head;
-    const _Float16* v = a.v.p + int64_t(sp.first) * a.v.token + int64_t(g) * a.v.head;
-    float m = -__builtin_inff(), l = 0.0f, o0 = 0.0f, o1 = 0.0f;
-    const int len = row - sp.first + 1;
-    for (int t0 = 0; t0 < len; t0 += 64) {
-        const int t = t0 + lane;
-        float x = -__builtin_inff();
-        if (t < len) {
-            float sum = 0.0f;
-            for (int d = 0; d < dim; ++d) sum += q[d] * float(k[int64_t(t) * a.k.token + d]);
-            x = sum * a.scale;
+    for (int t = 0; t < tiles; ++t) {
+        const int buf = t & 1;
+        if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
+        if (t * kTile <= row0 + 31) {                        // else no row of this wave sees the tile
+            const unsigned char* const kt = lds[buf][0];
+            const unsigned char* const vt = lds[buf][1];
+            const bool masked = t * kTile + kTile - 1 > row0;
+            f32x16 s[2];
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+                for (int k = 0; k < KK; ++k) {
+                    const int r = b * 32 + l32;
+                    const f16x8 x = *reinterpret_cast<const f16x8*>(kt + r * kRow + piece<DP>(r, 2 * k + half) * 16);
+                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[k], s[b], 0, 0, 0);
+                }
+            }
+            const int seen = row - t * kTile - 4 * half;     // key 32 b + 8 (i / 4) + 4 half + i % 4 is seen up to the row's own number
+            if (masked) {
+#pragma unroll
+                for (int b = 0; b < 2; ++b)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (32 * b + 8 * (i >> 2) + (i & 3) > seen) s[b][i] = -kInf;
+            }
+            float mx = -kInf;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+            mx = mx == -kInf ? mx : mx * scale;
+            if (__any(mx > m + kSlack)) {
+                // each row by itself: what one row sees does not change how another is rounded
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                const float to = mx > m + kSlack ? mx : m;
+                const float f = power(m - finite(to));
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] *= f;
+                m = to;
+            }
+            const float mb = finite(m);
+            f16x8 w[4];
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    float p = power(__builtin_fmaf(s[b][i], scale, -mb));
+                    if (masked && 32 * b + 8 * (i >> 2) + (i & 3) > seen) p = 0.0f;
+                    l += p;
+                    w[b * 2 + (i >> 3)][i & 7] = _Float16(p);
+                }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {                    // 16 keys
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    union { f16x8 v; i16x4 h[2]; uint16_t b[8]; } x;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const int r = u * 16 + e * 8 + half * 4 + ((lane & 15) >> 2);
+                        const int c = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+                        x.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                            (lds_i16x4*)(vt + r * kRow + piece<DP>(r, c) * 16 + (lane & 1) * 8));
+                    }
+                    if (masked) {
+                        // A weight of 0 does not take an infinity or a NaN out of a sum: they are left out here, and added for the rows that see them.
+                        bool odd = false;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) odd |= (x.b[i] & 0x7c00) == 0x7c00;
+                        if (__any(odd)) {
+                            const int key = u * 16 + 0;
+                            f16x8 sees, up, down, bad;
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) {
+                                const uint16_t v = x.b[i];
+                                sees[i] = key + 8 * (i >> 2) + (i & 3) > seen ? _Float16(0.0f) : _Float16(1.0f);
+                                up[i] = v == 0x7c00 ? _Float16(1.0f) : _Float16(0.0f);
+                                down[i] = v == 0xfc00 ? _Float16(1.0f) : _Float16(0.0f);
+                                bad[i] = (v & 0x7fff) > 0x7c00 ? _Float16(1.0f) : _Float16(0.0f);
+                                if ((v & 0x7c00) == 0x7c00) x.b[i] = 0;
+                            }
+#pragma unroll 1
+                            for (int kind = 0; kind < 3; ++kind) {
+                                f32x16 c;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) c[i] = 0.0f;
+                                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(kind == 0 ? up : kind == 1 ? down : bad, sees, c, 0, 0, 0);
+                                const float v = kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[d][i] += c[i] > 0.0f ? v : 0.0f;
+                            }
+                        }
+                    }
+                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.v, w[u], o[d], 0, 0, 0);
+                }
+            }
         }
-        float mx = x;
-        for (int i = 32; i; i >>= 1) mx = fmaxf(mx, __shfl_xor(mx, i));
-        const float now = fmaxf(m, mx), base = now == -__builtin_inff() ? 0.0f : now;
-        const float r = exp2f(m - base), e = t < len ? exp2f(x - base) : 0.0f;
-        float sum = e;
-        for (int i = 32; i; i >>= 1) sum += __shfl_xor(sum, i);
-        m = now;
-        l = l * r + sum;
-        o0 *= r;
-        o1 *= r;
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
-        p[lane] = e;
-        __syncthreads();
-        for (int i = 0; i < 64 && t0 + i < len; ++i) {
-            const _Float16* vi = v + int64_t(t0 + i) * a.v.token;
-            if (lane < dim) o0 += p[i] * float(vi[lane]);
-            if (lane + 64 < dim) o1 += p[i] * float(vi[lane + 64]);
-        }
     }
+
+    l += __shfl_xor(l, 32);
     const float f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-    _Float16* out = a.out.p + int64_t(row) * a.out.token + int64_t(h) * a.out.head;
-    if (lane < dim) out[lane] = _Float16(o0 * f);
-    if (lane + 64 < dim) out[lane + 64] = _Float16(o1 * f);
+    if (row < n) {
+        _Float16* out = a.out.p + int64_t(first + row) * a.out.token + int64_t(h) * a.out.head;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int at = d * 32 + i * 8 + half * 4;
+                if (at >= a.dim) continue;
+                f16x4 y;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = _Float16(o[d][i * 4 + j] * f);
+                *reinterpret_cast<f16x4*>(out + at) = y;
+            }
+    }
 }
 
 }  // namespace
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
 {
-    const dim3 grid(unsigned(a.b.tokens), unsigned(a.q_heads));
-    prompt_kernel<<<grid, 64, 0, s>>>(a);
+    constexpr int NW = 4;
+    const int64_t items = a.b.start ? a.b.tokens / (32 * NW) + a.b.seqs : a.b.seqs;
+    const unsigned grid = unsigned(items * a.q_heads);
+    if (a.dim <= 64) prompt_kernel<64, NW><<<grid, 64 * NW, 0, s>>>(a);
+    else prompt_kernel<128, NW><<<grid, 64 * NW, 0, s>>>(a);
     return hipGetLastError();
 }
 
