@@ -102,13 +102,15 @@ __device__ inline Item find_item(const Batch& b, int item, int per, int extra)
     return {lo, item - base};
 }
 
-// Page of a block of 16 tokens of sequence s, or -1.
+// Page of a block of 16 tokens of sequence s, or -1.  Without a branch: lanes ask for different blocks, and matrix instructions have to find them all together.
 __device__ inline int page_of(const Cache& c, int s, int64_t block)
 {
-    const int64_t i = block >> c.page_shift;
-    if (i >= c.pages_per_seq) return -1;
-    const int p = c.table[int64_t(s) * c.pages_per_seq + i];
-    return p >= 0 && p < c.pages ? p : -1;
+    const int64_t i = block >> c.page_shift, last = c.pages_per_seq - 1;
+    const int p = c.table[int64_t(s) * c.pages_per_seq + (i < last ? i : last)];
+    return i <= last && p >= 0 && p < c.pages ? p : -1;
 }
+
+// A value that all lanes have, in a scalar register.
+__device__ inline int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 }  // namespace tl

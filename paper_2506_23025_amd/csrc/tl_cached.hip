@@ -10,16 +10,19 @@
 // Softmax: weights p = 2^(x - m) are summed as they are, and reach the product as p * scale_v relative to a second running reference
 // R = max(x + log2 scale_v), so that their fp16 form (2^-11) is exact enough whatever the scales of the blocks are.  The references move only when a score
 // is more than 2^8 beyond them, so a tile needs no exchange between lanes.
-// Bound: memory.  A sequence's tiles are dealt to the 4 waves of a workgroup, and long ones to several workgroups, in parts whose size
-// follows from the whole call's work (read on the device, so that one captured launch serves every length); a second kernel joins them.
+// Bound: memory.  Short caches: a workgroup takes a row tile, its 4 waves deal the tiles among themselves and join their sums in LDS.  Otherwise the tiles of the whole
+// call stand in one row, sequence after sequence, and every wave of a grid that fills the chip once takes an equal piece of it, whatever the sequences' lengths; they are
+// read on the device, so one captured launch serves every step.  Pieces of row tiles that several waves share meet in a second kernel.
 #include "tl_attn.hpp"
+
+#include <type_traits>
 
 namespace tl {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kParts = 2048;              // workgroups that a call's work is cut into, about
-constexpr int kLeast = 16;                // tiles of a part at least: below this the second kernel costs more than the parts save
+constexpr int kPieces = 2048;             // waves that share a call's tiles: two on each SIMD of 256 CUs
+constexpr int kAlone = 16;                // up to so many tiles a sequence is left to one workgroup: the second kernel would cost more than it saves
 
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;            // log2 of how far a weight may pass its reference (fp16 holds 2^15)
@@ -29,28 +32,29 @@ struct Shape {
     int heads;                            // query heads of a row tile
     int subs;                             // row tiles that the query heads of a key head need
     int rows;                             // per * heads
-    int parts;                            // of the call, for one of kv_heads * subs
-    int64_t metas;                        // row tiles of the call at most
+    int nr;                               // blocks of 16 rows in a row tile
+    int64_t tiles;                        // row tiles of the call at most
 };
 
-inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group, int kv_heads, int nr)
+inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group)
 {
     Shape p;
-    const int most = 16 * nr;
+    // two blocks of 16 rows share the widened codes where the tokens of a sequence fill them
+    p.nr = tokens * group > 16 * seqs && !one ? 2 : 1;
+    const int most = 16 * p.nr;
     p.heads = group < most ? group : most;
     p.subs = (group + p.heads - 1) / p.heads;
     p.per = one ? 1 : most / p.heads;
     p.rows = p.per * p.heads;
-    p.parts = kParts / (kv_heads * p.subs);
-    if (p.parts < 1) p.parts = 1;
-    p.metas = one ? seqs : tokens / p.per + seqs;
+    p.tiles = one ? seqs : tokens / p.per + seqs;
     return p;
 }
 
 constexpr int kExtra = 4;                 // floats beside a row's sums: m, l, R
 
-// Eight codes as fp16, in order.
-template <bool FP8>
+// Eight codes as fp16, in order; with RAISED (whole numbers only) 1152 more than they are.
+constexpr float kRaise = 1152.0f;
+template <bool FP8, bool RAISED = false>
 __device__ inline f16x8 widen(uint32_t a, uint32_t b)
 {
     union { f16x8 v; f16x2 p[4]; uint32_t w[4]; } r;
@@ -67,14 +71,17 @@ __device__ inline f16x8 widen(uint32_t a, uint32_t b)
         r.w[1] = __builtin_amdgcn_perm(0x64646464u, a, 0x04030402u);
         r.w[2] = __builtin_amdgcn_perm(0x64646464u, b, 0x04010400u);
         r.w[3] = __builtin_amdgcn_perm(0x64646464u, b, 0x04030402u);
-        const f16x2 c = {_Float16(1152.0f), _Float16(1152.0f)};
+        if constexpr (!RAISED) {
+            const f16x2 c = {_Float16(kRaise), _Float16(kRaise)};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.p[i] -= c;
+            for (int i = 0; i < 4; ++i) r.p[i] -= c;
+        }
     }
     return r.v;
 }
 
 __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
+__device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // Tiles and row tiles of a sequence.
@@ -90,380 +97,555 @@ __device__ inline Need need_of(const CachedArgs& a, const Shape& p, int s)
     return {int((len + 63) >> 6), (sp.n + p.per - 1) / p.per};
 }
 
-// What a workgroup does: tiles [chunk * size, ...) of row tile rt of sequence seq.
-struct Part { int seq, rt, chunk, chunks, size, slot; };
-
-__device__ inline int ceil_div(int a, int b) { return int((unsigned(a) + unsigned(b) - 1u) / unsigned(b)); }
-
-__device__ inline Part find_part(const CachedArgs& a, const Shape& p, int item)
+// Sums over the wave, exact: whole numbers below 2^53 in doubles.
+template <int CTRL, int ROWS>
+__device__ inline double moved(double x)
 {
-    const int lane = threadIdx.x & 63;
-    int lo = 0, count = a.b.seqs, per = (count + 63) >> 6;
-    float work = 0.0f;
-    for (int i = 0; i < per; ++i) {
-        const int s = lane * per + i;
-        if (s < count) {
-            const Need n = need_of(a, p, s);
-            work += float(n.tiles) * float(n.rts);
-        }
-    }
-    for (int k = 32; k; k >>= 1) work += __shfl_xor(work, k);
-    int size = int(fminf(work * 1.0001f / float(p.parts), 1e9f)) + 1;
-    if (size < kLeast) size = kLeast;
-    int before = 0, slots = 0;
-    while (true) {
-        int items = 0, cut = 0;
-        for (int i = 0; i < per; ++i) {
-            const int s = lo + lane * per + i;
-            if (lane * per + i < count) {
-                const Need n = need_of(a, p, s);
-                const int c = n.tiles ? ceil_div(n.tiles, size) : 1;
-                items += n.rts * c;
-                if (c > 1) cut += n.rts * c;
-            }
-        }
-        int items_to = items, cut_to = cut;
-        for (int k = 1; k < 64; k <<= 1) {
-            const int x = __shfl_up(items_to, k), y = __shfl_up(cut_to, k);
-            if (lane >= k) { items_to += x; cut_to += y; }
-        }
-        const uint64_t there = __ballot(before + items_to > item);
-        if (!there) return {-1, 0, 0, 0, 0, 0};
-        const int owner = __builtin_ctzll(there);
-        before += __builtin_amdgcn_readlane(items_to, owner) - __builtin_amdgcn_readlane(items, owner);
-        slots += __builtin_amdgcn_readlane(cut_to, owner) - __builtin_amdgcn_readlane(cut, owner);
-        lo += owner * per;
-        count = count - owner * per < per ? count - owner * per : per;
-        if (per == 1) break;
-        per = (count + 63) >> 6;
-    }
-    const Need n = need_of(a, p, lo);
-    const int chunks = n.tiles ? ceil_div(n.tiles, size) : 1, i = item - before, rt = i / chunks;
-    return {lo, rt, i - rt * chunks, chunks, size, chunks > 1 ? slots + i : -1};
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, int(uint32_t(b)), CTRL, ROWS, 15, true);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(uint32_t(b >> 32)), CTRL, ROWS, 15, true);
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
 
-// The sums of one row from several parts; `get(i)` gives {m, l, R} of part i.
+__device__ inline double scanned(double x)
+{
+    x += moved<0x111, 15>(x);             // from the lane 1, 2, 4 and 8 before in the row of 16
+    x += moved<0x112, 15>(x);
+    x += moved<0x114, 15>(x);
+    x += moved<0x118, 15>(x);
+    x += moved<0x142, 10>(x);             // a row's last lane to the next row, rows 1 and 3
+    x += moved<0x143, 12>(x);             // lane 31 to rows 2 and 3
+    return x;
+}
+
+__device__ inline double of_lane(double x, int lane)
+{
+    const uint64_t b = __builtin_bit_cast(uint64_t, x);
+    const uint32_t lo = __builtin_amdgcn_readlane(int(uint32_t(b)), lane), hi = __builtin_amdgcn_readlane(int(uint32_t(b >> 32)), lane);
+    return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
+}
+
+// The call's tiles in one row: sequence after sequence, of each the key heads' row tiles one after the other, `units` of them with `tiles` tiles each.
+__device__ inline double share_of(const CachedArgs& a, const Shape& p, int s, int ys)
+{
+    const Need n = need_of(a, p, s);
+    return double(n.tiles) * double(n.rts) * double(ys);
+}
+
+__device__ inline double all_tiles(const CachedArgs& a, const Shape& p, int ys)
+{
+    const int lane = threadIdx.x & 63, per = (a.b.seqs + 63) >> 6;
+    double w = 0.0;
+    for (int i = 0; i < per; ++i)
+        if (lane * per + i < a.b.seqs) w += share_of(a, p, lane * per + i, ys);
+    return of_lane(scanned(w), 63);
+}
+
+// The sequence that holds tile x of the row, and how many tiles stand before it.
+struct Found { int seq; double before; };
+__device__ inline Found find_tile(const CachedArgs& a, const Shape& p, double x, int ys)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, count = a.b.seqs;
+    double before = 0.0;
+    while (true) {
+        const int per = (count + 63) >> 6;
+        double w = 0.0;
+        for (int i = 0; i < per; ++i)
+            if (lane * per + i < count) w += share_of(a, p, lo + lane * per + i, ys);
+        const double to = scanned(w);
+        const uint64_t there = __ballot(before + to > x);
+        if (!there) return {-1, 0.0};
+        const int owner = __builtin_ctzll(there);
+        before += of_lane(to, owner) - of_lane(w, owner);
+        lo += owner * per;
+        count = count - owner * per < per ? count - owner * per : per;
+        if (per == 1) return {lo, before};
+    }
+}
+
+// First tile of piece i, of `all` tiles: equal shares, or one each where there are fewer tiles than waves.
+__device__ inline double piece_begin(double all, int i)
+{
+    if (all <= kPieces) return fmin(double(i), all);
+    return floor(all * double(i) * (1.0 / kPieces));
+}
+
+// The piece that holds tile x.
+__device__ inline int piece_of(double all, double x)
+{
+    if (all <= kPieces) return int(x);
+    int i = int((x + 1.0) * kPieces / all);
+    if (i > kPieces - 1) i = kPieces - 1;
+    while (i > 0 && piece_begin(all, i) > x) --i;
+    while (i < kPieces - 1 && piece_begin(all, i + 1) <= x) ++i;
+    return i;
+}
+
 struct Row { float m, l, R; };
 
-template <bool FP8, int CH, int NR, bool SPLIT>
-__global__ __launch_bounds__(64 * kWaves, 2) void cached_kernel(CachedArgs a, Shape p)
+// Where the parts of a row tile of a key head are: in the pieces from w0 on, so many of them.
+struct Parts { int w0, n; };
+__device__ inline Parts* parts_of(const CachedArgs& a, const Shape& p, int dp)
 {
-    constexpr int J = (CH + 3) / 4, DP = CH * 16;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int m16 = lane & 15, g = lane >> 4;
-    Part part{int(blockIdx.x), 0, 0, 1, 1 << 30, -1};
-    if constexpr (SPLIT) {
-        part = find_part(a, p, int(blockIdx.x));
-    } else if (a.b.start) {
-        const Item it = find_item(a.b, int(blockIdx.x), p.per, 1);
-        part.seq = it.seq;
-        part.rt = it.i;
-    }
-    if (part.seq < 0) return;
-    const Span sp = span(a.b, part.seq);
-    const int past = cached_of(a.b, part.seq);
-    const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
-    const int first = part.rt * p.per;                    // the row tile's first token in the sequence
-    if (first >= sp.n) return;
-    const int tokens = sp.n - first < p.per ? sp.n - first : p.per;
-    const int heads = a.group - sub * p.heads < p.heads ? a.group - sub * p.heads : p.heads;
-    const int rows = tokens * p.heads;                    // those of heads beyond the group are computed and dropped
-    const int chunks_dim = a.c.dim >> 4;
+    return reinterpret_cast<Parts*>(a.part + int64_t(2 * kPieces) * p.rows * (dp + kExtra));
+}
 
-    // queries: row r is token r / p.heads, head r % p.heads; positions a row sees
+// One row tile of one key head: its queries, and its sums over tiles begin, begin + step, ... below end.
+// NB tiles are in registers or on their way to them.  EXACT: the head has CH * 16 dimensions, else fewer.
+template <bool FP8, int CH, bool EXACT, int NR, int NB>
+struct Walk {
+    static constexpr int J = (CH + 3) / 4;
     f16x8 q[NR][J][2];
-    int64_t sees[NR];
-    int64_t least = int64_t(1) << 40, most = 0;
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        const int r = n * 16 + m16, t = r / p.heads, h = r - t * p.heads;
-        const bool there = r < rows && h < heads;
-        sees[n] = past >= 0 ? int64_t(past) + first + (there ? t : 0) + 1 : 0;
-        const _Float16* from = a.q.p + int64_t(sp.first + first + (there ? t : 0)) * a.q.token + int64_t(head * a.group + sub * p.heads + (there ? h : 0)) * a.q.head;
-#pragma unroll
-        for (int j = 0; j < J; ++j) {
-            const int c = 4 * j + g;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                f16x8 x = *reinterpret_cast<const f16x8*>(from + (c < chunks_dim ? c : 0) * 16 + i * 8);
-                if (c >= chunks_dim) x = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
-                q[n][j][i] = x;
-            }
-        }
-        least = sees[n] < least ? sees[n] : least;
-        most = sees[n] > most ? sees[n] : most;
-    }
-    for (int k = 8; k; k >>= 1) {
-        const int64_t x = __shfl_xor(least, k), y = __shfl_xor(most, k);
-        least = x < least ? x : least;
-        most = y > most ? y : most;
-    }
-    // tiles of this part that some row sees
-    int end = int((most + 63) >> 6);
-    {
-        const int64_t to = (int64_t(part.chunk) + 1) * part.size;
-        if (to < end) end = int(to);
-    }
-    const int begin = part.chunk * (SPLIT ? part.size : 0);
-
+    int64_t sees[NR], least, most;        // positions that this lane's rows see; the fewest and most of the tile
     f32x4 o[NR][CH];
     float m[NR], l[NR], R[NR];
-#pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        m[n] = -kInf;
-        R[n] = -kInf;
-        l[n] = 0.0f;
-#pragma unroll
-        for (int d = 0; d < CH; ++d) o[n][d] = f32x4{0, 0, 0, 0};
-    }
+    float from[NR];                       // where a score's sum begins: it takes off what the raised keys add
+    int first, tokens, heads, rows;       // tokens of the sequence before the tile, tokens and heads in it
 
-    const int64_t block_bytes = int64_t(16) * a.c.dim, blocks = int64_t(1) << a.c.page_shift;
-    const int in_page = int(blocks - 1);
-    auto page_at = [&](int64_t block) { return page_of(a.c, part.seq, block); };
-    auto place = [&](int page, int64_t block) { return (int64_t(page < 0 ? 0 : page) * a.c.kv_heads + head) * blocks + (block & in_page); };
-
-    u32x4 kw[4][J], vw[CH];
-    float ks = 0.0f, vs = 0.0f;
-    int page_k = -1, page_v = -1, next_k = -1, next_v = -1;
-    auto load_k = [&](int tile) {
-        const uint8_t* from = a.c.k + place(page_k, int64_t(tile) * 4 + (m16 >> 2)) * block_bytes + (m16 & 3) * 16;
-#pragma unroll
-        for (int b = 0; b < 4; ++b)
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const int c = 4 * j + g < chunks_dim ? 4 * j + g : 0;
-                kw[b][j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + (b * chunks_dim + c) * 64));
-            }
-    };
-    auto load_v = [&](int tile) {
-        const int64_t at = place(page_v, int64_t(tile) * 4 + g);
-        const uint8_t* from = a.c.v + at * block_bytes + m16 * 16;
-#pragma unroll
-        for (int d = 0; d < CH; ++d) vw[d] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(from + (d < chunks_dim ? d : 0) * 256));
-        ks = a.c.ks[at];
-        vs = a.c.vs[at];
-    };
-
-    int tile = begin + wave;
-    if (tile < end) {
-        page_k = page_at(int64_t(tile) * 4 + (m16 >> 2));
-        page_v = page_at(int64_t(tile) * 4 + g);
-        load_k(tile);
-        load_v(tile);
-        next_k = page_at(int64_t(tile + kWaves) * 4 + (m16 >> 2));
-        next_v = page_at(int64_t(tile + kWaves) * 4 + g);
-    }
-    for (; tile < end; tile += kWaves) {
-        const bool more = tile + kWaves < end;
-        const bool masked = int64_t(tile) * 64 + 64 > least || !__all(page_v >= 0);
-        const bool there = page_v >= 0;
-        const float ksc = ks * a.scale, vsc = vs;
-        f32x4 s[NR][4];
-#pragma unroll
-        for (int b = 0; b < 4; ++b) {
-#pragma unroll
-            for (int n = 0; n < NR; ++n) s[n][b] = f32x4{0, 0, 0, 0};
-#pragma unroll
-            for (int j = 0; j < J; ++j) {
-                const f16x8 k0 = widen<FP8>(kw[b][j][0], kw[b][j][1]), k1 = widen<FP8>(kw[b][j][2], kw[b][j][3]);
-#pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][j][0], s[n][b], 0, 0, 0);
-                    s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][j][1], s[n][b], 0, 0, 0);
-                }
-            }
-        }
-        if (more) {
-            page_k = next_k;
-            load_k(tile + kWaves);
-        }
-        const float lv = __builtin_amdgcn_logf(vsc);
-        f16x8 w[NR][2];
+    __device__ inline void start(const CachedArgs& a, const Shape& p, const Span& sp, int past, int rt, int head, int sub)
+    {
+        const int m16 = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4, chunks = EXACT ? CH : a.c.dim >> 4;
+        first = rt * p.per;
+        tokens = sp.n - first < p.per ? sp.n - first : p.per;
+        heads = a.group - sub * p.heads < p.heads ? a.group - sub * p.heads : p.heads;
+        rows = tokens * p.heads;                             // those of heads beyond the group are computed and dropped
+        least = past < 0 ? 0 : int64_t(past) + first + 1;
+        most = past < 0 ? 0 : int64_t(past) + first + tokens;
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
-            float mx = -kInf;
+            // row r is token r / p.heads, head r % p.heads
+            const int r = n * 16 + m16, tr = r / p.heads, hr = r - tr * p.heads;
+            const bool there = r < rows && hr < heads;
+            const int t = there ? tr : 0, h = there ? hr : 0;
+            sees[n] = past < 0 ? 0 : int64_t(past) + first + t + 1;
+            const _Float16* row = a.q.p + int64_t(sp.first + first + t) * a.q.token + int64_t(head * a.group + sub * p.heads + h) * a.q.head;
+            float sum = 0.0f;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
+            for (int j = 0; j < J; ++j)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    float x = s[n][b][r] * ksc;
-                    if (masked && !(there && int64_t(tile) * 64 + g * 16 + b * 4 + r < sees[n])) x = -kInf;
-                    s[n][b][r] = x;
-                    mx = fmaxf(mx, x);
+                for (int i = 0; i < 2; ++i) {
+                    const int c = 4 * j + g;
+                    f16x8 x = *reinterpret_cast<const f16x8*>(row + (c < chunks ? c : 0) * 16 + i * 8);
+                    if (c >= chunks) x = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+                    if (a.scale < 0.0f) x = -x;              // so that the largest sum is the largest score
+                    q[n][j][i] = x;
+                    if constexpr (!FP8) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) sum += float(x[e]);
+                    }
                 }
-            const float top = mx == -kInf ? -kInf : mx + lv;
-            if (__any(mx > m[n] + kSlack || top > R[n] + kSlack)) {
-                // each row by itself: what one row sees does not change how another is rounded
-                float a1 = mx, a2 = top;
-                a1 = fmaxf(a1, __shfl_xor(a1, 16));
-                a2 = fmaxf(a2, __shfl_xor(a2, 16));
-                a1 = fmaxf(a1, __shfl_xor(a1, 32));
-                a2 = fmaxf(a2, __shfl_xor(a2, 32));
-                const bool moves = a1 > m[n] + kSlack || a2 > R[n] + kSlack;
-                a1 = moves ? fmaxf(a1, m[n]) : m[n];
-                a2 = moves ? fmaxf(a2, R[n]) : R[n];
-                l[n] *= power(m[n] - finite(a1));
-                const float f = power(R[n] - finite(a2));
-#pragma unroll
-                for (int d = 0; d < CH; ++d) o[n][d] *= f;
-                m[n] = a1;
-                R[n] = a2;
+            if constexpr (!FP8) {
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
             }
-            const float mb = finite(m[n]);
-            // p * scale_v relative to R
-            float f = power(fminf(lv + mb - finite(R[n]), 126.0f));
-            if (!(vsc == vsc)) f = vsc;
-            union { f16x8 v[2]; _Float16 h[16]; } u;
+            from[n] = -kRaise * sum;
+            m[n] = -kInf;
+            R[n] = -kInf;
+            l[n] = 0.0f;
 #pragma unroll
-            for (int b = 0; b < 4; ++b)
-#pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    const float x = power(s[n][b][r] - mb);
-                    l[n] += x;
-                    float y = x * f;
-                    if (masked && s[n][b][r] == -kInf) y = 0.0f;
-                    u.h[b * 4 + r] = _Float16(y);
-                }
-            w[n][0] = u.v[0];
-            w[n][1] = u.v[1];
-        }
-#pragma unroll
-        for (int d = 0; d < CH; ++d) {
-            const f16x8 v0 = widen<FP8>(vw[d][0], vw[d][1]), v1 = widen<FP8>(vw[d][2], vw[d][3]);
-#pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[n][0], o[n][d], 0, 0, 0);
-                o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[n][1], o[n][d], 0, 0, 0);
-            }
-        }
-        if (more) {
-            page_v = next_v;
-            load_v(tile + kWaves);
-            next_k = page_at(int64_t(tile + 2 * kWaves) * 4 + (m16 >> 2));
-            next_v = page_at(int64_t(tile + 2 * kWaves) * 4 + g);
+            for (int d = 0; d < CH; ++d) o[n][d] = f32x4{0, 0, 0, 0};
         }
     }
 
-    // the four waves' sums of a row
+    __device__ inline void walk(const CachedArgs& a, int seq, int head, int begin, int end, int step)
+    {
+        const int m16 = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4, chunks = EXACT ? CH : a.c.dim >> 4;
+        const float scale = fabsf(a.scale);
+        const int64_t block_bytes = int64_t(256) * chunks, blocks = int64_t(1) << a.c.page_shift;
+        const int in_page = int(blocks - 1);
+        auto page_at = [&](int64_t block) { return page_of(a.c, seq, block); };
+        auto place = [&](int page, int64_t block) { return (int64_t(page < 0 ? 0 : page) * a.c.kv_heads + head) * blocks + (block & in_page); };
+        u32x4 kw[NB][4][J], vw[NB][CH];
+        float ks[NB], vs[NB];
+        int page_v[NB], next_k = -1, next_v = -1;
+        auto ask_pages = [&](int tile) {
+            next_k = page_at(int64_t(tile) * 4 + (m16 >> 2));
+            next_v = page_at(int64_t(tile) * 4 + g);
+        };
+        auto load_k = [&](int tile, int at) {
+            const uint8_t* from = a.c.k + place(next_k, int64_t(tile) * 4 + (m16 >> 2)) * block_bytes + (m16 & 3) * 16;
+#pragma unroll
+            for (int b = 0; b < 4; ++b)
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const int c = EXACT || 4 * j + g < chunks ? 4 * j + g : 0;
+                    kw[at][b][j] = *reinterpret_cast<const u32x4*>(from + (b * chunks + c) * 64);
+                }
+        };
+        auto load_v = [&](int tile, int at) {
+            const int64_t block = place(next_v, int64_t(tile) * 4 + g);
+            const uint8_t* from = a.c.v + block * block_bytes + m16 * 16;
+#pragma unroll
+            for (int d = 0; d < CH; ++d) vw[at][d] = *reinterpret_cast<const u32x4*>(from + (EXACT || d < chunks ? d : 0) * 256);
+            ks[at] = a.c.ks[block];
+            vs[at] = a.c.vs[block];
+            page_v[at] = next_v;
+        };
+        begin = same(begin);
+        end = same(end);
+        if (begin >= end) return;
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            if (begin + u * step < end) {
+                ask_pages(begin + u * step);
+                load_k(begin + u * step, u);
+                load_v(begin + u * step, u);
+            }
+        }
+        ask_pages(begin + NB * step);
+        for (int tile0 = begin; tile0 < end; tile0 += NB * step) {
+#pragma unroll
+        for (int u = 0; u < NB; ++u) {
+            const int tile = tile0 + u * step, ahead = tile + NB * step;
+            if (tile >= end) break;
+            const bool more = ahead < end;
+            const bool there = page_v[u] >= 0;
+            const bool masked = int64_t(tile) * 64 + 64 > least || !__all(there);
+            const float ksc = ks[u] * scale, vsc = vs[u];
+            f32x4 s[NR][4];
+#pragma unroll
+            for (int b = 0; b < 4; ++b) {
+#pragma unroll
+                for (int n = 0; n < NR; ++n) s[n][b] = FP8 ? f32x4{0, 0, 0, 0} : f32x4{from[n], from[n], from[n], from[n]};
+#pragma unroll
+                for (int j = 0; j < J; ++j) {
+                    const f16x8 k0 = widen<FP8, true>(kw[u][b][j][0], kw[u][b][j][1]), k1 = widen<FP8, true>(kw[u][b][j][2], kw[u][b][j][3]);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][j][0], s[n][b], 0, 0, 0);
+                        s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k1, q[n][j][1], s[n][b], 0, 0, 0);
+                    }
+                }
+            }
+            if (more) load_k(ahead, u);
+            const float lv = __builtin_amdgcn_logf(vsc);
+            f16x8 w[NR][2];
+            auto weigh = [&](auto some) {
+                constexpr bool MASKED = decltype(some)::value;
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    // of the lane's 16 tokens those before `seen` are there
+                    int seen = 16;
+                    if constexpr (MASKED) {
+                        const int64_t x = sees[n] - int64_t(tile) * 64 - g * 16;
+                        seen = !there || x < 0 ? 0 : x > 16 ? 16 : int(x);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) if (i >= seen) s[n][i >> 2][i & 3] = -kInf;
+                    }
+                    float mx = -kInf;
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) mx = max3(mx, s[n][i >> 2][i & 3], s[n][i >> 2][(i & 3) + 1]);
+                    if (!MASKED || mx != -kInf) mx *= ksc;
+                    const float top = MASKED && mx == -kInf ? -kInf : mx + lv;
+                    if (__any(mx > m[n] + kSlack || top > R[n] + kSlack)) {
+                        // each row by itself: what one row sees does not change how another is rounded
+                        float a1 = mx, a2 = top;
+                        a1 = fmaxf(a1, __shfl_xor(a1, 16));
+                        a2 = fmaxf(a2, __shfl_xor(a2, 16));
+                        a1 = fmaxf(a1, __shfl_xor(a1, 32));
+                        a2 = fmaxf(a2, __shfl_xor(a2, 32));
+                        const bool moves = a1 > m[n] + kSlack || a2 > R[n] + kSlack;
+                        a1 = moves ? fmaxf(a1, m[n]) : m[n];
+                        a2 = moves ? fmaxf(a2, R[n]) : R[n];
+                        l[n] *= power(m[n] - finite(a1));
+                        const float f = power(R[n] - finite(a2));
+#pragma unroll
+                        for (int d = 0; d < CH; ++d) o[n][d] *= f;
+                        m[n] = a1;
+                        R[n] = a2;
+                    }
+                    const float mb = finite(m[n]);
+                    // p * scale_v relative to R
+                    float f = power(fminf(lv + mb - finite(R[n]), 126.0f));
+                    if (!(vsc == vsc)) f = vsc;
+                    union { f16x8 v[2]; _Float16 h[16]; } c;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        float x = power(__builtin_fmaf(s[n][i >> 2][i & 3], ksc, -mb)), y = x * f;
+                        if constexpr (MASKED) {
+                            x = i < seen ? x : 0.0f;
+                            y = i < seen ? y : 0.0f;
+                        }
+                        l[n] += x;
+                        c.h[i] = _Float16(y);
+                    }
+                    w[n][0] = c.v[0];
+                    w[n][1] = c.v[1];
+                }
+            };
+            if (masked) weigh(std::true_type{});
+            else weigh(std::false_type{});
+#pragma unroll
+            for (int d = 0; d < CH; ++d) {
+                const f16x8 v0 = widen<FP8>(vw[u][d][0], vw[u][d][1]), v1 = widen<FP8>(vw[u][d][2], vw[u][d][3]);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[n][0], o[n][d], 0, 0, 0);
+                    o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[n][1], o[n][d], 0, 0, 0);
+                }
+            }
+            if (more) {
+                load_v(ahead, u);
+                ask_pages(ahead + step);
+            }
+        }
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            l[n] += __shfl_xor(l[n], 16);
+            l[n] += __shfl_xor(l[n], 32);
+        }
+    }
+};
+
+__device__ inline float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
+
+__device__ inline _Float16* out_row(const CachedArgs& a, const Shape& p, int row, int head, int sub, int h)
+{
+    return a.out.p + int64_t(row) * a.out.token + int64_t(head * a.group + sub * p.heads + h) * a.out.head;
+}
+
+// A workgroup for each row tile of each key head.
+template <bool FP8, int CH, bool EXACT, int NR, int NB>
+__global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void short_kernel(CachedArgs a, Shape p)
+{
+    constexpr int DP = CH * 16;
+    const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
+    const int m16 = lane & 15, g = lane >> 4;
+    Item it{int(blockIdx.x), 0};
+    if (a.b.start) it = find_item(a.b, int(blockIdx.x), p.per, 1);
+    it = {same(it.seq), same(it.i)};
+    if (it.seq < 0) return;
+    Span sp = span(a.b, it.seq);
+    sp = {same(sp.first), same(sp.n)};
+    if (it.i * p.per >= sp.n) return;
+    const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
+    Walk<FP8, CH, EXACT, NR, NB> w;
+    w.start(a, p, sp, same(cached_of(a.b, it.seq)), it.i, head, sub);
+    w.walk(a, it.seq, head, wave, int((w.most + 63) >> 6), kWaves);
+
     __shared__ float sums[kWaves][16 * NR][DP + 4];
     __shared__ Row stats[kWaves][16 * NR];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-        l[n] += __shfl_xor(l[n], 16);
-        l[n] += __shfl_xor(l[n], 32);
-        if (g == 0) stats[wave][n * 16 + m16] = {m[n], l[n], R[n]};
+        if (g == 0) stats[wave][n * 16 + m16] = {w.m[n], w.l[n], w.R[n]};
 #pragma unroll
-        for (int d = 0; d < CH; ++d) *reinterpret_cast<f32x4*>(&sums[wave][n * 16 + m16][d * 16 + g * 4]) = o[n][d];
+        for (int d = 0; d < CH; ++d) *reinterpret_cast<f32x4*>(&sums[wave][n * 16 + m16][d * 16 + g * 4]) = w.o[n][d];
     }
     __syncthreads();
     constexpr int kQuads = DP / 4;
-    float* const to = SPLIT && part.slot >= 0 ? a.part + (int64_t(part.slot) * gridDim.y + blockIdx.y) * p.rows * (DP + kExtra) : nullptr;
-    if constexpr (SPLIT) {
-        if (part.chunk == 0 && blockIdx.y == 0 && threadIdx.x == 0) {
-            int* meta = reinterpret_cast<int*>(a.part + int64_t(2 * p.parts) * gridDim.y * p.rows * (DP + kExtra));
-            const int64_t at = a.b.start ? item_base(a.b, part.seq, p.per, 1) + part.rt : part.seq;
-            meta[2 * at] = part.slot;
-            meta[2 * at + 1] = part.chunks;
-        }
-    }
-    for (int i = threadIdx.x; i < rows * kQuads; i += 64 * kWaves) {
+    for (int i = threadIdx.x; i < w.rows * kQuads; i += 64 * kWaves) {
         const int r = i / kQuads, d = (i - r * kQuads) * 4, t = r / p.heads, h = r - t * p.heads;
-        if (h >= heads) continue;
-        float M = -kInf, top = -kInf, L = 0.0f;
+        if (h >= w.heads || d >= a.c.dim) continue;
+        float M = -kInf, L = 0.0f;
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
-            M = fmaxf(M, stats[v][r].m);
-            top = fmaxf(top, stats[v][r].R);
-        }
-        const float Mb = finite(M), Rb = SPLIT && to ? finite(top) : Mb;
+        for (int v = 0; v < kWaves; ++v) M = fmaxf(M, stats[v][r].m);
+        M = finite(M);
         f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) {
-            L += stats[v][r].l * power(stats[v][r].m - Mb);
-            sum += *reinterpret_cast<f32x4*>(&sums[v][r][d]) * power(stats[v][r].R - Rb);
+            L += stats[v][r].l * power(stats[v][r].m - M);
+            sum += *reinterpret_cast<f32x4*>(&sums[v][r][d]) * power(stats[v][r].R - M);
         }
-        if (SPLIT && to) {
-            float* row = to + r * (DP + kExtra);
-            *reinterpret_cast<f32x4*>(row + d) = sum;
-            if (d == 0) *reinterpret_cast<f32x4*>(row + DP) = f32x4{M, L, top, 0.0f};
-        } else if (d < a.c.dim) {
-            sum *= L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
-            f16x4 y;
+        sum *= inverse(L);
+        f16x4 y;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = _Float16(sum[j]);
-            *reinterpret_cast<f16x4*>(a.out.p + int64_t(sp.first + first + t) * a.out.token + int64_t(head * a.group + sub * p.heads + h) * a.out.head + d) = y;
+        for (int j = 0; j < 4; ++j) y[j] = _Float16(sum[j]);
+        *reinterpret_cast<f16x4*>(out_row(a, p, sp.first + w.first + t, head, sub, h) + d) = y;
+    }
+}
+
+// A wave for each piece of the row of all tiles.  A row tile that it has whole is written out; of the others, sums go to the workspace: the begin of one
+// in the wave's second place, the rest of one that an earlier wave began in its first.
+template <bool FP8, int CH, bool EXACT, int NR, int NB>
+__global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_kernel(CachedArgs a, Shape p)
+{
+    constexpr int DP = CH * 16;
+    const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
+    // few pieces go to as many compute units
+    const int wave = same(threadIdx.x >> 6) * (kPieces / kWaves) + int(blockIdx.x);
+    const int ys = a.c.kv_heads * p.subs;
+    const double all = all_tiles(a, p, ys);
+    const double begin = piece_begin(all, wave);
+    double left = piece_begin(all, wave + 1) - begin;
+    if (!(left > 0.0)) return;
+    const double all_left = left;
+    const Found f = find_tile(a, p, begin, ys);
+    int seq = f.seq;
+    if (seq < 0) return;
+    Need need = need_of(a, p, seq);
+    // unit and tile in it
+    double inside = begin - f.before;
+    double u = floor(inside / double(need.tiles));
+    if (u * need.tiles > inside) u -= 1.0;
+    if ((u + 1.0) * need.tiles <= inside) u += 1.0;
+    int unit = same(int(u)), tile = same(int(inside - u * need.tiles));
+    seq = same(seq);
+    while (true) {
+        const int tiles = same(need.tiles), rts = same(need.rts);
+        const int to = same(double(tiles - tile) <= left ? tiles : tile + int(left));
+        const int y = unit / rts, rt = unit - y * rts, head = y / p.subs, sub = y - head * p.subs;
+        Span sp = span(a.b, seq);
+        sp = {same(sp.first), same(sp.n)};
+        Walk<FP8, CH, EXACT, NR, NB> w;
+        w.start(a, p, sp, same(cached_of(a.b, seq)), rt, head, sub);
+        const int seen = int((w.most + 63) >> 6);
+        w.walk(a, seq, head, tile, to < seen ? to : seen, 1);
+        const bool whole = tile == 0 && to == tiles;
+        if (tile == 0 && lane == 0) {
+            const int at = (a.b.start ? item_base(a.b, seq, p.per, 1) + rt : seq) * ys + y;
+            parts_of(a, p, DP)[at] = {wave, whole ? 1 : piece_of(all, begin + (all_left - left) + tiles - 1.0) - wave + 1};
+        }
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            const int r = n * 16 + m16, t = r / p.heads, h = r - t * p.heads;
+            if (r >= w.rows || h >= w.heads) continue;
+            if (whole) {
+                const float x = inverse(w.l[n]) * power(w.R[n] - finite(w.m[n]));
+                _Float16* out = out_row(a, p, sp.first + w.first + t, head, sub, h);
+#pragma unroll
+                for (int d = 0; d < CH; ++d) {
+                    if (d * 16 >= a.c.dim) continue;
+                    f16x4 v;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] = _Float16(w.o[n][d][j] * x);
+                    *reinterpret_cast<f16x4*>(out + d * 16 + g * 4) = v;
+                }
+            } else {
+                float* row = a.part + ((int64_t(wave) * 2 + (tile == 0)) * p.rows + r) * (DP + kExtra);
+#pragma unroll
+                for (int d = 0; d < CH; ++d) *reinterpret_cast<f32x4*>(row + d * 16 + g * 4) = w.o[n][d];
+                if (g == 0) *reinterpret_cast<f32x4*>(row + DP) = f32x4{w.m[n], w.l[n], w.R[n], 0.0f};
+            }
+        }
+        left -= double(to - tile);
+        if (same(left > 0.0) == 0) break;
+        tile = 0;
+        if (++unit == rts * ys) {
+            unit = 0;
+            do {
+                if (++seq >= a.b.seqs) return;
+                need = need_of(a, p, seq);
+            } while (same(need.tiles * (need.rts > 0)) == 0);
         }
     }
 }
 
-// Joins the parts of the row tiles that were cut: a wave takes a row, a lane two dimensions.
+// Joins the pieces of row tiles that several waves share: a workgroup takes a row.  Four dimensions are a thread's, and the parts are dealt among the threads that
+// have the same ones; the sums of the first parts are asked for before it is known how they weigh.
 template <int CH>
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p)
 {
-    constexpr int DP = CH * 16;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int DP = CH * 16, kQuads = DP / 4, kGroups = 64 * kWaves / kQuads, kAhead = 8, kMost = kPieces / (64 * kWaves);
+    const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
     Item it{int(blockIdx.x), 0};
     if (a.b.start) it = find_item(a.b, int(blockIdx.x), p.per, 1);
     if (it.seq < 0) return;
+    const Parts found = parts_of(a, p, DP)[int64_t(blockIdx.x) * gridDim.y + blockIdx.y];      // of a sequence without tiles: anything
     const Span sp = span(a.b, it.seq);
-    const int first = it.i * p.per;
-    if (first >= sp.n) return;
-    const int* meta = reinterpret_cast<const int*>(a.part + int64_t(2 * p.parts) * gridDim.y * p.rows * (DP + kExtra));
-    const int slot = meta[2 * blockIdx.x], chunks = meta[2 * blockIdx.x + 1];
-    if (chunks < 2) return;
+    const int first = it.i * p.per, tokens = sp.n - first < p.per ? sp.n - first : p.per;
+    const bool none = need_of(a, p, it.seq).tiles == 0;
     const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
-    const int tokens = sp.n - first < p.per ? sp.n - first : p.per;
-    const int64_t stride = int64_t(gridDim.y) * p.rows * (DP + kExtra);
-    for (int r = int(blockIdx.z) * kWaves + wave; r < tokens * p.heads; r += int(gridDim.z) * kWaves) {
+    const int quad = int(threadIdx.x) % kQuads, d = quad * 4, mine = int(threadIdx.x) / kQuads;
+    if (!none && found.n == 1) return;
+    const int w0 = found.w0, parts = found.n;
+    __shared__ float weight[kPieces];
+    __shared__ float most[kWaves], total[kWaves];
+    __shared__ f32x4 sums[kGroups][kQuads];
+    for (int r = int(blockIdx.z); r < tokens * p.heads; r += int(gridDim.z)) {
         const int t = r / p.heads, h = r - t * p.heads;
         if (sub * p.heads + h >= a.group) continue;
-        const float* from = a.part + (int64_t(slot) * gridDim.y + blockIdx.y) * p.rows * (DP + kExtra) + int64_t(r) * (DP + kExtra);
-        float M = -kInf;
-        for (int c = lane; c < chunks; c += 64) M = fmaxf(M, from[c * stride + DP]);
-        for (int k = 32; k; k >>= 1) M = fmaxf(M, __shfl_xor(M, k));
-        const float Mb = finite(M);
-        float L = 0.0f, x0 = 0.0f, x1 = 0.0f;
-        for (int c0 = 0; c0 < chunks; c0 += 64) {
-            float w = 0.0f;
-            if (c0 + lane < chunks) {
-                const f32x4 s = *reinterpret_cast<const f32x4*>(from + (c0 + lane) * stride + DP);
-                L += s[1] * power(s[0] - Mb);
-                w = power(s[2] - Mb);
-            }
-            const int n = chunks - c0 < 64 ? chunks - c0 : 64;
-            for (int c = 0; c < n; c += 8) {
+        _Float16* out = out_row(a, p, sp.first + first + t, head, sub, h) + d;
+        if (none) {
+            if (mine == 0 && d < a.c.dim) *reinterpret_cast<f16x4*>(out) = f16x4{0, 0, 0, 0};
+            continue;
+        }
+        // part c is in piece w0 + c: the first in its second place, the others in their first
+        auto row_of = [&](int c) { return a.part + ((int64_t(w0 + c) * 2 + (c == 0)) * p.rows + r) * (DP + kExtra); };
+        f32x4 ahead[kAhead];
 #pragma unroll
-                for (int u = 0; u < 8; ++u) {
-                    const float f = __shfl(w, c + u);        // 0 beyond the last part
-                    const float* row = from + (c0 + (c + u < n ? c + u : n - 1)) * stride + (2 * lane < DP ? 2 * lane : 0);
-                    x0 += row[0] * f;
-                    x1 += row[1] * f;
-                }
-            }
+        for (int u = 0; u < kAhead; ++u) {
+            const int c = mine + u * kGroups;
+            ahead[u] = *reinterpret_cast<const f32x4*>(row_of(c < parts ? c : 0) + d);
+        }
+        f32x4 stat[kMost];
+        float M = -kInf;
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int c = int(threadIdx.x) + u * 64 * kWaves;
+            stat[u] = f32x4{-kInf, 0, -kInf, 0};
+            if (c < parts) stat[u] = *reinterpret_cast<const f32x4*>(row_of(c) + DP);
+            M = fmaxf(M, stat[u][0]);
+        }
+        for (int k = 32; k; k >>= 1) M = fmaxf(M, __shfl_xor(M, k));
+        if (lane == 0) most[wave] = M;
+        __syncthreads();
+#pragma unroll
+        for (int v = 0; v < kWaves; ++v) M = fmaxf(M, most[v]);
+        M = finite(M);
+        float L = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kMost; ++u) {
+            const int c = int(threadIdx.x) + u * 64 * kWaves;
+            if (c >= parts) break;
+            L += stat[u][1] * power(stat[u][0] - M);
+            weight[c] = power(stat[u][2] - M);
         }
         for (int k = 32; k; k >>= 1) L += __shfl_xor(L, k);
-        const float f = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
-        if (2 * lane < a.c.dim)
-            *reinterpret_cast<f16x2*>(a.out.p + int64_t(sp.first + first + t) * a.out.token + int64_t(head * a.group + sub * p.heads + h) * a.out.head + 2 * lane) =
-                f16x2{_Float16(x0 * f), _Float16(x1 * f)};
+        if (lane == 0) total[wave] = L;
+        __syncthreads();
+        f32x4 x = {0, 0, 0, 0};
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (mine + u * kGroups < parts) x += ahead[u] * weight[mine + u * kGroups];
+        for (int c = mine + kAhead * kGroups; c < parts; c += kGroups) x += *reinterpret_cast<const f32x4*>(row_of(c) + d) * weight[c];
+        sums[mine][quad] = x;
+        __syncthreads();
+        if (mine == 0 && d < a.c.dim) {
+            L = 0.0f;
+#pragma unroll
+            for (int v = 0; v < kWaves; ++v) L += total[v];
+#pragma unroll
+            for (int v = 1; v < kGroups; ++v) x += sums[v][quad];
+            x *= inverse(L);
+            f16x4 y;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] = _Float16(x[j]);
+            *reinterpret_cast<f16x4*>(out) = y;
+        }
     }
 }
 
 inline int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
-template <bool FP8, int CH, int NR>
-hipError_t launch(const CachedArgs& a, const Shape& p, bool split, hipStream_t s)
+template <bool FP8, int CH, bool EXACT, int NR>
+hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
 {
     const unsigned y = unsigned(a.c.kv_heads * p.subs);
-    if (!split) {
-        cached_kernel<FP8, CH, NR, false><<<dim3(unsigned(p.metas), y), 64 * kWaves, 0, s>>>(a, p);
+    if (alone) {
+        short_kernel<FP8, CH, EXACT, NR, 1><<<dim3(unsigned(p.tiles), y), 64 * kWaves, 0, s>>>(a, p);
         return hipGetLastError();
     }
-    cached_kernel<FP8, CH, NR, true><<<dim3(unsigned(p.metas + p.parts), y), 64 * kWaves, 0, s>>>(a, p);
-    hipError_t e = hipGetLastError();
+    piece_kernel<FP8, CH, EXACT, NR, 1><<<kPieces / kWaves, 64 * kWaves, 0, s>>>(a, p);
+    const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    join_kernel<CH><<<dim3(unsigned(p.metas), y, unsigned((p.rows + kWaves - 1) / kWaves)), 64 * kWaves, 0, s>>>(a, p);
+    join_kernel<CH><<<dim3(unsigned(p.tiles), y, unsigned(p.rows < 16 ? p.rows : 16)), 64 * kWaves, 0, s>>>(a, p);
     return hipGetLastError();
+}
+
+template <bool FP8, int NR>
+hipError_t launch_dim(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
+{
+    if (a.c.dim == 128) return launch<FP8, 8, true, NR>(a, p, alone, s);
+    if (a.c.dim == 64) return launch<FP8, 4, true, NR>(a, p, alone, s);
+    return a.c.dim < 64 ? launch<FP8, 4, false, NR>(a, p, alone, s) : launch<FP8, 8, false, NR>(a, p, alone, s);
+}
+
+template <bool FP8>
+hipError_t launch_type(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
+{
+    return p.nr == 2 ? launch_dim<FP8, 2>(a, p, alone, s) : launch_dim<FP8, 1>(a, p, alone, s);
 }
 
 }  // namespace
@@ -473,8 +655,8 @@ size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t k
     size_t most = 0;
     for (const bool one : {false, true}) {
         if (one && tokens != seqs) continue;
-        const Shape p = shape_of(seqs, tokens, one, int(q_heads / kv_heads), int(kv_heads), 1);
-        const size_t n = size_t(2 * p.parts) * size_t(kv_heads * p.subs) * p.rows * (padded(dim) + kExtra) * sizeof(float) + size_t(p.metas) * 2 * sizeof(int);
+        const Shape p = shape_of(seqs, tokens, one, int(q_heads / kv_heads));
+        const size_t n = size_t(2 * kPieces) * p.rows * (padded(dim) + kExtra) * sizeof(float) + size_t(p.tiles) * size_t(kv_heads * p.subs) * sizeof(Parts);
         if (n > most) most = n;
     }
     return (most + 15) / 16 * 16;
@@ -482,10 +664,9 @@ size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t k
 
 hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s)
 {
-    const bool split = longest == 0 || longest > kLeast * 64;
-    const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group, a.c.kv_heads, 1);
-    if (a.c.fp8) return padded(a.c.dim) == 64 ? launch<true, 4, 1>(a, p, split, s) : launch<true, 8, 1>(a, p, split, s);
-    return padded(a.c.dim) == 64 ? launch<false, 4, 1>(a, p, split, s) : launch<false, 8, 1>(a, p, split, s);
+    const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group);
+    const bool alone = longest > 0 && longest <= kAlone * 64;
+    return a.c.fp8 ? launch_type<true>(a, p, alone, s) : launch_type<false>(a, p, alone, s);
 }
 
 }  // namespace tl

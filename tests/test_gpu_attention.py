@@ -249,7 +249,10 @@ def test_cached_one_token(kind, H, HK, D, page):
     q = f16(rng, st.T, H, D)
     got = cached(st, q, D ** -0.5, extra=2)
     check_cached(st, q, got, D ** -0.5)
-    assert np.array_equal(got, cached(st, q, D ** -0.5, one=False, longest=0))
+    assert np.array_equal(got, cached(st, q, D ** -0.5, one=False))
+    got = cached(st, q, D ** -0.5, longest=0)             # the way of long caches: sums meet in another order
+    check_cached(st, q, got, D ** -0.5)
+    assert np.array_equal(got, cached(st, q, D ** -0.5, longest=0))
 
 
 @pytest.mark.parametrize("kind", ["int8", "fp8"])
@@ -259,6 +262,7 @@ def test_cached_several_tokens(kind, H, HK, D):
     st = Setup(H * 17 + D, [5, 0, 1, 37, 70, 2, 3], [0, 3, 100, 61, 250, -1, 15], H, HK, D, 32, kind)
     q = f16(rng, st.T, H, D)
     check_cached(st, q, cached(st, q, D ** -0.5, extra=1), D ** -0.5)
+    check_cached(st, q, cached(st, q, D ** -0.5, longest=0), D ** -0.5)
 
 
 @pytest.mark.parametrize("kind", ["int8", "fp8"])
@@ -324,6 +328,7 @@ def test_cached_nan_block_missing_pages_and_rows_that_see_nothing():
     q = f16(rng, st.T, 4, 64)
     got = cached(st, q, 0.125)
     check_cached(st, q, got, 0.125)
+    check_cached(st, q, cached(st, q, 0.125, longest=0), 0.125)
     assert (got[42] == 0).all() and np.isfinite(got[:16]).all() and np.isfinite(got[:40, :2]).all() and np.isnan(got[16:40, 2:]).all()
 
 
