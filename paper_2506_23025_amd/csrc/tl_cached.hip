@@ -21,7 +21,7 @@ namespace tl {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kPieces = 2048;             // waves that share a call's tiles: two on each SIMD of 256 CUs
+constexpr int kWavesAll = 2048;           // waves that share a call's tiles: two on each SIMD of 256 CUs
 constexpr int kAlone = 16;                // up to so many tiles a sequence is left to one workgroup: the second kernel would cost more than it saves
 
 constexpr float kInf = __builtin_inff();
@@ -33,10 +33,12 @@ struct Shape {
     int subs;                             // row tiles that the query heads of a key head need
     int rows;                             // per * heads
     int nr;                               // blocks of 16 rows in a row tile
+    int ys;                               // key heads * subs: what a token of the cache is read for
+    int pieces;                           // that the row of all tiles is cut into, each for ys waves
     int64_t tiles;                        // row tiles of the call at most
 };
 
-inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group)
+inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group, int kv_heads)
 {
     Shape p;
     // two blocks of 16 rows share the widened codes where the tokens of a sequence fill them
@@ -46,6 +48,9 @@ inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group)
     p.subs = (group + p.heads - 1) / p.heads;
     p.per = one ? 1 : most / p.heads;
     p.rows = p.per * p.heads;
+    p.ys = kv_heads * p.subs;
+    p.pieces = kWavesAll / p.ys;
+    if (p.pieces < 1) p.pieces = 1;
     p.tiles = one ? seqs : tokens / p.per + seqs;
     return p;
 }
@@ -78,6 +83,14 @@ __device__ inline f16x8 widen(uint32_t a, uint32_t b)
         }
     }
     return r.v;
+}
+
+// 16 bytes of codes; ONCE: that nobody else will ask for.
+template <bool ONCE>
+__device__ inline u32x4 fetch(const uint8_t* p)
+{
+    if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+    else return *reinterpret_cast<const u32x4*>(p);
 }
 
 __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
@@ -125,25 +138,25 @@ __device__ inline double of_lane(double x, int lane)
     return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
 
-// The call's tiles in one row: sequence after sequence, of each the key heads' row tiles one after the other, `units` of them with `tiles` tiles each.
-__device__ inline double share_of(const CachedArgs& a, const Shape& p, int s, int ys)
+// The call's tiles in one row: sequence after sequence, of each its row tiles one after the other.
+__device__ inline double share_of(const CachedArgs& a, const Shape& p, int s)
 {
     const Need n = need_of(a, p, s);
-    return double(n.tiles) * double(n.rts) * double(ys);
+    return double(n.tiles) * double(n.rts);
 }
 
-__device__ inline double all_tiles(const CachedArgs& a, const Shape& p, int ys)
+__device__ inline double all_tiles(const CachedArgs& a, const Shape& p)
 {
     const int lane = threadIdx.x & 63, per = (a.b.seqs + 63) >> 6;
     double w = 0.0;
     for (int i = 0; i < per; ++i)
-        if (lane * per + i < a.b.seqs) w += share_of(a, p, lane * per + i, ys);
+        if (lane * per + i < a.b.seqs) w += share_of(a, p, lane * per + i);
     return of_lane(scanned(w), 63);
 }
 
 // The sequence that holds tile x of the row, and how many tiles stand before it.
 struct Found { int seq; double before; };
-__device__ inline Found find_tile(const CachedArgs& a, const Shape& p, double x, int ys)
+__device__ inline Found find_tile(const CachedArgs& a, const Shape& p, double x)
 {
     const int lane = threadIdx.x & 63;
     int lo = 0, count = a.b.seqs;
@@ -152,7 +165,7 @@ __device__ inline Found find_tile(const CachedArgs& a, const Shape& p, double x,
         const int per = (count + 63) >> 6;
         double w = 0.0;
         for (int i = 0; i < per; ++i)
-            if (lane * per + i < count) w += share_of(a, p, lo + lane * per + i, ys);
+            if (lane * per + i < count) w += share_of(a, p, lo + lane * per + i);
         const double to = scanned(w);
         const uint64_t there = __ballot(before + to > x);
         if (!there) return {-1, 0.0};
@@ -164,31 +177,38 @@ __device__ inline Found find_tile(const CachedArgs& a, const Shape& p, double x,
     }
 }
 
-// First tile of piece i, of `all` tiles: equal shares, or one each where there are fewer tiles than waves.
-__device__ inline double piece_begin(double all, int i)
+// First tile of piece i, of `all` tiles: equal shares, or one each where there are fewer tiles than pieces.  Whole numbers below 2^52 with a
+// divisor below 2^12: the quotient's rounding cannot reach the next whole number.
+__device__ inline double piece_begin(const Shape& p, double all, int i)
 {
-    if (all <= kPieces) return fmin(double(i), all);
-    return floor(all * double(i) * (1.0 / kPieces));
+    if (all <= p.pieces) return fmin(double(i), all);
+    return floor(all * double(i) / double(p.pieces));
 }
 
 // The piece that holds tile x.
-__device__ inline int piece_of(double all, double x)
+__device__ inline int piece_of(const Shape& p, double all, double x)
 {
-    if (all <= kPieces) return int(x);
-    int i = int((x + 1.0) * kPieces / all);
-    if (i > kPieces - 1) i = kPieces - 1;
-    while (i > 0 && piece_begin(all, i) > x) --i;
-    while (i < kPieces - 1 && piece_begin(all, i + 1) <= x) ++i;
+    if (all <= p.pieces) return int(x);
+    int i = int((x + 1.0) * p.pieces / all);
+    if (i > p.pieces - 1) i = p.pieces - 1;
+    while (i > 0 && piece_begin(p, all, i) > x) --i;
+    while (i < p.pieces - 1 && piece_begin(p, all, i + 1) <= x) ++i;
     return i;
 }
 
 struct Row { float m, l, R; };
 
-// Where the parts of a row tile of a key head are: in the pieces from w0 on, so many of them.
+// Where the parts of a row tile are: in the pieces from w0 on, so many of them.
 struct Parts { int w0, n; };
 __device__ inline Parts* parts_of(const CachedArgs& a, const Shape& p, int dp)
 {
-    return reinterpret_cast<Parts*>(a.part + int64_t(2 * kPieces) * p.rows * (dp + kExtra));
+    return reinterpret_cast<Parts*>(a.part + int64_t(2 * p.pieces) * p.ys * p.rows * (dp + kExtra));
+}
+
+// A row's sums of a piece: its second place has a row tile that begins in it, its first the rest of one that an earlier piece began.
+__device__ inline float* part_row(const CachedArgs& a, const Shape& p, int dp, int piece, bool begins, int y, int r)
+{
+    return a.part + (((int64_t(piece) * 2 + begins) * p.ys + y) * p.rows + r) * (dp + kExtra);
 }
 
 // One row tile of one key head: its queries, and its sums over tiles begin, begin + step, ... below end.
@@ -258,50 +278,54 @@ struct Walk {
         auto place = [&](int page, int64_t block) { return (int64_t(page < 0 ? 0 : page) * a.c.kv_heads + head) * blocks + (block & in_page); };
         u32x4 kw[NB][4][J], vw[NB][CH];
         float ks[NB], vs[NB];
-        int page_v[NB], next_k = -1, next_v = -1;
+        bool there[NB];                                      // the lane's block has a page
+        // Loads come back in order, so what is needed first is asked for first: the pages of the tile after, a tile's scales, its keys, its values.
+        int next_k = 0, next_v = 0;
+        int64_t value_block = 0;
         auto ask_pages = [&](int tile) {
             next_k = page_at(int64_t(tile) * 4 + (m16 >> 2));
             next_v = page_at(int64_t(tile) * 4 + g);
         };
         auto load_k = [&](int tile, int at) {
-            const uint8_t* from = a.c.k + place(next_k, int64_t(tile) * 4 + (m16 >> 2)) * block_bytes + (m16 & 3) * 16;
+            const int64_t key_block = place(next_k, int64_t(tile) * 4 + (m16 >> 2));
+            value_block = place(next_v, int64_t(tile) * 4 + g);
+            there[at] = next_v >= 0;
+            ask_pages(tile + step);
+            ks[at] = a.c.ks[value_block];
+            vs[at] = a.c.vs[value_block];
+            const uint8_t* from = a.c.k + key_block * block_bytes + (m16 & 3) * 16;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     const int c = EXACT || 4 * j + g < chunks ? 4 * j + g : 0;
-                    kw[at][b][j] = *reinterpret_cast<const u32x4*>(from + (b * chunks + c) * 64);
+                    kw[at][b][j] = fetch<NR == 1>(from + (b * chunks + c) * 64);
                 }
         };
-        auto load_v = [&](int tile, int at) {
-            const int64_t block = place(next_v, int64_t(tile) * 4 + g);
-            const uint8_t* from = a.c.v + block * block_bytes + m16 * 16;
+        auto load_v = [&](int at) {
+            const uint8_t* from = a.c.v + value_block * block_bytes + m16 * 16;
 #pragma unroll
-            for (int d = 0; d < CH; ++d) vw[at][d] = *reinterpret_cast<const u32x4*>(from + (EXACT || d < chunks ? d : 0) * 256);
-            ks[at] = a.c.ks[block];
-            vs[at] = a.c.vs[block];
-            page_v[at] = next_v;
+            for (int d = 0; d < CH; ++d) vw[at][d] = fetch<NR == 1>(from + (EXACT || d < chunks ? d : 0) * 256);
         };
         begin = same(begin);
         end = same(end);
         if (begin >= end) return;
+        ask_pages(begin);
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
             if (begin + u * step < end) {
-                ask_pages(begin + u * step);
                 load_k(begin + u * step, u);
-                load_v(begin + u * step, u);
+                load_v(u);
             }
         }
-        ask_pages(begin + NB * step);
         for (int tile0 = begin; tile0 < end; tile0 += NB * step) {
 #pragma unroll
         for (int u = 0; u < NB; ++u) {
             const int tile = tile0 + u * step, ahead = tile + NB * step;
             if (tile >= end) break;
             const bool more = ahead < end;
-            const bool there = page_v[u] >= 0;
-            const bool masked = int64_t(tile) * 64 + 64 > least || !__all(there);
+            const bool inside = there[u];
+            const bool masked = int64_t(tile) * 64 + 64 > least || !__all(inside);
             const float ksc = ks[u] * scale, vsc = vs[u];
             f32x4 s[NR][4];
 #pragma unroll
@@ -329,7 +353,7 @@ struct Walk {
                     int seen = 16;
                     if constexpr (MASKED) {
                         const int64_t x = sees[n] - int64_t(tile) * 64 - g * 16;
-                        seen = !there || x < 0 ? 0 : x > 16 ? 16 : int(x);
+                        seen = !inside || x < 0 ? 0 : x > 16 ? 16 : int(x);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) if (i >= seen) s[n][i >> 2][i & 3] = -kInf;
                     }
@@ -385,10 +409,7 @@ struct Walk {
                     o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[n][1], o[n][d], 0, 0, 0);
                 }
             }
-            if (more) {
-                load_v(ahead, u);
-                ask_pages(ahead + step);
-            }
+            if (more) load_v(u);
         }
         }
 #pragma unroll
@@ -456,36 +477,34 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void short_k
     }
 }
 
-// A wave for each piece of the row of all tiles.  A row tile that it has whole is written out; of the others, sums go to the workspace: the begin of one
-// in the wave's second place, the rest of one that an earlier wave began in its first.
+// A wave for each piece of the row of all tiles and each key head: neighbouring waves read the heads of the same tokens, which lie side by side in
+// a page.  A row tile that a piece has whole is written out, of the others the sums go to the workspace.
 template <bool FP8, int CH, bool EXACT, int NR, int NB>
 __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_kernel(CachedArgs a, Shape p)
 {
     constexpr int DP = CH * 16;
     const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
-    // few pieces go to as many compute units
-    const int wave = same(threadIdx.x >> 6) * (kPieces / kWaves) + int(blockIdx.x);
-    const int ys = a.c.kv_heads * p.subs;
-    const double all = all_tiles(a, p, ys);
-    const double begin = piece_begin(all, wave);
-    double left = piece_begin(all, wave + 1) - begin;
-    if (!(left > 0.0)) return;
-    const double all_left = left;
-    const Found f = find_tile(a, p, begin, ys);
-    int seq = f.seq;
+    const int wave = int(blockIdx.x) * kWaves + same(threadIdx.x >> 6), piece = wave / p.ys, y = wave - piece * p.ys;
+    if (piece >= p.pieces) return;
+    const int head = y / p.subs, sub = y - head * p.subs;
+    const double all = all_tiles(a, p);
+    double at = piece_begin(p, all, piece);
+    const double stop = piece_begin(p, all, piece + 1);
+    if (same(at < stop) == 0) return;
+    const Found f = find_tile(a, p, at);
+    int seq = same(f.seq);
     if (seq < 0) return;
     Need need = need_of(a, p, seq);
-    // unit and tile in it
-    double inside = begin - f.before;
+    // row tile, and tile in it
+    const double inside = at - f.before;
     double u = floor(inside / double(need.tiles));
     if (u * need.tiles > inside) u -= 1.0;
     if ((u + 1.0) * need.tiles <= inside) u += 1.0;
-    int unit = same(int(u)), tile = same(int(inside - u * need.tiles));
-    seq = same(seq);
+    int rt = same(int(u)), tile = same(int(inside - u * need.tiles));
     while (true) {
         const int tiles = same(need.tiles), rts = same(need.rts);
+        const double left = stop - at;
         const int to = same(double(tiles - tile) <= left ? tiles : tile + int(left));
-        const int y = unit / rts, rt = unit - y * rts, head = y / p.subs, sub = y - head * p.subs;
         Span sp = span(a.b, seq);
         sp = {same(sp.first), same(sp.n)};
         Walk<FP8, CH, EXACT, NR, NB> w;
@@ -493,10 +512,8 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
         const int seen = int((w.most + 63) >> 6);
         w.walk(a, seq, head, tile, to < seen ? to : seen, 1);
         const bool whole = tile == 0 && to == tiles;
-        if (tile == 0 && lane == 0) {
-            const int at = (a.b.start ? item_base(a.b, seq, p.per, 1) + rt : seq) * ys + y;
-            parts_of(a, p, DP)[at] = {wave, whole ? 1 : piece_of(all, begin + (all_left - left) + tiles - 1.0) - wave + 1};
-        }
+        if (tile == 0 && y == 0 && lane == 0)
+            parts_of(a, p, DP)[a.b.start ? item_base(a.b, seq, p.per, 1) + rt : seq] = {piece, whole ? 1 : piece_of(p, all, at + tiles - 1.0) - piece + 1};
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             const int r = n * 16 + m16, t = r / p.heads, h = r - t * p.heads;
@@ -513,17 +530,17 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
                     *reinterpret_cast<f16x4*>(out + d * 16 + g * 4) = v;
                 }
             } else {
-                float* row = a.part + ((int64_t(wave) * 2 + (tile == 0)) * p.rows + r) * (DP + kExtra);
+                float* row = part_row(a, p, DP, piece, tile == 0, y, r);
 #pragma unroll
                 for (int d = 0; d < CH; ++d) *reinterpret_cast<f32x4*>(row + d * 16 + g * 4) = w.o[n][d];
                 if (g == 0) *reinterpret_cast<f32x4*>(row + DP) = f32x4{w.m[n], w.l[n], w.R[n], 0.0f};
             }
         }
-        left -= double(to - tile);
-        if (same(left > 0.0) == 0) break;
+        at += double(to - tile);
+        if (same(at < stop) == 0) break;
         tile = 0;
-        if (++unit == rts * ys) {
-            unit = 0;
+        if (++rt == rts) {
+            rt = 0;
             do {
                 if (++seq >= a.b.seqs) return;
                 need = need_of(a, p, seq);
@@ -537,12 +554,12 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
 template <int CH>
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p)
 {
-    constexpr int DP = CH * 16, kQuads = DP / 4, kGroups = 64 * kWaves / kQuads, kAhead = 8, kMost = kPieces / (64 * kWaves);
+    constexpr int DP = CH * 16, kQuads = DP / 4, kGroups = 64 * kWaves / kQuads, kAhead = 8, kMost = kWavesAll / (64 * kWaves);
     const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
     Item it{int(blockIdx.x), 0};
     if (a.b.start) it = find_item(a.b, int(blockIdx.x), p.per, 1);
     if (it.seq < 0) return;
-    const Parts found = parts_of(a, p, DP)[int64_t(blockIdx.x) * gridDim.y + blockIdx.y];      // of a sequence without tiles: anything
+    const Parts found = parts_of(a, p, DP)[blockIdx.x];      // of a sequence without tiles: anything
     const Span sp = span(a.b, it.seq);
     const int first = it.i * p.per, tokens = sp.n - first < p.per ? sp.n - first : p.per;
     const bool none = need_of(a, p, it.seq).tiles == 0;
@@ -550,7 +567,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p
     const int quad = int(threadIdx.x) % kQuads, d = quad * 4, mine = int(threadIdx.x) / kQuads;
     if (!none && found.n == 1) return;
     const int w0 = found.w0, parts = found.n;
-    __shared__ float weight[kPieces];
+    __shared__ float weight[kWavesAll];
     __shared__ float most[kWaves], total[kWaves];
     __shared__ f32x4 sums[kGroups][kQuads];
     for (int r = int(blockIdx.z); r < tokens * p.heads; r += int(gridDim.z)) {
@@ -562,7 +579,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p
             continue;
         }
         // part c is in piece w0 + c: the first in its second place, the others in their first
-        auto row_of = [&](int c) { return a.part + ((int64_t(w0 + c) * 2 + (c == 0)) * p.rows + r) * (DP + kExtra); };
+        auto row_of = [&](int c) { return part_row(a, p, DP, w0 + c, c == 0, int(blockIdx.y), r); };
         f32x4 ahead[kAhead];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
@@ -622,12 +639,12 @@ inline int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
 template <bool FP8, int CH, bool EXACT, int NR>
 hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
 {
-    const unsigned y = unsigned(a.c.kv_heads * p.subs);
+    const unsigned y = unsigned(p.ys);
     if (alone) {
         short_kernel<FP8, CH, EXACT, NR, 1><<<dim3(unsigned(p.tiles), y), 64 * kWaves, 0, s>>>(a, p);
         return hipGetLastError();
     }
-    piece_kernel<FP8, CH, EXACT, NR, 1><<<kPieces / kWaves, 64 * kWaves, 0, s>>>(a, p);
+    piece_kernel<FP8, CH, EXACT, NR, 1><<<unsigned((p.pieces * p.ys + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     join_kernel<CH><<<dim3(unsigned(p.tiles), y, unsigned(p.rows < 16 ? p.rows : 16)), 64 * kWaves, 0, s>>>(a, p);
@@ -655,8 +672,8 @@ size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t k
     size_t most = 0;
     for (const bool one : {false, true}) {
         if (one && tokens != seqs) continue;
-        const Shape p = shape_of(seqs, tokens, one, int(q_heads / kv_heads));
-        const size_t n = size_t(2 * kPieces) * p.rows * (padded(dim) + kExtra) * sizeof(float) + size_t(p.tiles) * size_t(kv_heads * p.subs) * sizeof(Parts);
+        const Shape p = shape_of(seqs, tokens, one, int(q_heads / kv_heads), int(kv_heads));
+        const size_t n = size_t(2 * p.pieces) * p.ys * p.rows * (padded(dim) + kExtra) * sizeof(float) + size_t(p.tiles) * sizeof(Parts);
         if (n > most) most = n;
     }
     return (most + 15) / 16 * 16;
@@ -664,7 +681,7 @@ size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t k
 
 hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s)
 {
-    const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group);
+    const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group, a.c.kv_heads);
     const bool alone = longest > 0 && longest <= kAlone * 64;
     return a.c.fp8 ? launch_type<true>(a, p, alone, s) : launch_type<false>(a, p, alone, s);
 }
