@@ -22,6 +22,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kWavesAll = 2048;           // waves that share a call's tiles: two on each SIMD of 256 CUs
+constexpr int kFewRows = 1024;            // up to so many rows a workgroup joins the parts of each, beyond a wave
 constexpr int kAlone = 16;                // up to so many tiles a sequence is left to one workgroup: the second kernel would cost more than it saves
 
 constexpr float kInf = __builtin_inff();
@@ -97,17 +98,30 @@ __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
 __device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// Tiles and row tiles of a sequence.
-struct Need { int tiles, rts; };
+// A sequence: its tokens in the call, those before them, and the tiles and row tiles that it needs.
+struct Need {
+    int first, n, past, tiles, rts;
+    __device__ inline double share() const { return double(tiles) * double(rts); }
+};
+
 __device__ inline Need need_of(const CachedArgs& a, const Shape& p, int s)
 {
     const Span sp = span(a.b, s);
     const int past = cached_of(a.b, s);
-    if (sp.n == 0) return {0, 0};
+    Need need{sp.first, sp.n, past, 0, 0};
+    if (sp.n == 0) return need;
     int64_t len = past < 0 ? 0 : int64_t(past) + sp.n;
     const int64_t room = a.c.pages_per_seq << (a.c.page_shift + 4);
     if (len > room) len = room;
-    return {int((len + 63) >> 6), (sp.n + p.per - 1) / p.per};
+    need.tiles = int((len + 63) >> 6);
+    need.rts = p.per == 1 ? sp.n : (sp.n + p.per - 1) / p.per;
+    return need;
+}
+
+__device__ inline Need of_lane(const Need& x, int lane)
+{
+    return {__builtin_amdgcn_readlane(x.first, lane), __builtin_amdgcn_readlane(x.n, lane), __builtin_amdgcn_readlane(x.past, lane),
+            __builtin_amdgcn_readlane(x.tiles, lane), __builtin_amdgcn_readlane(x.rts, lane)};
 }
 
 // Sums over the wave, exact: whole numbers below 2^53 in doubles.
@@ -139,18 +153,12 @@ __device__ inline double of_lane(double x, int lane)
 }
 
 // The call's tiles in one row: sequence after sequence, of each its row tiles one after the other.
-__device__ inline double share_of(const CachedArgs& a, const Shape& p, int s)
-{
-    const Need n = need_of(a, p, s);
-    return double(n.tiles) * double(n.rts);
-}
-
 __device__ inline double all_tiles(const CachedArgs& a, const Shape& p)
 {
     const int lane = threadIdx.x & 63, per = (a.b.seqs + 63) >> 6;
     double w = 0.0;
     for (int i = 0; i < per; ++i)
-        if (lane * per + i < a.b.seqs) w += share_of(a, p, lane * per + i);
+        if (lane * per + i < a.b.seqs) w += need_of(a, p, lane * per + i).share();
     return of_lane(scanned(w), 63);
 }
 
@@ -165,7 +173,7 @@ __device__ inline Found find_tile(const CachedArgs& a, const Shape& p, double x)
         const int per = (count + 63) >> 6;
         double w = 0.0;
         for (int i = 0; i < per; ++i)
-            if (lane * per + i < count) w += share_of(a, p, lo + lane * per + i);
+            if (lane * per + i < count) w += need_of(a, p, lo + lane * per + i).share();
         const double to = scanned(w);
         const uint64_t there = __ballot(before + to > x);
         if (!there) return {-1, 0.0};
@@ -487,17 +495,34 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
     const int wave = int(blockIdx.x) * kWaves + same(threadIdx.x >> 6), piece = wave / p.ys, y = wave - piece * p.ys;
     if (piece >= p.pieces) return;
     const int head = y / p.subs, sub = y - head * p.subs;
-    const double all = all_tiles(a, p);
-    double at = piece_begin(p, all, piece);
-    const double stop = piece_begin(p, all, piece + 1);
-    if (same(at < stop) == 0) return;
-    const Found f = find_tile(a, p, at);
+    double all, at, stop;
+    Found f;
+    Need need;
+    if (a.b.seqs <= 64) {
+        // a lane for each sequence: one look at the lengths is all
+        Need mine{0, 0, 0, 0, 0};
+        if (lane < a.b.seqs) mine = need_of(a, p, lane);
+        const double w = mine.share(), to = scanned(w);
+        all = of_lane(to, 63);
+        at = piece_begin(p, all, piece);
+        stop = piece_begin(p, all, piece + 1);
+        if (same(at < stop) == 0) return;
+        const int owner = __builtin_ctzll(__ballot(to > at));
+        f = {owner, of_lane(to, owner) - of_lane(w, owner)};
+        need = of_lane(mine, owner);
+    } else {
+        all = all_tiles(a, p);
+        at = piece_begin(p, all, piece);
+        stop = piece_begin(p, all, piece + 1);
+        if (same(at < stop) == 0) return;
+        f = find_tile(a, p, at);
+        if (same(f.seq) < 0) return;
+        need = need_of(a, p, same(f.seq));
+    }
     int seq = same(f.seq);
-    if (seq < 0) return;
-    Need need = need_of(a, p, seq);
     // row tile, and tile in it
     const double inside = at - f.before;
-    double u = floor(inside / double(need.tiles));
+    double u = need.rts == 1 ? 0.0 : floor(inside / double(need.tiles));
     if (u * need.tiles > inside) u -= 1.0;
     if ((u + 1.0) * need.tiles <= inside) u += 1.0;
     int rt = same(int(u)), tile = same(int(inside - u * need.tiles));
@@ -505,10 +530,9 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
         const int tiles = same(need.tiles), rts = same(need.rts);
         const double left = stop - at;
         const int to = same(double(tiles - tile) <= left ? tiles : tile + int(left));
-        Span sp = span(a.b, seq);
-        sp = {same(sp.first), same(sp.n)};
+        const Span sp = {same(need.first), same(need.n)};
         Walk<FP8, CH, EXACT, NR, NB> w;
-        w.start(a, p, sp, same(cached_of(a.b, seq)), rt, head, sub);
+        w.start(a, p, sp, same(need.past), rt, head, sub);
         const int seen = int((w.most + 63) >> 6);
         w.walk(a, seq, head, tile, to < seen ? to : seen, 1);
         const bool whole = tile == 0 && to == tiles;
@@ -549,88 +573,95 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
     }
 }
 
-// Joins the pieces of row tiles that several waves share: a workgroup takes a row.  Four dimensions are a thread's, and the parts are dealt among the threads that
-// have the same ones; the sums of the first parts are asked for before it is known how they weigh.
-template <int CH>
+// Joins the pieces of row tiles that several waves share.  A row is a wave's, or the four waves' of a workgroup (W = 4) where there are so few rows that the
+// parts of each are worth dealing out.  Four dimensions are a lane's, and the parts go round among the lanes that have the same ones; the sums of the first
+// are asked for before it is known how they weigh.
+template <int CH, int W>
 __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p)
 {
-    constexpr int DP = CH * 16, kQuads = DP / 4, kGroups = 64 * kWaves / kQuads, kAhead = 8, kMost = kWavesAll / (64 * kWaves);
+    constexpr int DP = CH * 16, kQuads = DP / 4, kGroups = 64 * W / kQuads, kAhead = 8;
     const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
+    const int tid = W == 1 ? lane : int(threadIdx.x);
     Item it{int(blockIdx.x), 0};
     if (a.b.start) it = find_item(a.b, int(blockIdx.x), p.per, 1);
+    it = {same(it.seq), same(it.i)};
     if (it.seq < 0) return;
     const Parts found = parts_of(a, p, DP)[blockIdx.x];      // of a sequence without tiles: anything
-    const Span sp = span(a.b, it.seq);
-    const int first = it.i * p.per, tokens = sp.n - first < p.per ? sp.n - first : p.per;
-    const bool none = need_of(a, p, it.seq).tiles == 0;
+    const Need need = need_of(a, p, it.seq);
+    const int w0 = same(found.w0), parts = same(found.n), n = same(need.n), first = it.i * p.per;
+    const bool none = same(need.tiles) == 0;
+    if (!none && parts == 1) return;
+    const int r = W == 1 ? int(blockIdx.z) * kWaves + wave : int(blockIdx.z), t = r / p.heads, h = r - t * p.heads;
     const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
-    const int quad = int(threadIdx.x) % kQuads, d = quad * 4, mine = int(threadIdx.x) / kQuads;
-    if (!none && found.n == 1) return;
-    const int w0 = found.w0, parts = found.n;
-    __shared__ float weight[kWavesAll];
+    if (r >= p.rows || first + t >= n || sub * p.heads + h >= a.group) return;
+    const int quad = tid % kQuads, d = quad * 4, mine = tid / kQuads;
+    _Float16* out = out_row(a, p, same(need.first) + first + t, head, sub, h) + d;
+    if (none) {
+        if (mine == 0 && d < a.c.dim) *reinterpret_cast<f16x4*>(out) = f16x4{0, 0, 0, 0};
+        return;
+    }
+    // part c is in piece w0 + c: the first in its second place, the others in their first
+    auto row_of = [&](int c) { return part_row(a, p, DP, w0 + c, c == 0, int(blockIdx.y), r); };
+    f32x4 ahead[kAhead];
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+        const int c = mine + u * kGroups;
+        ahead[u] = *reinterpret_cast<const f32x4*>(row_of(c < parts ? c : 0) + d);
+    }
+    // references first, over all parts
+    f32x4 stat = {-kInf, 0, -kInf, 0};
+    if (tid < parts) stat = *reinterpret_cast<const f32x4*>(row_of(tid) + DP);
+    float M = stat[0];
+    for (int c = tid + 64 * W; c < parts; c += 64 * W) M = fmaxf(M, row_of(c)[DP]);
+    for (int k = 32; k; k >>= 1) M = fmaxf(M, __shfl_xor(M, k));
     __shared__ float most[kWaves], total[kWaves];
-    __shared__ f32x4 sums[kGroups][kQuads];
-    for (int r = int(blockIdx.z); r < tokens * p.heads; r += int(gridDim.z)) {
-        const int t = r / p.heads, h = r - t * p.heads;
-        if (sub * p.heads + h >= a.group) continue;
-        _Float16* out = out_row(a, p, sp.first + first + t, head, sub, h) + d;
-        if (none) {
-            if (mine == 0 && d < a.c.dim) *reinterpret_cast<f16x4*>(out) = f16x4{0, 0, 0, 0};
-            continue;
-        }
-        // part c is in piece w0 + c: the first in its second place, the others in their first
-        auto row_of = [&](int c) { return part_row(a, p, DP, w0 + c, c == 0, int(blockIdx.y), r); };
-        f32x4 ahead[kAhead];
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            const int c = mine + u * kGroups;
-            ahead[u] = *reinterpret_cast<const f32x4*>(row_of(c < parts ? c : 0) + d);
-        }
-        f32x4 stat[kMost];
-        float M = -kInf;
-#pragma unroll
-        for (int u = 0; u < kMost; ++u) {
-            const int c = int(threadIdx.x) + u * 64 * kWaves;
-            stat[u] = f32x4{-kInf, 0, -kInf, 0};
-            if (c < parts) stat[u] = *reinterpret_cast<const f32x4*>(row_of(c) + DP);
-            M = fmaxf(M, stat[u][0]);
-        }
-        for (int k = 32; k; k >>= 1) M = fmaxf(M, __shfl_xor(M, k));
+    __shared__ f32x4 sums[W == 1 ? 1 : kWaves][kQuads];
+    if constexpr (W > 1) {
         if (lane == 0) most[wave] = M;
         __syncthreads();
 #pragma unroll
         for (int v = 0; v < kWaves; ++v) M = fmaxf(M, most[v]);
-        M = finite(M);
-        float L = 0.0f;
+    }
+    M = finite(M);
+    float L = 0.0f;
+    f32x4 x = {0, 0, 0, 0};
+    for (int c = tid; c < parts; c += 64 * W) {
+        if (c != tid) stat = *reinterpret_cast<const f32x4*>(row_of(c) + DP);
+        L += stat[1] * power(stat[0] - M);
+    }
 #pragma unroll
-        for (int u = 0; u < kMost; ++u) {
-            const int c = int(threadIdx.x) + u * 64 * kWaves;
-            if (c >= parts) break;
-            L += stat[u][1] * power(stat[u][0] - M);
-            weight[c] = power(stat[u][2] - M);
-        }
-        for (int k = 32; k; k >>= 1) L += __shfl_xor(L, k);
+    for (int u = 0; u < kAhead; ++u) {
+        const int c = mine + u * kGroups;
+        if (c < parts) x += ahead[u] * power(row_of(c)[DP + 2] - M);
+    }
+#pragma unroll 4
+    for (int c = mine + kAhead * kGroups; c < parts; c += kGroups) {
+        const float* row = row_of(c);
+        x += *reinterpret_cast<const f32x4*>(row + d) * power(row[DP + 2] - M);
+    }
+    for (int k = 32; k; k >>= 1) L += __shfl_xor(L, k);
+    for (int k = 32; k >= kQuads; k >>= 1) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] += __shfl_xor(x[j], k);
+    }
+    if constexpr (W > 1) {
         if (lane == 0) total[wave] = L;
+        if (lane < kQuads) sums[wave][lane] = x;
         __syncthreads();
-        f32x4 x = {0, 0, 0, 0};
+        L = 0.0f;
+        x = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int u = 0; u < kAhead; ++u)
-            if (mine + u * kGroups < parts) x += ahead[u] * weight[mine + u * kGroups];
-        for (int c = mine + kAhead * kGroups; c < parts; c += kGroups) x += *reinterpret_cast<const f32x4*>(row_of(c) + d) * weight[c];
-        sums[mine][quad] = x;
-        __syncthreads();
-        if (mine == 0 && d < a.c.dim) {
-            L = 0.0f;
-#pragma unroll
-            for (int v = 0; v < kWaves; ++v) L += total[v];
-#pragma unroll
-            for (int v = 1; v < kGroups; ++v) x += sums[v][quad];
-            x *= inverse(L);
-            f16x4 y;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = _Float16(x[j]);
-            *reinterpret_cast<f16x4*>(out) = y;
+        for (int v = 0; v < kWaves; ++v) {
+            L += total[v];
+            x += sums[v][quad];
         }
+    }
+    if (mine == 0 && d < a.c.dim) {
+        x *= inverse(L);
+        f16x4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = _Float16(x[j]);
+        *reinterpret_cast<f16x4*>(out) = y;
     }
 }
 
@@ -647,7 +678,8 @@ hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s
     piece_kernel<FP8, CH, EXACT, NR, 1><<<unsigned((p.pieces * p.ys + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    join_kernel<CH><<<dim3(unsigned(p.tiles), y, unsigned(p.rows < 16 ? p.rows : 16)), 64 * kWaves, 0, s>>>(a, p);
+    if (p.tiles * p.ys * p.rows <= kFewRows) join_kernel<CH, kWaves><<<dim3(unsigned(p.tiles), y, unsigned(p.rows)), 64 * kWaves, 0, s>>>(a, p);
+    else join_kernel<CH, 1><<<dim3(unsigned(p.tiles), y, unsigned((p.rows + kWaves - 1) / kWaves)), 64 * kWaves, 0, s>>>(a, p);
     return hipGetLastError();
 }
 
