@@ -12,6 +12,8 @@
 // Bound: the matrix pipes and, beside them, the softmax's vector instructions; two workgroups on a CU, so that one's products run beside the other's softmax.
 #include "tl_attn.hpp"
 
+#include <type_traits>
+
 namespace tl {
 namespace {
 
@@ -19,8 +21,12 @@ constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;
 constexpr int kTile = 64;                 // keys
 
+// LDS addresses are 32-bit numbers here
+#pragma clang diagnostic ignored "-Wint-to-pointer-cast"
+
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
 
 __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -51,6 +57,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     constexpr int kSteps = kBytes / (NW * 1024);             // transfers of a wave for keys, and as many for values
     constexpr int kRows1 = 1024 / kRow;                      // tokens of a transfer
     constexpr int KK = DP / 16, DT = DP / 32;
+    static_assert(32 * NW % (2 * kTile) == 0, "an even number of tiles before a workgroup's rows");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kBytes];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
@@ -119,110 +126,146 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
     float m = -kInf, l = 0.0f;
 
-    fetch(0, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    for (int t = 0; t < tiles; ++t) {
-        const int buf = t & 1;
-        if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
-        if (t * kTile <= row0 + 31) {                        // else no row of this wave sees the tile
-            const unsigned char* const kt = lds[buf][0];
-            const unsigned char* const vt = lds[buf][1];
-            const bool masked = t * kTile + kTile - 1 > row0;
-            f32x16 s[2];
+    // Where this lane's pieces stand in a tile: keys 2 k + half of token l32, values of 32 dimensions d and tokens 8 e + 4 half + 0 .. 3.  The rest of an
+    // address is a multiple of a row count that the permutation does not see, and goes into the instruction.
+    const uint32_t base = lds_address(&lds[0][0][0]);
+    uint32_t ka[KK], va[DT][2];
 #pragma unroll
-            for (int b = 0; b < 2; ++b) {
+    for (int k = 0; k < KK; ++k) ka[k] = base + l32 * kRow + piece<DP>(l32, 2 * k + half) * 16;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int k = 0; k < KK; ++k) {
-                    const int r = b * 32 + l32;
-                    const f16x8 x = *reinterpret_cast<const f16x8*>(kt + r * kRow + piece<DP>(r, 2 * k + half) * 16);
-                    s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, q[k], s[b], 0, 0, 0);
-                }
-            }
-            const int seen = row - t * kTile - 4 * half;     // key 32 b + 8 (i / 4) + 4 half + i % 4 is seen up to the row's own number
-            if (masked) {
+        for (int e = 0; e < 2; ++e) {
+            const int r = e * 8 + half * 4 + ((lane & 15) >> 2), c = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            va[d][e] = base + kBytes + r * kRow + piece<DP>(r, c) * 16 + (lane & 1) * 8;
+        }
+
+    // One tile, `at` bytes behind the first; MASKED: some row of the wave does not see all of it.
+    auto work = [&](int t, auto at, auto some) {
+        constexpr bool MASKED = decltype(some)::value;
+        f32x16 s[2];
 #pragma unroll
-                for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < 2; ++b) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i)
-                        if (32 * b + 8 * (i >> 2) + (i & 3) > seen) s[b][i] = -kInf;
-            }
-            float mx = -kInf;
+            for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KK; ++k)
+                s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_f16x8*)(ka[k] + (at + b * 32 * kRow)), q[k], s[b], 0, 0, 0);
+        }
+        const int seen = row - t * kTile - 4 * half;         // key 32 b + 8 (i / 4) + 4 half + i % 4 is seen up to the row's own number
+        if constexpr (MASKED) {
 #pragma unroll
             for (int b = 0; b < 2; ++b)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-            mx = mx == -kInf ? mx : mx * scale;
-            if (__any(mx > m + kSlack)) {
-                // each row by itself: what one row sees does not change how another is rounded
-                mx = fmaxf(mx, __shfl_xor(mx, 32));
-                const float to = mx > m + kSlack ? mx : m;
-                const float f = power(m - finite(to));
-                l *= f;
+                for (int i = 0; i < 16; ++i)
+                    if (32 * b + 8 * (i >> 2) + (i & 3) > seen) s[b][i] = -kInf;
+        }
+        float mx = -kInf;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) o[d] *= f;
-                m = to;
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[b][i]), s[b][i + 1]);
+        mx = mx == -kInf ? mx : mx * scale;
+        if (__any(mx > m + kSlack)) {
+            // each row by itself: what one row sees does not change how another is rounded
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float to = mx > m + kSlack ? mx : m;
+            const float f = power(m - finite(to));
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= f;
+            m = to;
+        }
+        const float mb = finite(m);
+        f16x8 w[4];
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                float p = power(__builtin_fmaf(s[b][i], scale, -mb));
+                if (MASKED && 32 * b + 8 * (i >> 2) + (i & 3) > seen) p = 0.0f;
+                l += p;
+                w[b * 2 + (i >> 3)][i & 7] = _Float16(p);
             }
-            const float mb = finite(m);
-            f16x8 w[4];
+        // values of 16 keys and 32 dimensions, in the order of the weights
+        auto values = [&](int u, int d) {
+            union { f16x8 v; i16x4 h[2]; } x;
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
+            for (int e = 0; e < 2; ++e) x.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(va[d][e] + (at + u * 16 * kRow)));
+            return x.v;
+        };
+        if constexpr (MASKED) {
+            // A weight of 0 does not take an infinity or a NaN out of a sum: where the tile has any, they are left out, and added for the rows that see them.
+            f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    float p = power(__builtin_fmaf(s[b][i], scale, -mb));
-                    if (masked && 32 * b + 8 * (i >> 2) + (i & 3) > seen) p = 0.0f;
-                    l += p;
-                    w[b * 2 + (i >> 3)][i & 7] = _Float16(p);
-                }
+            for (int i = 0; i < kBytes / 1024; ++i) zero += *(const lds_f16x8*)(base + kBytes + lane * 16 + (at + i * 1024)) * _Float16(0.0f);
+            bool odd = false;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {                    // 16 keys
+            for (int i = 0; i < 8; ++i) odd |= !(zero[i] == _Float16(0.0f));
+            if (__any(odd)) {
+#pragma unroll 1
+                for (int u = 0; u < 4; ++u) {
+                    f16x8 sees;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    union { f16x8 v; i16x4 h[2]; uint16_t b[8]; } x;
+                    for (int i = 0; i < 8; ++i) sees[i] = u * 16 + 8 * (i >> 2) + (i & 3) > seen ? _Float16(0.0f) : _Float16(1.0f);
+                    const f16x8 wu = u == 0 ? w[0] : u == 1 ? w[1] : u == 2 ? w[2] : w[3];
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int r = u * 16 + e * 8 + half * 4 + ((lane & 15) >> 2);
-                        const int c = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
-                        x.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                            (lds_i16x4*)(vt + r * kRow + piece<DP>(r, c) * 16 + (lane & 1) * 8));
-                    }
-                    if (masked) {
-                        // A weight of 0 does not take an infinity or a NaN out of a sum: they are left out here, and added for the rows that see them.
-                        bool odd = false;
+                    for (int d = 0; d < DT; ++d) {
+                        f16x8 x = values(u, d);
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) odd |= (x.b[i] & 0x7c00) == 0x7c00;
-                        if (__any(odd)) {
-                            const int key = u * 16 + 0;
-                            f16x8 sees, up, down, bad;
+                        for (int kind = 0; kind < 3; ++kind) {
+                            const float add = kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
+                            f16x8 is;
 #pragma unroll
                             for (int i = 0; i < 8; ++i) {
-                                const uint16_t v = x.b[i];
-                                sees[i] = key + 8 * (i >> 2) + (i & 3) > seen ? _Float16(0.0f) : _Float16(1.0f);
-                                up[i] = v == 0x7c00 ? _Float16(1.0f) : _Float16(0.0f);
-                                down[i] = v == 0xfc00 ? _Float16(1.0f) : _Float16(0.0f);
-                                bad[i] = (v & 0x7fff) > 0x7c00 ? _Float16(1.0f) : _Float16(0.0f);
-                                if ((v & 0x7c00) == 0x7c00) x.b[i] = 0;
+                                const float v = float(x[i]);
+                                is[i] = (kind == 2 ? !(v == v) : v == add) ? _Float16(1.0f) : _Float16(0.0f);
                             }
-#pragma unroll 1
-                            for (int kind = 0; kind < 3; ++kind) {
-                                f32x16 c;
+                            f32x16 c;
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) c[i] = 0.0f;
-                                c = __builtin_amdgcn_mfma_f32_32x32x16_f16(kind == 0 ? up : kind == 1 ? down : bad, sees, c, 0, 0, 0);
-                                const float v = kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
+                            for (int i = 0; i < 16; ++i) c[i] = 0.0f;
+                            c = __builtin_amdgcn_mfma_f32_32x32x16_f16(is, sees, c, 0, 0, 0);
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) o[d][i] += c[i] > 0.0f ? v : 0.0f;
-                            }
+                            for (int i = 0; i < 16; ++i) o[d][i] += c[i] > 0.0f ? add : 0.0f;
                         }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) x[i] = fabsf(float(x[i])) < kInf ? x[i] : _Float16(0.0f);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, wu, o[d], 0, 0, 0);
                     }
-                    o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.v, w[u], o[d], 0, 0, 0);
                 }
+                return;
             }
         }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(u, d), w[u], o[d], 0, 0, 0);
+    };
+
+    auto arrived = [] {
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
+    };
+    constexpr std::integral_constant<int, 0> even{};
+    constexpr std::integral_constant<int, 2 * kBytes> odd{};
+    fetch(0, 0);
+    arrived();
+    // tiles that all rows of the workgroup see: an even number
+    int t = 0;
+    for (; t < q0 / kTile; t += 2) {
+        fetch(t + 1, 1);
+        work(t, even, std::false_type{});
+        arrived();
+        fetch(t + 2, 0);
+        work(t + 1, odd, std::false_type{});
+        arrived();
+    }
+#pragma unroll 1
+    for (; t < tiles; ++t) {
+        const int buf = t & 1;
+        if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
+        if (t * kTile <= row0 + 31) work(t, buf * 2 * kBytes, std::true_type{});      // behind, no row of this wave sees a key
+        arrived();
     }
 
     l += __shfl_xor(l, 32);
