@@ -110,6 +110,20 @@ __device__ inline int page_of(const Cache& c, int s, int64_t block)
     return i <= last && p >= 0 && p < c.pages ? p : -1;
 }
 
+// The sum over the wave.
+template <int CTRL, int ROWS>
+__device__ inline int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 15, true); }
+__device__ inline int wave_sum(int x)
+{
+    x += moved<0x111, 15>(x);             // from the lane 1, 2, 4 and 8 before in the row of 16
+    x += moved<0x112, 15>(x);
+    x += moved<0x114, 15>(x);
+    x += moved<0x118, 15>(x);
+    x += moved<0x142, 10>(x);             // a row's last lane to the next row, rows 1 and 3
+    x += moved<0x143, 12>(x);             // lane 31 to rows 2 and 3
+    return __builtin_amdgcn_readlane(x, 63);
+}
+
 // A value that all lanes have, in a scalar register.
 __device__ inline int same(int x) { return __builtin_amdgcn_readfirstlane(x); }
 

@@ -129,8 +129,7 @@ template <int CTRL, int ROWS>
 __device__ inline double moved(double x)
 {
     const uint64_t b = __builtin_bit_cast(uint64_t, x);
-    const uint32_t lo = __builtin_amdgcn_update_dpp(0, int(uint32_t(b)), CTRL, ROWS, 15, true);
-    const uint32_t hi = __builtin_amdgcn_update_dpp(0, int(uint32_t(b >> 32)), CTRL, ROWS, 15, true);
+    const uint32_t lo = tl::moved<CTRL, ROWS>(int(uint32_t(b))), hi = tl::moved<CTRL, ROWS>(int(uint32_t(b >> 32)));
     return __builtin_bit_cast(double, uint64_t(hi) << 32 | lo);
 }
 

@@ -50,6 +50,34 @@ __device__ inline int piece(int r, int c)
     else return c ^ ((((r >> 1) & 1) << 2) | ((r >> 2) & 3));
 }
 
+// Blocks of `rows` query rows of all sequences (64 at most), those with most keys before others: the one in that place.  What is heavy begins early, so that the chip is
+// full until the end; where all fit at once, two to a compute unit, the second half comes in the opposite order, so that a heavy one shares its unit with a light one.
+__device__ inline Item nth_longest(const PromptArgs& a, int rows, int place)
+{
+    const int lane = threadIdx.x & 63;
+    const int n = lane < a.b.seqs ? span(a.b, lane).n : 0, blocks = (n + rows - 1) / rows;
+    auto from = [&](int j) {                                 // blocks with numbers from j on
+        return wave_sum(blocks > j ? blocks - j : 0);
+    };
+    const int all = from(0);
+    if (place >= all) return {-1, 0};
+    const int half = 256 / a.q_heads;
+    if (int64_t(all) * a.q_heads <= 512 && place >= half) place = all - 1 - (place - half);
+    if (a.b.seqs == 1) return {0, all - 1 - place};
+    // the largest number j with more than `place` blocks from j on
+    int lo = 0, hi = 1;
+    while (from(hi) > place) { lo = hi; hi *= 2; }
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (from(mid) > place) lo = mid;
+        else hi = mid;
+    }
+    int skip = place - from(lo + 1);
+    uint64_t there = __ballot(blocks > lo);
+    while (skip-- > 0) there &= there - 1;
+    return {int(__builtin_ctzll(there)), lo};
+}
+
 template <int DP, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
 {
@@ -59,15 +87,17 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     constexpr int KK = DP / 16, DT = DP / 32;
     static_assert(32 * NW % (2 * kTile) == 0, "an even number of tiles before a workgroup's rows");
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kBytes];
+    __shared__ int strange[2][NW];                           // whether the values that a wave brought hold an infinity or a NaN
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
     // heads that share keys go to one chiplet (workgroups are dealt to the 8 of them in turn); the rows with most keys first
     int h = int(blockIdx.x) % a.q_heads;
-    const int item = int(gridDim.x) / a.q_heads - 1 - int(blockIdx.x) / a.q_heads;
+    const int place = int(blockIdx.x) / a.q_heads, places = int(gridDim.x) / a.q_heads;
+    Item it{places - 1 - place, 0};
+    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, 32 * NW, place);
+    else if (a.b.start) it = find_item(a.b, places - 1 - place, 32 * NW, 1);
     if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads >> 3) + (h >> 3);
-    Item it{item, 0};
-    if (a.b.start) it = find_item(a.b, item, 32 * NW, 1);
     const int seq = __builtin_amdgcn_readfirstlane(it.seq);
     if (seq < 0) return;
     const Span sp = span(a.b, seq);
@@ -103,18 +133,36 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     const char* const vbase = reinterpret_cast<const char*>(a.v.p + int64_t(first) * a.v.token + int64_t(g) * a.v.head);
     const uint32_t kstride = uint32_t(a.k.token) * 2u, vstride = uint32_t(a.v.token) * 2u;
     const uint32_t lds0 = lds_address(&lds[0][0][0]) + wave * kSteps * 1024;
+    uint32_t koff[kSteps], voff[kSteps];                     // this lane's pieces of a whole tile
+    bool mine[kSteps];
+#pragma unroll
+    for (int i = 0; i < kSteps; ++i) {
+        const int r = (wave * kSteps + i) * kRows1 + lane / kPieces, c = piece<DP>(r, lane % kPieces);
+        koff[i] = uint32_t(r) * kstride + c * 16;
+        voff[i] = uint32_t(r) * vstride + c * 16;
+        mine[i] = c < pieces;
+    }
     auto fetch = [&](int t, int buf) {
         const char* const kb = kbase + int64_t(t) * kTile * kstride;
         const char* const vb = vbase + int64_t(t) * kTile * vstride;
         const int last = n - 1 - t * kTile;
+        if (last >= kTile - 1) {
 #pragma unroll
-        for (int i = 0; i < kSteps; ++i) {
-            int r = (wave * kSteps + i) * kRows1 + lane / kPieces;
-            const int c = piece<DP>(r, lane % kPieces);
-            if (r > last) r = last;                          // tokens behind the sequence: masked, but no NaN that is not there
-            if (c < pieces) {
-                transfer(kb, uint32_t(r) * kstride + c * 16, lds0 + buf * 2 * kBytes + i * 1024);
-                transfer(vb, uint32_t(r) * vstride + c * 16, lds0 + (buf * 2 + 1) * kBytes + i * 1024);
+            for (int i = 0; i < kSteps; ++i)
+                if (mine[i]) {
+                    transfer(kb, koff[i], lds0 + buf * 2 * kBytes + i * 1024);
+                    transfer(vb, voff[i], lds0 + (buf * 2 + 1) * kBytes + i * 1024);
+                }
+        } else {
+            // tokens behind the sequence are masked: the last one again, no NaN that is not there
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                const int r = (wave * kSteps + i) * kRows1 + lane / kPieces;
+                const uint32_t back = uint32_t(r > last ? r - last : 0);
+                if (mine[i]) {
+                    transfer(kb, koff[i] - back * kstride, lds0 + buf * 2 * kBytes + i * 1024);
+                    transfer(vb, voff[i] - back * vstride, lds0 + (buf * 2 + 1) * kBytes + i * 1024);
+                }
             }
         }
     };
@@ -145,12 +193,20 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         constexpr bool MASKED = decltype(some)::value;
         f32x16 s[2];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[b][i] = 0.0f;
 #pragma unroll
-            for (int k = 0; k < KK; ++k)
+        for (int k = 0; k < KK; ++k)
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
                 s[b] = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_f16x8*)(ka[k] + (at + b * 32 * kRow)), q[k], s[b], 0, 0, 0);
+        // reads six products ahead: one at a time, each product would wait for its read
+        __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+        for (int i = 0; i < 2 * KK; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
         const int seen = row - t * kTile - 4 * half;         // key 32 b + 8 (i / 4) + 4 half + i % 4 is seen up to the row's own number
         if constexpr (MASKED) {
@@ -184,9 +240,13 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
             for (int i = 0; i < 16; ++i) {
                 float p = power(__builtin_fmaf(s[b][i], scale, -mb));
                 if (MASKED && 32 * b + 8 * (i >> 2) + (i & 3) > seen) p = 0.0f;
-                l += p;
                 w[b * 2 + (i >> 3)][i & 7] = _Float16(p);
             }
+        // the sum of the weights as they are rounded, two at a time
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) l = __builtin_amdgcn_fdot2(f16x2{w[u][i], w[u][i + 1]}, f16x2{_Float16(1.0f), _Float16(1.0f)}, l, false);
         // values of 16 keys and 32 dimensions, in the order of the weights
         auto values = [&](int u, int d) {
             union { f16x8 v; i16x4 h[2]; } x;
@@ -196,12 +256,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         };
         if constexpr (MASKED) {
             // A weight of 0 does not take an infinity or a NaN out of a sum: where the tile has any, they are left out, and added for the rows that see them.
-            f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
-#pragma unroll
-            for (int i = 0; i < kBytes / 1024; ++i) zero += *(const lds_f16x8*)(base + kBytes + lane * 16 + (at + i * 1024)) * _Float16(0.0f);
             bool odd = false;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) odd |= !(zero[i] == _Float16(0.0f));
+            for (int v = 0; v < NW; ++v) odd |= strange[t & 1][v] != 0;
             if (__any(odd)) {
 #pragma unroll 1
                 for (int u = 0; u < 4; ++u) {
@@ -246,9 +303,23 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();
     };
+    // looks at the values that this wave has transferred to a buffer, before others may read them
+    auto look = [&](int buf) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i)
+            zero += *(const lds_f16x8*)(base + kBytes + (wave * kSteps + i) * 1024 + lane * 16 + buf * 2 * kBytes) * _Float16(0.0f);
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) odd |= !(zero[i] == _Float16(0.0f));
+        odd = __any(odd);
+        if (lane == 0) strange[buf][wave] = odd;
+    };
     constexpr std::integral_constant<int, 0> even{};
     constexpr std::integral_constant<int, 2 * kBytes> odd{};
     fetch(0, 0);
+    if (q0 == 0) look(0);
     arrived();
     // tiles that all rows of the workgroup see: an even number
     int t = 0;
@@ -258,6 +329,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         arrived();
         fetch(t + 2, 0);
         work(t + 1, odd, std::false_type{});
+        if (t + 2 == q0 / kTile) look(0);
         arrived();
     }
 #pragma unroll 1
@@ -265,6 +337,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         const int buf = t & 1;
         if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
         if (t * kTile <= row0 + 31) work(t, buf * 2 * kBytes, std::true_type{});      // behind, no row of this wave sees a key
+        if (t + 1 < tiles) look(buf ^ 1);
         arrived();
     }
 
