@@ -107,21 +107,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     const int g = h / a.group;
     const int row0 = q0 + wave * 32, row = row0 + l32;       // this lane's query in the sequence
     const int pieces = a.dim >> 3;
-    const bool flip = a.scale < 0.0f;
-    const float scale = fabsf(a.scale);
-
-    f16x8 q[KK];
-    {
-        const _Float16* from = a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head;
-#pragma unroll
-        for (int k = 0; k < KK; ++k) {
-            const int c = 2 * k + half;
-            f16x8 x = *reinterpret_cast<const f16x8*>(from + (c < pieces ? c : 0) * 8);
-            if (c >= pieces) x = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
-            if (flip) x = -x;
-            q[k] = x;
-        }
-    }
+    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);      // with queries that are turned round, or 0: the largest product is the largest score
 
     if (pieces < kPieces) {                                  // dimensions beyond the head are never transferred
         for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 64 * NW) reinterpret_cast<u32x4*>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
@@ -167,11 +153,27 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         }
     };
 
+    fetch(0, 0);
+    f16x8 q[KK];
+    {
+        const _Float16* from = a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head;
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+            const int c = 2 * k + half;
+            q[k] = *reinterpret_cast<const f16x8*>(from + (c < pieces ? c : 0) * 8);
+            if (c >= pieces || a.scale == 0.0f) q[k] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        }
+        if (a.scale < 0.0f) {
+#pragma unroll
+            for (int k = 0; k < KK; ++k) q[k] = -q[k];
+        }
+    }
     f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    bool left_out = false;                                   // infinities and NaN of values, of which some row must not hear
     float m = -kInf, l = 0.0f;
 
     // Where this lane's pieces stand in a tile: keys 2 k + half of token l32, values of 32 dimensions d and tokens 8 e + 4 half + 0 .. 3.  The rest of an
@@ -238,9 +240,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                float p = power(__builtin_fmaf(s[b][i], scale, -mb));
-                if (MASKED && 32 * b + 8 * (i >> 2) + (i & 3) > seen) p = 0.0f;
-                w[b * 2 + (i >> 3)][i & 7] = _Float16(p);
+                w[b * 2 + (i >> 3)][i & 7] = _Float16(power(__builtin_fmaf(s[b][i], scale, -mb)));
             }
         // the sum of the weights as they are rounded, two at a time
 #pragma unroll
@@ -255,41 +255,21 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
             return x.v;
         };
         if constexpr (MASKED) {
-            // A weight of 0 does not take an infinity or a NaN out of a sum: where the tile has any, they are left out, and added for the rows that see them.
+            // A weight of 0 does not take an infinity or a NaN out of a sum: where the tile has any, they are left out here and added at the end.
             bool odd = false;
 #pragma unroll
             for (int v = 0; v < NW; ++v) odd |= strange[t & 1][v] != 0;
             if (__any(odd)) {
-#pragma unroll 1
-                for (int u = 0; u < 4; ++u) {
-                    f16x8 sees;
+                left_out = true;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) sees[i] = u * 16 + 8 * (i >> 2) + (i & 3) > seen ? _Float16(0.0f) : _Float16(1.0f);
-                    const f16x8 wu = u == 0 ? w[0] : u == 1 ? w[1] : u == 2 ? w[2] : w[3];
+                for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
                         f16x8 x = values(u, d);
 #pragma unroll
-                        for (int kind = 0; kind < 3; ++kind) {
-                            const float add = kind == 0 ? kInf : kind == 1 ? -kInf : __builtin_nanf("");
-                            f16x8 is;
-#pragma unroll
-                            for (int i = 0; i < 8; ++i) {
-                                const float v = float(x[i]);
-                                is[i] = (kind == 2 ? !(v == v) : v == add) ? _Float16(1.0f) : _Float16(0.0f);
-                            }
-                            f32x16 c;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) c[i] = 0.0f;
-                            c = __builtin_amdgcn_mfma_f32_32x32x16_f16(is, sees, c, 0, 0, 0);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) o[d][i] += c[i] > 0.0f ? add : 0.0f;
-                        }
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = fabsf(float(x[i])) < kInf ? x[i] : _Float16(0.0f);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, wu, o[d], 0, 0, 0);
+                        for (int i = 0; i < 8; ++i) x[i] = __builtin_fabsf16(x[i]) < _Float16(kInf) ? x[i] : _Float16(0.0f);
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w[u], o[d], 0, 0, 0);
                     }
-                }
                 return;
             }
         }
@@ -318,7 +298,6 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     };
     constexpr std::integral_constant<int, 0> even{};
     constexpr std::integral_constant<int, 2 * kBytes> odd{};
-    fetch(0, 0);
     if (q0 == 0) look(0);
     arrived();
     // tiles that all rows of the workgroup see: an even number
@@ -341,21 +320,45 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         arrived();
     }
 
+    if (left_out) {
+        // values of the tokens that only some rows see, once more: an infinity or a NaN goes to the rows that see it
+        for (int key = q0; key < most; ++key) {
+            const _Float16* v = reinterpret_cast<const _Float16*>(vbase) + int64_t(key) * a.v.token;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int at = d * 32 + i * 8 + half * 4;
+                    const f16x4 x = *reinterpret_cast<const f16x4*>(v + (at < a.dim ? at : 0));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (key <= row && !(__builtin_fabsf16(x[j]) < _Float16(kInf))) o[d][i * 4 + j] += float(x[j]);
+                }
+        }
+    }
     l += __shfl_xor(l, 32);
     const float f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
-    if (row < n) {
-        _Float16* out = a.out.p + int64_t(first + row) * a.out.token + int64_t(h) * a.out.head;
+    // Through LDS, which nobody reads any more, so that whole rows are written at once.  A row has 16 bytes beside it: rows begin in different banks.
+    constexpr int kOut = kRow + 16;
+    static_assert(NW * 32 * kOut <= 4 * kBytes, "a workgroup's rows in LDS");
+    unsigned char* const rows = &lds[0][0][0] + wave * 32 * kOut;
 #pragma unroll
-        for (int d = 0; d < DT; ++d)
+    for (int d = 0; d < DT; ++d)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int at = d * 32 + i * 8 + half * 4;
-                if (at >= a.dim) continue;
-                f16x4 y;
+        for (int i = 0; i < 4; ++i) {
+            f16x4 y;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = _Float16(o[d][i * 4 + j] * f);
-                *reinterpret_cast<f16x4*>(out + at) = y;
-            }
+            for (int j = 0; j < 4; ++j) y[j] = _Float16(o[d][i * 4 + j] * f);
+            *reinterpret_cast<f16x4*>(rows + l32 * kOut + (d * 32 + i * 8 + half * 4) * 2) = y;
+        }
+    // a wave reads what it wrote itself
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int c = lane % kPieces;
+#pragma unroll
+    for (int i = 0; i < 32 / kRows1; ++i) {
+        const int r = i * kRows1 + lane / kPieces;
+        if (row0 + r < n && c < pieces)
+            *reinterpret_cast<f16x8*>(a.out.p + int64_t(first + row0 + r) * a.out.token + int64_t(h) * a.out.head + c * 8) = *reinterpret_cast<const f16x8*>(rows + r * kOut + c * 16);
     }
 }
 
