@@ -265,10 +265,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
-                        f16x8 x = values(u, d);
+                        // an exponent of ones carries into the sign's place
+                        union { f16x8 v; uint32_t w[4]; } x{values(u, d)};
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) x[i] = __builtin_fabsf16(x[i]) < _Float16(kInf) ? x[i] : _Float16(0.0f);
-                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x, w[u], o[d], 0, 0, 0);
+                        for (int i = 0; i < 4; ++i) {
+                            const uint32_t bad = (((x.w[i] & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15;
+                            x.w[i] &= ~(bad * 0xffffu);
+                        }
+                        o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.v, w[u], o[d], 0, 0, 0);
                     }
                 return;
             }
@@ -311,13 +315,19 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         if (t + 2 == q0 / kTile) look(0);
         arrived();
     }
-#pragma unroll 1
-    for (; t < tiles; ++t) {
-        const int buf = t & 1;
-        if (t + 1 < tiles) fetch(t + 1, buf ^ 1);
-        if (t * kTile <= row0 + 31) work(t, buf * 2 * kBytes, std::true_type{});      // behind, no row of this wave sees a key
-        if (t + 1 < tiles) look(buf ^ 1);
+    // tiles that some row does not see, or not all of
+    auto last = [&](auto buf) {
+        constexpr int B = decltype(buf)::value != 0;
+        if (t + 1 < tiles) fetch(t + 1, B ^ 1);
+        if (t * kTile <= row0 + 31) work(t, buf, std::true_type{});      // behind, no row of this wave sees a key
+        if (t + 1 < tiles) look(B ^ 1);
         arrived();
+        ++t;
+    };
+#pragma unroll 1
+    while (t < tiles) {
+        last(even);
+        if (t < tiles) last(odd);
     }
 
     if (left_out) {
