@@ -78,16 +78,16 @@ __device__ inline Item nth_longest(const PromptArgs& a, int rows, int place)
     return {int(__builtin_ctzll(there)), lo};
 }
 
-template <int DP, int NW>
+template <int DP, int NW, int NB>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
 {
     constexpr int kRow = DP * 2, kPieces = DP / 8, kBytes = kTile * kRow;
     constexpr int kSteps = kBytes / (NW * 1024);             // transfers of a wave for keys, and as many for values
     constexpr int kRows1 = 1024 / kRow;                      // tokens of a transfer
     constexpr int KK = DP / 16, DT = DP / 32;
-    static_assert(32 * NW % (2 * kTile) == 0, "an even number of tiles before a workgroup's rows");
-    __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kBytes];
-    __shared__ int strange[2][NW];                           // whether the values that a wave brought hold an infinity or a NaN
+    static_assert(32 * NW % (NB * kTile) == 0, "whole rounds of buffers before a workgroup's rows");
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[NB][2][kBytes];
+    __shared__ int strange[NB][NW];                           // whether the values that a wave brought hold an infinity or a NaN
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);      // with queries that are turned round, or 0: the largest product is the largest score
 
     if (pieces < kPieces) {                                  // dimensions beyond the head are never transferred
-        for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 64 * NW) reinterpret_cast<u32x4*>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
+        for (int i = threadIdx.x; i < NB * 2 * kBytes / 16; i += 64 * NW) reinterpret_cast<u32x4*>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
     const int most = q0 + 32 * NW < n ? q0 + 32 * NW : n;    // keys that the workgroup sees
@@ -129,6 +129,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         mine[i] = c < pieces;
     }
     auto fetch = [&](int t, int buf) {
+        if (t > tiles - 1) t = tiles - 1;                    // so that the number of transfers on their way is always the same
         const char* const kb = kbase + int64_t(t) * kTile * kstride;
         const char* const vb = vbase + int64_t(t) * kTile * vstride;
         const int last = n - 1 - t * kTile;
@@ -153,7 +154,8 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         }
     };
 
-    fetch(0, 0);
+#pragma unroll
+    for (int u = 0; u < NB - 1; ++u) fetch(u, u);
     f16x8 q[KK];
     {
         const _Float16* from = a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head;
@@ -193,6 +195,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     // One tile, `at` bytes behind the first; MASKED: some row of the wave does not see all of it.
     auto work = [&](int t, auto at, auto some) {
         constexpr bool MASKED = decltype(some)::value;
+        constexpr int B = decltype(at)::value / (2 * kBytes);
         f32x16 s[2];
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -258,7 +261,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
             // A weight of 0 does not take an infinity or a NaN out of a sum: where the tile has any, they are left out here and added at the end.
             bool odd = false;
 #pragma unroll
-            for (int v = 0; v < NW; ++v) odd |= strange[t & 1][v] != 0;
+            for (int v = 0; v < NW; ++v) odd |= strange[B][v] != 0;
             if (__any(odd)) {
                 left_out = true;
 #pragma unroll
@@ -283,13 +286,14 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
             for (int d = 0; d < DT; ++d) o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(values(u, d), w[u], o[d], 0, 0, 0);
     };
 
-    auto arrived = [] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // the next tile is there, and all waves are done with the last one
+    auto arrived = [&] {
+        asm volatile("s_waitcnt vmcnt(%0)" : : "i"((NB - 2) * 2 * kSteps) : "memory");
         __syncthreads();
     };
     // looks at the values that this wave has transferred to a buffer, before others may read them
     auto look = [&](int buf) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" : : "i"((NB - 2) * 2 * kSteps) : "memory");
         f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < kSteps; ++i)
@@ -300,35 +304,40 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
         odd = __any(odd);
         if (lane == 0) strange[buf][wave] = odd;
     };
-    constexpr std::integral_constant<int, 0> even{};
-    constexpr std::integral_constant<int, 2 * kBytes> odd{};
     if (q0 == 0) look(0);
     arrived();
-    // tiles that all rows of the workgroup see: an even number
+    // Tiles that all rows of the workgroup see, a round of buffers at a time; while a tile is worked on, the NB - 1 after it are on their way.
     int t = 0;
-    for (; t < q0 / kTile; t += 2) {
-        fetch(t + 1, 1);
-        work(t, even, std::false_type{});
+    auto whole = [&](auto buf) {
+        constexpr int B = decltype(buf)::value;
+        fetch(t + NB - 1, (B + NB - 1) % NB);
+        work(t, std::integral_constant<int, B * 2 * kBytes>{}, std::false_type{});
+        ++t;
+        if (B == NB - 1 && t == q0 / kTile) look(0);
         arrived();
-        fetch(t + 2, 0);
-        work(t + 1, odd, std::false_type{});
-        if (t + 2 == q0 / kTile) look(0);
-        arrived();
-    }
+    };
     // tiles that some row does not see, or not all of
     auto last = [&](auto buf) {
-        constexpr int B = decltype(buf)::value != 0;
-        if (t + 1 < tiles) fetch(t + 1, B ^ 1);
-        if (t * kTile <= row0 + 31) work(t, buf, std::true_type{});      // behind, no row of this wave sees a key
-        if (t + 1 < tiles) look(B ^ 1);
-        arrived();
+        constexpr int B = decltype(buf)::value;
+        if (t >= tiles) return;
+        fetch(t + NB - 1, (B + NB - 1) % NB);
+        if (t * kTile <= row0 + 31) work(t, std::integral_constant<int, B * 2 * kBytes>{}, std::true_type{});      // behind, no row of this wave sees a key
         ++t;
+        if (t < tiles) look((B + 1) % NB);
+        arrived();
     };
-#pragma unroll 1
-    while (t < tiles) {
-        last(even);
-        if (t < tiles) last(odd);
-    }
+    auto round = [&](auto step) {
+        step(std::integral_constant<int, 0>{});
+        step(std::integral_constant<int, 1>{});
+        if constexpr (NB > 2) {
+            step(std::integral_constant<int, 2>{});
+            step(std::integral_constant<int, 3>{});
+        }
+    };
+    while (t < q0 / kTile) round(whole);
+    round(last);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
 
     if (left_out) {
         // values of the tokens that only some rows see, once more: an infinity or a NaN goes to the rows that see it
@@ -350,7 +359,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     const float f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
     // Through LDS, which nobody reads any more, so that whole rows are written at once.  A row has 16 bytes beside it: rows begin in different banks.
     constexpr int kOut = kRow + 16;
-    static_assert(NW * 32 * kOut <= 4 * kBytes, "a workgroup's rows in LDS");
+    static_assert(NW * 32 * kOut <= NB * 2 * kBytes, "a workgroup's rows in LDS");
     unsigned char* const rows = &lds[0][0][0] + wave * 32 * kOut;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -376,11 +385,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
 {
-    constexpr int NW = 4;
-    const int64_t items = a.b.start ? a.b.tokens / (32 * NW) + a.b.seqs : a.b.seqs;
-    const unsigned grid = unsigned(items * a.q_heads);
-    if (a.dim <= 64) prompt_kernel<64, NW><<<grid, 64 * NW, 0, s>>>(a);
-    else prompt_kernel<128, NW><<<grid, 64 * NW, 0, s>>>(a);
+    const auto grid = [&](int rows) { return unsigned((a.b.start ? a.b.tokens / rows + a.b.seqs : a.b.seqs) * a.q_heads); };
+    if (a.dim <= 64) prompt_kernel<64, 4, 2><<<grid(128), 256, 0, s>>>(a);
+    else prompt_kernel<128, 4, 2><<<grid(128), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
