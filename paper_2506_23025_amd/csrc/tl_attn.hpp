@@ -29,6 +29,7 @@ struct Rope {
     const float* table;                   // NULL: no rotation
     int64_t positions;
     int rot, pairs;
+    int wide;                             // rows of the table and groups of 8 dimensions can be read 16 bytes at a time
 };
 
 struct AppendArgs {

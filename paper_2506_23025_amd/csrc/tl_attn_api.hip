@@ -122,7 +122,9 @@ tl_status tl_kv_append(const tl_append_job* job, void* stream)
         if (!r.table) return TL_ERR_NULL;
         if (r.positions < 1 || r.positions >= (int64_t(1) << 40) || r.rot_dim < 2 || r.rot_dim % 2 != 0 || r.rot_dim > j.head_dim) return TL_ERR_SHAPE;
         if (!aligned(r.table, 4)) return TL_ERR_ALIGN;
-        a.r = {r.table, r.positions, int(r.rot_dim), r.pairs != 0};
+        const bool pairs = r.pairs != 0;
+        const bool wide = aligned(r.table, 16) && r.rot_dim % (pairs ? 8 : 16) == 0;
+        a.r = {r.table, r.positions, int(r.rot_dim), pairs, wide};
     }
     if ((e = heads_status(j.q, j.q_heads)) != TL_OK || (e = heads_status(j.k, j.kv_heads)) != TL_OK) return e;
     if (j.q_out.ptr && (e = heads_status(j.q_out, j.q_heads)) != TL_OK) return e;

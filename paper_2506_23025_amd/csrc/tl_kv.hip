@@ -1,8 +1,9 @@
 // Rotation of queries and keys, and the way of keys and values into the paged 8-bit cache.
 //
-// A wave takes up to 16 tokens of one head, those of one call that fall into one block of the cache (positions 16 b .. 16 b + 15 of a sequence),
-// since they share a scale: the tokens' values stay in its registers (8 dimensions a lane, so dim / 8 lanes to a token), the largest magnitude is
-// a reduction over the wave, and nobody else touches the block.  Query heads take the same way without the cache.
+// A wave takes a block of the cache (16 positions of a sequence) of one head after another, with those of its tokens that the call brings: the tokens of a
+// block share a scale, nobody else touches the block, and the cosines and sines of the 16 positions stay in registers for all heads.  A lane has 8
+// dimensions (16 bytes) of T consecutive tokens, T = 4, 2 or 1 for heads of up to 128, 64 or 32 dimensions, so that a value's codes of T tokens, neighbours in memory,
+// are written together.  Query heads take the same way without the cache.
 // Bound: memory for prompts; for a step of a few sequences the chain of dependent reads (length, page, scale).
 #include "tl_attn.hpp"
 
@@ -14,202 +15,431 @@ constexpr int kWaves = 4;
 template <bool FP8>
 __device__ inline float top() { return FP8 ? 448.0f : 127.0f; }
 
-// The nearest code of x, |x| at most a rounding beyond the top; NaN has none and gives anything.
+// The codes of a and b, at most a rounding beyond the top, in the low and the second byte; a NaN gives anything.
 template <bool FP8>
-__device__ inline uint32_t code_of(float x)
+__device__ inline uint32_t two_codes(float a, float b)
 {
-    x = fminf(fmaxf(x, -top<FP8>()), top<FP8>());
-    if constexpr (FP8) return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(x, x, 0, false)) & 255u;
-    else return uint32_t(int(rintf(x))) & 255u;
+    a = fminf(fmaxf(a, -top<FP8>()), top<FP8>());
+    b = fminf(fmaxf(b, -top<FP8>()), top<FP8>());
+    if constexpr (FP8) return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false)) & 0xffffu;
+    else return (uint32_t(int(rintf(a))) & 255u) | (uint32_t(int(rintf(b))) & 255u) << 8;
 }
 
 template <bool FP8>
-__device__ inline float value_of(uint32_t code)
+__device__ inline uint32_t four_codes(float a, float b, float c, float d)
 {
-    if constexpr (FP8) return __builtin_amdgcn_cvt_f32_fp8(int(code), 0);
-    else return float(int(int8_t(code)));
+    return two_codes<FP8>(a, b) | two_codes<FP8>(c, d) << 16;
+}
+
+template <bool FP8, int I>
+__device__ inline float value_of(uint32_t codes)
+{
+    if constexpr (FP8) return __builtin_amdgcn_cvt_f32_fp8(int(codes), I);
+    else return float(int(int8_t(codes >> (8 * I))));
 }
 
 template <bool FP8>
 __device__ inline uint32_t recode4(uint32_t w, float ratio)
 {
-    uint32_t r = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r |= code_of<FP8>(value_of<FP8>((w >> (8 * i)) & 255u) * ratio) << (8 * i);
-    return r;
+    return four_codes<FP8>(value_of<FP8, 0>(w) * ratio, value_of<FP8, 1>(w) * ratio, value_of<FP8, 2>(w) * ratio, value_of<FP8, 3>(w) * ratio);
 }
 
-// Dimensions d .. d + 7 of one token's head, rotated.  `row` is where the head begins.
-__device__ inline void rotated(const Rope& r, const _Float16* row, int d, int64_t pos, float (&x)[8])
+// How 8 dimensions of a lane are turned: not at all; as 4 pairs of neighbours; with the 8 half a head away; one by one (rows of the table or
+// halves that are no multiples of 16 bytes).
+enum Turn { kNone, kPairs, kHalves, kAny };
+
+// Cosines and sines for 8 dimensions from d on at one position.  pairs: 4 and 4 (c0 and s0); halves: 8 and 8.
+struct Angles { f32x4 c0, c1, s0, s1; };
+
+template <Turn TURN>
+__device__ inline Angles angles(const Rope r, int64_t pos, int d)
+{
+    Angles a{};
+    if constexpr (TURN == kPairs || TURN == kHalves) {
+        const int half = r.rot >> 1, j = TURN == kPairs ? d >> 1 : d < half ? d : d - half;
+        const bool there = pos < r.positions;
+        const float* t = r.table + (there ? pos : 0) * r.rot + j;
+        a.c0 = *reinterpret_cast<const f32x4*>(t);
+        a.s0 = *reinterpret_cast<const f32x4*>(t + half);
+        if constexpr (TURN == kHalves) {
+            a.c1 = *reinterpret_cast<const f32x4*>(t + 4);
+            a.s1 = *reinterpret_cast<const f32x4*>(t + half + 4);
+        }
+        if (!there) {
+            const float nan = __builtin_nanf("");
+            a.c0 = a.c1 = f32x4{nan, nan, nan, nan};
+        }
+    }
+    return a;
+}
+
+// Eight dimensions from d on, in 32 bits, rotated.  `other`: their partners (halves); `row`: where the head begins.
+template <Turn TURN>
+__device__ inline void turn8(const Rope r, int64_t pos, const _Float16* row, int d, f16x8 own, f16x8 other, const Angles cs, float (&x)[8])
 {
 #pragma clang fp contract(off)
-    const f16x8 own = *reinterpret_cast<const f16x8*>(row + d);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = float(own[i]);
-    if (!r.table || d >= r.rot) return;
     const int half = r.rot >> 1;
-    if (pos >= r.positions) {
+    if (TURN == kNone || d >= r.rot) return;
+    if constexpr (TURN == kPairs) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) if (d + i < r.rot) x[i] = __builtin_nanf("");
-        return;
-    }
-    const float* cs = r.table + pos * r.rot;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int e = d + i;
-        if (e >= r.rot) break;
-        const bool second = r.pairs ? (e & 1) : e >= half;
-        const int j = r.pairs ? e >> 1 : second ? e - half : e;
-        const int other = r.pairs ? e ^ 1 : second ? e - half : e + half;
-        const float c = cs[j], s = cs[half + j], y = float(row[other]);
-        const float p = x[i] * c, q = y * s;
-        x[i] = second ? p + q : p - q;
-    }
-}
-
-// One head of the block: `n` tokens in the slots from `slot` on, of whom token i stands in row `row0 + i`.
-template <bool FP8, bool KEY>
-__device__ inline void put_block(const AppendArgs& a, const Heads& in, int head, int row0, int n, int slot, int64_t pos, int page, int blk,
-                                 uint8_t* codes, float* scales)
-{
-#pragma clang fp contract(off)
-    const int lane = threadIdx.x & 63, per = a.dim >> 3, at_once = 64 / per;
-    const int t_lane = lane / per, d = (lane - t_lane * per) * 8;
-    float x[4][8];
-    float amax = 0.0f;
-    bool odd = false;                                    // a NaN or an infinity
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int t = u * at_once + t_lane;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[u][i] = 0.0f;
-        if (t_lane >= at_once || t >= n) continue;
-        const _Float16* row = in.p + int64_t(row0 + t) * in.token + int64_t(head) * in.head;
-        if constexpr (KEY) {
-            rotated(a.r, row, d, pos + t, x[u]);
-            if (a.k_out.p) {
-                f16x8 o;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) o[i] = _Float16(x[u][i]);
-                *reinterpret_cast<f16x8*>(a.k_out.p + int64_t(row0 + t) * a.k_out.token + int64_t(head) * a.k_out.head + d) = o;
-            }
-        } else {
-            const f16x8 own = *reinterpret_cast<const f16x8*>(row + d);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = float(own[i]);
+        for (int i = 0; i < 4; ++i) {
+            const float c = cs.c0[i], s = cs.s0[i], p = x[2 * i], q = x[2 * i + 1];
+            const float pc = p * c, qs = q * s, qc = q * c, ps = p * s;
+            x[2 * i] = pc - qs;
+            x[2 * i + 1] = qc + ps;
         }
+    } else if constexpr (TURN == kHalves) {
+        const bool second = d >= half;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            amax = fmaxf(amax, fabsf(x[u][i]));
-            odd |= !(fabsf(x[u][i]) < __builtin_inff());
+            const float p = x[i] * (i < 4 ? cs.c0[i & 3] : cs.c1[i & 3]), q = float(other[i]) * (i < 4 ? cs.s0[i & 3] : cs.s1[i & 3]);
+            x[i] = second ? p + q : p - q;
         }
-    }
-    if (page < 0) return;
-    for (int s = 32; s; s >>= 1) amax = fmaxf(amax, __shfl_xor(amax, s));
-    odd = __any(odd);
-    const int blocks = 1 << a.c.page_shift, chunks = a.dim >> 4;
-    const int64_t block = (int64_t(page) * a.kv_heads + head) * blocks + blk;
-    uint8_t* const to = codes + block * (int64_t(16) * a.dim);
-    const float was = slot ? scales[block] : 0.0f;
-    float now = fmaxf(was, amax / top<FP8>());
-    if (odd || !(was == was)) now = __builtin_nanf("");
-    if (lane == 0) scales[block] = now;
-    if (slot && now > was) {                             // what stands before the new tokens, in the new scale
-        const float ratio = was / now;
-        if constexpr (KEY) {
-            // 4 tokens of 16 dimensions are 64 bytes: one lane, one token
-            for (int i = lane; i < slot * chunks; i += 64) {
-                const int t = i / chunks, c = i - t * chunks;
-                uint32_t* w = reinterpret_cast<uint32_t*>(to + ((t >> 2) * chunks + c) * 64 + (t & 3) * 16);
+    } else if constexpr (TURN == kAny) {
+        const bool there = pos < r.positions;
+        const float* t = r.table + (there ? pos : 0) * r.rot;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) w[j] = recode4<FP8>(w[j], ratio);
-            }
-        } else {
-            for (int i = lane; i < a.dim; i += 64) {
-                for (int t = 0; t < slot; ++t) to[i * 16 + t] = uint8_t(code_of<FP8>(value_of<FP8>(to[i * 16 + t]) * ratio));
-            }
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int t = u * at_once + t_lane;
-        if (t_lane >= at_once || t >= n) continue;
-        const int at = slot + t;
-        uint32_t w[2] = {0, 0};
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i >> 2] |= (now > 0.0f ? code_of<FP8>(x[u][i] / now) : 0u) << (8 * (i & 3));
-        if constexpr (KEY) {
-            *reinterpret_cast<u32x2*>(to + ((at >> 2) * chunks + (d >> 4)) * 64 + (at & 3) * 16 + (d & 15)) = u32x2{w[0], w[1]};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) to[(d + i) * 16 + at] = uint8_t(w[i >> 2] >> (8 * (i & 3)));
+        for (int i = 0; i < 8; ++i) {
+            const int e = d + i;
+            if (e >= r.rot) break;
+            const bool second = r.pairs ? (e & 1) : e >= half;
+            const int j = r.pairs ? e >> 1 : second ? e - half : e;
+            const int o = r.pairs ? e ^ 1 : second ? e - half : e + half;
+            const float p = x[i] * t[j], q = float(row[o]) * t[half + j];
+            x[i] = !there ? __builtin_nanf("") : second ? p + q : p - q;
         }
     }
 }
 
-__device__ inline void turn_head(const AppendArgs& a, const Heads& in, const Heads& out, int head, int row0, int n, int64_t pos, bool used)
+template <Turn TURN>
+__device__ inline f16x8 partners(const Rope r, const _Float16* row, int d)
 {
-    const int lane = threadIdx.x & 63, per = a.dim >> 3, at_once = 64 / per;
-    const int t_lane = lane / per, d = (lane - t_lane * per) * 8;
-    if (t_lane >= at_once) return;
+    if constexpr (TURN == kHalves) {
+        const int half = r.rot >> 1;
+        if (d < r.rot) return *reinterpret_cast<const f16x8*>(row + (d < half ? d + half : d - half));
+    }
+    return f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+}
+
+// What stands in the first `slots` slots of a block, in another scale; lanes i, i + step, ... share it.
+template <bool FP8, bool KEY>
+__device__ inline void recode(uint8_t* to, int dim, int slots, float ratio, int i, int step)
+{
+    const int chunks = dim >> 4;
+    if constexpr (KEY) {
+        for (; i < slots * chunks; i += step) {
+            const int t = i / chunks, c = i - t * chunks;
+            uint32_t* w = reinterpret_cast<uint32_t*>(to + ((t >> 2) * chunks + c) * 64 + (t & 3) * 16);
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int t = u * at_once + t_lane;
-        if (t >= n) break;
-        float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (used) rotated(a.r, in.p + int64_t(row0 + t) * in.token + int64_t(head) * in.head, d, pos + t, x);
-        f16x8 o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = _Float16(x[i]);
-        *reinterpret_cast<f16x8*>(out.p + int64_t(row0 + t) * out.token + int64_t(head) * out.head + d) = o;
+            for (int j = 0; j < 4; ++j) w[j] = recode4<FP8>(w[j], ratio);
+        }
+    } else {
+        // whole words of 4 tokens, then the tokens that share a word with new ones
+        for (; i < dim; i += step) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(to + i * 16);
+            int t = 0;
+            for (; t + 4 <= slots; t += 4) w[t >> 2] = recode4<FP8>(w[t >> 2], ratio);
+            for (; t < slots; ++t) to[i * 16 + t] = uint8_t(two_codes<FP8>(value_of<FP8, 0>(to[i * 16 + t]) * ratio, 0.0f));
+        }
     }
 }
 
+// The scale of a block that takes tokens with magnitudes up to amax (or an infinity or a NaN: odd) and had `was` (0 if it held nothing).
 template <bool FP8>
-__global__ __launch_bounds__(64 * kWaves) void append_kernel(AppendArgs a)
+__device__ inline float scale_of(float was, float amax, bool odd)
+{
+    const float now = fmaxf(was, amax / top<FP8>());
+    return odd || !(was == was) ? __builtin_nanf("") : now;
+}
+
+// One token's codes of 8 dimensions from d on.
+template <bool FP8, bool KEY>
+__device__ inline void put_codes(uint8_t* to, int dim, int slot, int d, const float (&x)[8])
+{
+    if constexpr (KEY) {
+        *reinterpret_cast<u32x2*>(to + ((slot >> 2) * (dim >> 4) + (d >> 4)) * 64 + (slot & 3) * 16 + (d & 15)) =
+            u32x2{four_codes<FP8>(x[0], x[1], x[2], x[3]), four_codes<FP8>(x[4], x[5], x[6], x[7])};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const uint32_t w = two_codes<FP8>(x[i], x[i + 1]);
+            to[(d + i) * 16 + slot] = uint8_t(w);
+            to[(d + i + 1) * 16 + slot] = uint8_t(w >> 8);
+        }
+    }
+}
+
+__device__ inline void put_row(const Heads& out, int64_t row, int head, int d, const float (&x)[8])
+{
+    f16x8 o;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = _Float16(x[i]);
+    *reinterpret_cast<f16x8*>(out.p + row * out.token + int64_t(head) * out.head + d) = o;
+}
+
+// One token of every sequence: 16 lanes take a head, so a wave four.
+template <bool FP8, Turn TURN>
+__global__ __launch_bounds__(64 * kWaves) void step_kernel(AppendArgs a)
+{
+#pragma clang fp contract(off)
+    const int seq = blockIdx.x, lane = threadIdx.x & 15, kv = a.kv_heads;
+    const int unit = int(blockIdx.y) * (4 * kWaves) + int(threadIdx.x >> 4), d = lane * 8;
+    const bool here = d < a.dim && unit < 2 * kv + a.q_heads;
+    const bool value = unit >= kv && unit < 2 * kv, key = unit < kv;
+    const int head = key ? unit : value ? unit - kv : unit - 2 * kv;
+    const int past = same(cached_of(a.b, seq));
+    const bool used = past >= 0;
+    const Heads in = key ? a.k : value ? a.v : a.q, out = key ? a.k_out : a.q_out;
+    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (here && used && in.p) {
+        const _Float16* row = in.p + int64_t(seq) * in.token + int64_t(head) * in.head;
+        const f16x8 own = *reinterpret_cast<const f16x8*>(row + d);
+        if (value) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = float(own[i]);
+        } else {
+            const f16x8 other = partners<TURN>(a.r, row, d);
+            Angles cs{};
+            if (d < a.r.rot) cs = angles<TURN>(a.r, past, d);
+            turn8<TURN>(a.r, past, row, d, own, other, cs, x);
+        }
+    }
+    if (here && !value && out.p) put_row(out, seq, head, d, x);
+    // the cache
+    const int64_t number = past >> 4;
+    const int page = used && a.c.k ? same(page_of(a.c, seq, number)) : -1;
+    if (page < 0 || unit >= 2 * kv) return;
+    const int slot = past & 15, blocks = 1 << a.c.page_shift;
+    const int64_t block = (int64_t(page) * kv + head) * blocks + (number & (blocks - 1));
+    float* const scales = key ? a.c.ks : a.c.vs;
+    uint8_t* const to = (key ? a.c.k : a.c.v) + block * (int64_t(16) * a.dim);
+    const float was = slot ? scales[block] : 0.0f;
+    float amax = 0.0f;
+    int odd = 0;                                             // a NaN or an infinity
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        amax = fmaxf(amax, fabsf(x[i]));
+        odd |= !(fabsf(x[i]) < __builtin_inff());
+    }
+    for (int s = 8; s; s >>= 1) {
+        amax = fmaxf(amax, __shfl_xor(amax, s));
+        odd |= __shfl_xor(odd, s);
+    }
+    const float now = scale_of<FP8>(was, amax, odd);
+    if (lane == 0) scales[block] = now;
+    if (slot && now > was) {
+        const float ratio = was / now;
+        if (key) recode<FP8, true>(to, a.dim, slot, ratio, lane, 16);
+        else recode<FP8, false>(to, a.dim, slot, ratio, lane, 16);
+    }
+    if (!here) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = now > 0.0f ? x[i] / now : 0.0f;
+    if (key) put_codes<FP8, true>(to, a.dim, slot, d, x);
+    else put_codes<FP8, false>(to, a.dim, slot, d, x);
+}
+
+// One block: tokens [0, n) of the call's rows from row0 on, in the block's slots from `slot` on.
+struct Place {
+    int row0, n, slot;
+    int64_t pos;                          // of the block's first slot
+};
+
+template <int T>
+struct Rows {
+    f16x8 own[T], other[T];               // 8 dimensions of T tokens, and (halves) their partners
+};
+
+template <bool FP8, int T, Turn TURN>
+struct Append {
+    const Rope r;
+    const Heads k_out;
+    const Place at;
+    const int dim;
+    int lane, first, d;                   // this lane's first slot and first dimension
+    Angles cs[T];
+
+    __device__ inline bool has(int u) const { return d < dim && first + u >= at.slot && first + u < at.slot + at.n; }
+    __device__ inline int64_t row(int u) const { return at.row0 + (first + u - at.slot); }
+
+    __device__ inline Append(const Rope& rope, const Heads& keys, int size, const Place& place) : r(rope), k_out(keys), at(place), dim(size)
+    {
+        lane = threadIdx.x & 63;
+        first = (lane / (4 * T)) * T;
+        d = (lane % (4 * T)) * 8;
+#pragma unroll
+        for (int u = 0; u < T; ++u)
+            if (d < r.rot && has(u)) cs[u] = angles<TURN>(r, at.pos + first + u, d);
+    }
+
+    __device__ inline void ask(const Heads in, int head, bool turns, Rows<T>& x) const
+    {
+#pragma unroll
+        for (int u = 0; u < T; ++u) {
+            if (!has(u)) continue;
+            const _Float16* p = in.p + row(u) * in.token + int64_t(head) * in.head;
+            x.own[u] = *reinterpret_cast<const f16x8*>(p + d);
+            if (turns) x.other[u] = partners<TURN>(r, p, d);
+        }
+    }
+
+    __device__ inline void turn_it(const Heads in, int head, const Rows<T>& y, int u, float (&x)[8]) const
+    {
+        turn8<TURN>(r, at.pos + first + u, in.p + row(u) * in.token + int64_t(head) * in.head, d, y.own[u], y.other[u], cs[u], x);
+    }
+
+    // Rotated rows of one head (or zeros, where the sequence is not in use).
+    __device__ inline void head_out(const Heads in, const Heads out, int head, bool used, const Rows<T>& y) const
+    {
+#pragma unroll
+        for (int u = 0; u < T; ++u) {
+            if (!has(u)) continue;
+            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (used) turn_it(in, head, y, u, x);
+            put_row(out, row(u), head, d, x);
+        }
+    }
+
+    // One head's block into the cache; `block` is its number there, or negative: none.
+    template <bool KEY>
+    __device__ inline void block_in(const Heads in, int head, const Rows<T>& y, int64_t block, uint8_t* codes, float* scales) const
+    {
+#pragma clang fp contract(off)
+        float x[T][8];
+        float amax = 0.0f;
+        bool odd = false;                                    // a NaN or an infinity
+#pragma unroll
+        for (int u = 0; u < T; ++u) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] = 0.0f;
+            if (!has(u)) continue;
+            if constexpr (KEY) {
+                turn_it(in, head, y, u, x[u]);
+                if (k_out.p) put_row(k_out, row(u), head, d, x[u]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u][i] = float(y.own[u][i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                amax = fmaxf(amax, fabsf(x[u][i]));
+                odd |= !(fabsf(x[u][i]) < __builtin_inff());
+            }
+        }
+        if (block < 0) return;
+        const float was = at.slot ? scales[block] : 0.0f;
+        for (int s = 32; s; s >>= 1) amax = fmaxf(amax, __shfl_xor(amax, s));
+        odd = __any(odd);
+        uint8_t* const to = codes + block * (int64_t(16) * dim);
+        const float now = scale_of<FP8>(was, amax, odd);
+        if (lane == 0) scales[block] = now;
+        if (at.slot && now > was) recode<FP8, KEY>(to, dim, at.slot, was / now, lane, 64);
+        if (d >= dim) return;
+        if (!KEY && T > 1 && at.n == 16) {                   // the codes of a lane's tokens are neighbours
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint8_t* p = to + (d + i) * 16 + first;
+#pragma unroll
+                for (int u = 0; u < T; ++u) x[u][i] = now > 0.0f ? x[u][i] / now : 0.0f;
+                __builtin_amdgcn_sched_barrier(0);           // a few divisions at a time: all at once take the registers of another wave
+                if constexpr (T == 4) *reinterpret_cast<uint32_t*>(p) = four_codes<FP8>(x[0][i], x[1][i], x[2][i], x[3][i]);
+                if constexpr (T == 2) *reinterpret_cast<uint16_t*>(p) = uint16_t(two_codes<FP8>(x[0][i], x[1][i]));
+            }
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < T; ++u) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[u][i] = now > 0.0f ? x[u][i] / now : 0.0f;
+            if (has(u)) put_codes<FP8, KEY>(to, dim, first + u, d, x[u]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+};
+
+template <bool FP8, int T, Turn TURN>
+__global__ __launch_bounds__(64 * kWaves) void append_kernel(AppendArgs a, int each)
 {
     Item it{int(blockIdx.x), 0};
     if (a.b.start) it = find_item(a.b, int(blockIdx.x), 16, 2);
+    it = {same(it.seq), same(it.i)};
     if (it.seq < 0) return;
-    const Span sp = span(a.b, it.seq);
-    const int past = cached_of(a.b, it.seq);
+    Span sp = span(a.b, it.seq);
+    sp = {same(sp.first), same(sp.n)};
+    const int past = same(cached_of(a.b, it.seq));
     const bool used = past >= 0;
     const int before = used ? past : 0;
     // tokens [i0, i1) of the sequence are those of this block
-    const int64_t block = (before >> 4) + it.i;
-    const int i0 = it.i == 0 ? 0 : int(block * 16 - before);
-    const int i1 = block * 16 + 16 - before < sp.n ? int(block * 16 + 16 - before) : sp.n;
+    const int64_t number = int64_t(before >> 4) + it.i;
+    const int64_t i0 = it.i == 0 ? 0 : number * 16 - before;
+    const int64_t i1 = number * 16 + 16 - before < sp.n ? number * 16 + 16 - before : sp.n;
     if (i0 >= i1) return;
-    const int n = i1 - i0, row0 = sp.first + i0;
-    const int64_t pos = int64_t(before) + i0;
-    int unit = int(blockIdx.y) * kWaves + int(threadIdx.x >> 6);
-    const int kv = a.kv_heads;
-    if (unit < 2 * kv) {
+    const Place at{sp.first + int(i0), int(i1 - i0), int((before + i0) & 15), number * 16};
+    const int kv = a.kv_heads, units = 2 * kv + a.q_heads;
+    int unit = int(blockIdx.y) * kWaves * each + same(threadIdx.x >> 6);
+    const int stop = unit + kWaves * each < units ? unit + kWaves * each : units;
+    if (unit >= stop) return;
+    const int page = used && a.c.k ? same(page_of(a.c, it.seq, number)) : -1;
+    const int blocks = 1 << a.c.page_shift;
+    const Append<FP8, T, TURN> work(a.r, a.k_out, a.dim, at);
+    // key heads, value heads, query heads
+    for (; unit < stop; unit += kWaves) {
+        Rows<T> rows;
+        if (unit >= 2 * kv) {
+            const int head = unit - 2 * kv;
+            work.ask(a.q, head, true, rows);
+            work.head_out(a.q, a.q_out, head, used, rows);
+            continue;
+        }
         const bool key = unit < kv;
         const int head = key ? unit : unit - kv;
-        if (!used || !a.c.k) {
-            if (key && a.k_out.p) turn_head(a, a.k, a.k_out, head, row0, n, pos, used);
-            return;
+        const int64_t block = page < 0 ? -1 : (int64_t(page) * kv + head) * blocks + (number & (blocks - 1));
+        if (key) {
+            work.ask(a.k, head, true, rows);
+            if (used && a.c.k) work.template block_in<true>(a.k, head, rows, block, a.c.k, a.c.ks);
+            else if (a.k_out.p) work.head_out(a.k, a.k_out, head, used, rows);
+        } else if (block >= 0) {
+            work.ask(a.v, head, false, rows);
+            work.template block_in<false>(a.v, head, rows, block, a.c.v, a.c.vs);
         }
-        const int page = page_of(a.c, it.seq, block), blk = int(block & ((1 << a.c.page_shift) - 1));
-        if (key) put_block<FP8, true>(a, a.k, head, row0, n, int(pos & 15), pos, page, blk, a.c.k, a.c.ks);
-        else put_block<FP8, false>(a, a.v, head, row0, n, int(pos & 15), pos, page, blk, a.c.v, a.c.vs);
-        return;
     }
-    unit -= 2 * kv;
-    if (unit < a.q_heads && a.q_out.p) turn_head(a, a.q, a.q_out, unit, row0, n, pos, used);
+}
+
+template <bool FP8, int T, Turn TURN>
+hipError_t launch(const AppendArgs& a, hipStream_t s)
+{
+    const int units = 2 * a.kv_heads + a.q_heads;
+    if (!a.b.start) {
+        step_kernel<FP8, TURN><<<dim3(unsigned(a.b.seqs), unsigned((units + 4 * kWaves - 1) / (4 * kWaves))), 64 * kWaves, 0, s>>>(a);
+        return hipGetLastError();
+    }
+    const int64_t items = a.b.tokens / 16 + 2 * int64_t(a.b.seqs);
+    // heads for each wave: as many as leave the chip 8 waves on each SIMD
+    int64_t each = items * units / (8 * 1024);
+    if (each < 1) each = 1;
+    if (each > (units + kWaves - 1) / kWaves) each = (units + kWaves - 1) / kWaves;
+    append_kernel<FP8, T, TURN><<<dim3(unsigned(items), unsigned((units + kWaves * each - 1) / (kWaves * each))), 64 * kWaves, 0, s>>>(a, int(each));
+    return hipGetLastError();
+}
+
+template <bool FP8, Turn TURN>
+hipError_t launch_dim(const AppendArgs& a, hipStream_t s)
+{
+    return a.dim <= 32 ? launch<FP8, 1, TURN>(a, s) : a.dim <= 64 ? launch<FP8, 2, TURN>(a, s) : launch<FP8, 4, TURN>(a, s);
+}
+
+template <bool FP8>
+hipError_t launch_turn(const AppendArgs& a, hipStream_t s)
+{
+    if (!a.r.table) return launch_dim<FP8, kNone>(a, s);
+    if (!a.r.wide) return launch_dim<FP8, kAny>(a, s);
+    return a.r.pairs ? launch_dim<FP8, kPairs>(a, s) : launch_dim<FP8, kHalves>(a, s);
 }
 
 }  // namespace
 
-hipError_t launch_append(const AppendArgs& a, hipStream_t s)
-{
-    const int64_t items = a.b.start ? a.b.tokens / 16 + 2 * int64_t(a.b.seqs) : a.b.seqs;
-    const int units = 2 * a.kv_heads + a.q_heads;
-    const dim3 grid(unsigned(items), unsigned((units + kWaves - 1) / kWaves));
-    if (a.c.fp8) append_kernel<true><<<grid, 64 * kWaves, 0, s>>>(a);
-    else append_kernel<false><<<grid, 64 * kWaves, 0, s>>>(a);
-    return hipGetLastError();
-}
+hipError_t launch_append(const AppendArgs& a, hipStream_t s) { return a.c.fp8 ? launch_turn<true>(a, s) : launch_turn<false>(a, s); }
 
 }  // namespace tl
