@@ -15,21 +15,36 @@ constexpr int kWaves = 4;
 template <bool FP8>
 __device__ inline float top() { return FP8 ? 448.0f : 127.0f; }
 
-// The codes of a and b, at most a rounding beyond the top, in the low and the second byte; a NaN gives anything.
-template <bool FP8>
-__device__ inline uint32_t two_codes(float a, float b)
-{
-    a = fminf(fmaxf(a, -top<FP8>()), top<FP8>());
-    b = fminf(fmaxf(b, -top<FP8>()), top<FP8>());
-    if constexpr (FP8) return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false)) & 0xffffu;
-    else return (uint32_t(int(rintf(a))) & 255u) | (uint32_t(int(rintf(b))) & 255u) << 8;
-}
-
+// The codes nearest to four numbers (ties to the even one) that are at most a rounding beyond the top, which every block's scale sees to.
 template <bool FP8>
 __device__ inline uint32_t four_codes(float a, float b, float c, float d)
 {
-    return two_codes<FP8>(a, b) | two_codes<FP8>(c, d) << 16;
+    if constexpr (FP8) {
+        return uint32_t(__builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true));
+    } else {
+        // beside 1.5 * 2^23 a whole number's two's complement stands in the last byte
+        const float m = 12582912.0f;
+        const uint32_t ab = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, b + m), __builtin_bit_cast(uint32_t, a + m), 0x0c0c0400u);
+        const uint32_t cd = __builtin_amdgcn_perm(__builtin_bit_cast(uint32_t, d + m), __builtin_bit_cast(uint32_t, c + m), 0x0c0c0400u);
+        return ab | cd << 16;
+    }
 }
+
+template <bool FP8>
+__device__ inline uint32_t two_codes(float a, float b) { return four_codes<FP8>(a, b, 0.0f, 0.0f) & 0xffffu; }
+
+// Quotients by one number b, rounded as a division rounds them: with the rounded reciprocal, the remainder of the first guess sets it right (Markstein, IBM
+// Journal of Research and Development 34, 1990).  0 for all where b is 0 or NaN.  Magnitudes here stay far from both ends of the range.
+struct Divide {
+    float b, inv;
+    bool any;
+    __device__ inline explicit Divide(float x) : b(x), inv(1.0f / x), any(x > 0.0f) {}
+    __device__ inline float operator()(float a) const
+    {
+        const float q = a * inv;
+        return any ? __builtin_copysignf(__builtin_fmaf(__builtin_fmaf(-q, b, a), inv, q), a) : 0.0f;      // -0 stays -0
+    }
+};
 
 template <bool FP8, int I>
 __device__ inline float value_of(uint32_t codes)
@@ -216,18 +231,17 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(AppendArgs a)
     float* const scales = key ? a.c.ks : a.c.vs;
     uint8_t* const to = (key ? a.c.k : a.c.v) + block * (int64_t(16) * a.dim);
     const float was = slot ? scales[block] : 0.0f;
-    float amax = 0.0f;
-    int odd = 0;                                             // a NaN or an infinity
+    float amax = 0.0f, zero = 0.0f;                          // a NaN or an infinity leaves no 0
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         amax = fmaxf(amax, fabsf(x[i]));
-        odd |= !(fabsf(x[i]) < __builtin_inff());
+        zero = __builtin_fmaf(x[i], 0.0f, zero);
     }
     for (int s = 8; s; s >>= 1) {
         amax = fmaxf(amax, __shfl_xor(amax, s));
-        odd |= __shfl_xor(odd, s);
+        zero += __shfl_xor(zero, s);
     }
-    const float now = scale_of<FP8>(was, amax, odd);
+    const float now = scale_of<FP8>(was, amax, !(zero == 0.0f));
     if (lane == 0) scales[block] = now;
     if (slot && now > was) {
         const float ratio = was / now;
@@ -235,8 +249,9 @@ __global__ __launch_bounds__(64 * kWaves) void step_kernel(AppendArgs a)
         else recode<FP8, false>(to, a.dim, slot, ratio, lane, 16);
     }
     if (!here) return;
+    const Divide over(now);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = now > 0.0f ? x[i] / now : 0.0f;
+    for (int i = 0; i < 8; ++i) x[i] = over(x[i]);
     if (key) put_codes<FP8, true>(to, a.dim, slot, d, x);
     else put_codes<FP8, false>(to, a.dim, slot, d, x);
 }
@@ -308,8 +323,7 @@ struct Append {
     {
 #pragma clang fp contract(off)
         float x[T][8];
-        float amax = 0.0f;
-        bool odd = false;                                    // a NaN or an infinity
+        float amax = 0.0f, zero = 0.0f;                      // a NaN or an infinity leaves no 0
 #pragma unroll
         for (int u = 0; u < T; ++u) {
 #pragma unroll
@@ -325,25 +339,25 @@ struct Append {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 amax = fmaxf(amax, fabsf(x[u][i]));
-                odd |= !(fabsf(x[u][i]) < __builtin_inff());
+                zero = __builtin_fmaf(x[u][i], 0.0f, zero);
             }
         }
         if (block < 0) return;
         const float was = at.slot ? scales[block] : 0.0f;
         for (int s = 32; s; s >>= 1) amax = fmaxf(amax, __shfl_xor(amax, s));
-        odd = __any(odd);
+        const bool odd = __any(!(zero == 0.0f));
         uint8_t* const to = codes + block * (int64_t(16) * dim);
         const float now = scale_of<FP8>(was, amax, odd);
         if (lane == 0) scales[block] = now;
         if (at.slot && now > was) recode<FP8, KEY>(to, dim, at.slot, was / now, lane, 64);
         if (d >= dim) return;
+        const Divide over(now);
         if (!KEY && T > 1 && at.n == 16) {                   // the codes of a lane's tokens are neighbours
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 uint8_t* p = to + (d + i) * 16 + first;
 #pragma unroll
-                for (int u = 0; u < T; ++u) x[u][i] = now > 0.0f ? x[u][i] / now : 0.0f;
-                __builtin_amdgcn_sched_barrier(0);           // a few divisions at a time: all at once take the registers of another wave
+                for (int u = 0; u < T; ++u) x[u][i] = over(x[u][i]);
                 if constexpr (T == 4) *reinterpret_cast<uint32_t*>(p) = four_codes<FP8>(x[0][i], x[1][i], x[2][i], x[3][i]);
                 if constexpr (T == 2) *reinterpret_cast<uint16_t*>(p) = uint16_t(two_codes<FP8>(x[0][i], x[1][i]));
             }
@@ -352,9 +366,8 @@ struct Append {
 #pragma unroll
         for (int u = 0; u < T; ++u) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = now > 0.0f ? x[u][i] / now : 0.0f;
+            for (int i = 0; i < 8; ++i) x[u][i] = over(x[u][i]);
             if (has(u)) put_codes<FP8, KEY>(to, dim, first + u, d, x[u]);
-            __builtin_amdgcn_sched_barrier(0);
         }
     }
 };
