@@ -144,6 +144,7 @@ __device__ inline void recode(uint8_t* to, int dim, int slots, float ratio, int 
 {
     const int chunks = dim >> 4;
     if constexpr (KEY) {
+#pragma clang loop unroll(disable)
         for (; i < slots * chunks; i += step) {
             const int t = i / chunks, c = i - t * chunks;
             uint32_t* w = reinterpret_cast<uint32_t*>(to + ((t >> 2) * chunks + c) * 64 + (t & 3) * 16);
@@ -152,10 +153,13 @@ __device__ inline void recode(uint8_t* to, int dim, int slots, float ratio, int 
         }
     } else {
         // whole words of 4 tokens, then the tokens that share a word with new ones
+#pragma clang loop unroll(disable)
         for (; i < dim; i += step) {
             uint32_t* w = reinterpret_cast<uint32_t*>(to + i * 16);
             int t = 0;
+#pragma clang loop unroll(disable)
             for (; t + 4 <= slots; t += 4) w[t >> 2] = recode4<FP8>(w[t >> 2], ratio);
+#pragma clang loop unroll(disable)
             for (; t < slots; ++t) to[i * 16 + t] = uint8_t(two_codes<FP8>(value_of<FP8, 0>(to[i * 16 + t]) * ratio, 0.0f));
         }
     }
@@ -262,112 +266,200 @@ struct Place {
     int64_t pos;                          // of the block's first slot
 };
 
+// What the two ways through a block share: a lane's first slot and dimension, and where a head's rows are.
 template <int T>
-struct Rows {
-    f16x8 own[T], other[T];               // 8 dimensions of T tokens, and (halves) their partners
-};
-
-template <bool FP8, int T, Turn TURN>
-struct Append {
+struct Lane {
     const Rope r;
-    const Heads k_out;
     const Place at;
     const int dim;
-    int lane, first, d;                   // this lane's first slot and first dimension
-    Angles cs[T];
+    int lane, first, d;
 
-    __device__ inline bool has(int u) const { return d < dim && first + u >= at.slot && first + u < at.slot + at.n; }
-    __device__ inline int64_t row(int u) const { return at.row0 + (first + u - at.slot); }
-
-    __device__ inline Append(const Rope& rope, const Heads& keys, int size, const Place& place) : r(rope), k_out(keys), at(place), dim(size)
+    __device__ inline Lane(const AppendArgs& a, const Place& place) : r(a.r), at(place), dim(a.dim)
     {
         lane = threadIdx.x & 63;
         first = (lane / (4 * T)) * T;
         d = (lane % (4 * T)) * 8;
-#pragma unroll
-        for (int u = 0; u < T; ++u)
-            if (d < r.rot && has(u)) cs[u] = angles<TURN>(r, at.pos + first + u, d);
     }
+    // a row's 8 dimensions: the head's place in the block's first row is the wave's, what a lane adds to it (15 rows at most) fits 32 bits
+    __device__ inline _Float16* place(const Heads h, int head, int u) const
+    {
+        char* base = reinterpret_cast<char*>(h.p + int64_t(at.row0) * h.token + int64_t(head) * h.head);
+        return reinterpret_cast<_Float16*>(base + (uint32_t(first + u - at.slot) * (uint32_t(h.token) * 2u) + uint32_t(d) * 2u));
+    }
+    __device__ inline void put(const Heads h, int head, int u, const float (&x)[8]) const
+    {
+        f16x8 o;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = _Float16(x[i]);
+        *reinterpret_cast<f16x8*>(place(h, head, u)) = o;
+    }
+    // The block's new scale, written down; what it holds already is coded anew.
+    template <bool FP8, bool KEY>
+    __device__ inline float rescale(float amax, float zero, int64_t block, uint8_t* to, float* scales) const
+    {
+        const float was = at.slot ? scales[block] : 0.0f;
+        for (int s = 32; s; s >>= 1) amax = fmaxf(amax, __shfl_xor(amax, s));
+        const float now = scale_of<FP8>(was, amax, __any(!(zero == 0.0f)));
+        if (lane == 0) scales[block] = now;
+        if (at.slot && now > was) recode<FP8, KEY>(to, dim, at.slot, was / now, lane, 64);
+        return now;
+    }
+};
 
-    __device__ inline void ask(const Heads in, int head, bool turns, Rows<T>& x) const
+// A block that the call fills, of heads of 32 T dimensions: every lane has T tokens, and all of them stay in registers.
+template <bool FP8, int T, Turn TURN>
+struct Whole : Lane<T> {
+    const Heads k_out;
+    Angles cs[T];
+    using Lane<T>::r;
+    using Lane<T>::at;
+    using Lane<T>::d;
+    using Lane<T>::dim;
+    using Lane<T>::first;
+
+    __device__ inline Whole(const AppendArgs& a, const Place& place) : Lane<T>(a, place), k_out(a.k_out)
     {
 #pragma unroll
         for (int u = 0; u < T; ++u) {
-            if (!has(u)) continue;
-            const _Float16* p = in.p + row(u) * in.token + int64_t(head) * in.head;
-            x.own[u] = *reinterpret_cast<const f16x8*>(p + d);
-            if (turns) x.other[u] = partners<TURN>(r, p, d);
+            cs[u] = Angles{};
+            if (d < r.rot) cs[u] = angles<TURN>(r, at.pos + first + u, d);
         }
     }
 
-    __device__ inline void turn_it(const Heads in, int head, const Rows<T>& y, int u, float (&x)[8]) const
+    template <bool TURNED>
+    __device__ inline void rows(const Heads in, int head, float (&x)[T][8]) const
     {
-        turn8<TURN>(r, at.pos + first + u, in.p + row(u) * in.token + int64_t(head) * in.head, d, y.own[u], y.other[u], cs[u], x);
-    }
-
-    // Rotated rows of one head (or zeros, where the sequence is not in use).
-    __device__ inline void head_out(const Heads in, const Heads out, int head, bool used, const Rows<T>& y) const
-    {
+        f16x8 own[T], other[T];
 #pragma unroll
         for (int u = 0; u < T; ++u) {
-            if (!has(u)) continue;
-            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (used) turn_it(in, head, y, u, x);
-            put_row(out, row(u), head, d, x);
+            const _Float16* p = this->place(in, head, u);
+            own[u] = *reinterpret_cast<const f16x8*>(p);
+            if constexpr (TURNED) other[u] = partners<TURN>(r, p - d, d);
         }
-    }
-
-    // One head's block into the cache; `block` is its number there, or negative: none.
-    template <bool KEY>
-    __device__ inline void block_in(const Heads in, int head, const Rows<T>& y, int64_t block, uint8_t* codes, float* scales) const
-    {
-#pragma clang fp contract(off)
-        float x[T][8];
-        float amax = 0.0f, zero = 0.0f;                      // a NaN or an infinity leaves no 0
 #pragma unroll
         for (int u = 0; u < T; ++u) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = 0.0f;
-            if (!has(u)) continue;
-            if constexpr (KEY) {
-                turn_it(in, head, y, u, x[u]);
-                if (k_out.p) put_row(k_out, row(u), head, d, x[u]);
+            if constexpr (TURNED) {
+                turn8<TURN>(r, at.pos + first + u, this->place(in, head, u) - d, d, own[u], other[u], cs[u], x[u]);
             } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) x[u][i] = float(y.own[u][i]);
+                for (int i = 0; i < 8; ++i) x[u][i] = float(own[u][i]);
             }
+        }
+    }
+
+    __device__ inline void turn(const Heads in, const Heads out, int head) const
+    {
+        float x[T][8];
+        rows<true>(in, head, x);
+#pragma unroll
+        for (int u = 0; u < T; ++u) this->put(out, head, u, x[u]);
+    }
+
+    template <bool KEY>
+    __device__ inline void keep(const Heads in, int head, int64_t block, uint8_t* codes, float* scales) const
+    {
+        float x[T][8];
+        rows<KEY>(in, head, x);
+        if (KEY && k_out.p) {
+#pragma unroll
+            for (int u = 0; u < T; ++u) this->put(k_out, head, u, x[u]);
+        }
+        if (block < 0) return;
+        float amax = 0.0f, zero = 0.0f;                      // a NaN or an infinity leaves no 0
+#pragma unroll
+        for (int u = 0; u < T; ++u)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 amax = fmaxf(amax, fabsf(x[u][i]));
                 zero = __builtin_fmaf(x[u][i], 0.0f, zero);
             }
-        }
-        if (block < 0) return;
-        const float was = at.slot ? scales[block] : 0.0f;
-        for (int s = 32; s; s >>= 1) amax = fmaxf(amax, __shfl_xor(amax, s));
-        const bool odd = __any(!(zero == 0.0f));
         uint8_t* const to = codes + block * (int64_t(16) * dim);
-        const float now = scale_of<FP8>(was, amax, odd);
-        if (lane == 0) scales[block] = now;
-        if (at.slot && now > was) recode<FP8, KEY>(to, dim, at.slot, was / now, lane, 64);
-        if (d >= dim) return;
-        const Divide over(now);
-        if (!KEY && T > 1 && at.n == 16) {                   // the codes of a lane's tokens are neighbours
+        const Divide over(this->template rescale<FP8, KEY>(amax, zero, block, to, scales));
+        if constexpr (!KEY && T > 1) {                       // the codes of a lane's tokens are neighbours
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 uint8_t* p = to + (d + i) * 16 + first;
-#pragma unroll
-                for (int u = 0; u < T; ++u) x[u][i] = over(x[u][i]);
-                if constexpr (T == 4) *reinterpret_cast<uint32_t*>(p) = four_codes<FP8>(x[0][i], x[1][i], x[2][i], x[3][i]);
-                if constexpr (T == 2) *reinterpret_cast<uint16_t*>(p) = uint16_t(two_codes<FP8>(x[0][i], x[1][i]));
+                if constexpr (T == 4) *reinterpret_cast<uint32_t*>(p) = four_codes<FP8>(over(x[0][i]), over(x[1][i]), over(x[2][i]), over(x[3][i]));
+                if constexpr (T == 2) *reinterpret_cast<uint16_t*>(p) = uint16_t(two_codes<FP8>(over(x[0][i]), over(x[1][i])));
             }
-            return;
+        } else {
+#pragma unroll
+            for (int u = 0; u < T; ++u) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[u][i] = over(x[u][i]);
+                put_codes<FP8, KEY>(to, dim, first + u, d, x[u]);
+            }
         }
+    }
+};
+
+// Any other block: a token at a time, and once more when the scale is known.
+template <bool FP8, int T, Turn TURN>
+struct Some : Lane<T> {
+    const Heads k_out;
+    using Lane<T>::r;
+    using Lane<T>::at;
+    using Lane<T>::d;
+    using Lane<T>::dim;
+    using Lane<T>::first;
+
+    __device__ inline Some(const AppendArgs& a, const Place& place) : Lane<T>(a, place), k_out(a.k_out) {}
+    __device__ inline bool has(int u) const { return d < dim && first + u >= at.slot && first + u < at.slot + at.n; }
+
+    template <bool TURNED>
+    __device__ inline void row(const Heads in, int head, int u, float (&x)[8]) const
+    {
+        const _Float16* p = this->place(in, head, u);
+        const f16x8 own = *reinterpret_cast<const f16x8*>(p);
+        if constexpr (TURNED) {
+            Angles cs{};
+            if (d < r.rot) cs = angles<TURN>(r, at.pos + first + u, d);
+            turn8<TURN>(r, at.pos + first + u, p - d, d, own, partners<TURN>(r, p - d, d), cs, x);
+        } else {
 #pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = float(own[i]);
+        }
+    }
+
+    // rotated rows, or zeros where the sequence is not in use
+    __device__ inline void turn(const Heads in, const Heads out, int head, bool used) const
+    {
+#pragma clang loop unroll(disable)
         for (int u = 0; u < T; ++u) {
+            if (!has(u)) continue;
+            float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+            if (used) row<true>(in, head, u, x);
+            this->put(out, head, u, x);
+        }
+    }
+
+    template <bool KEY>
+    __device__ inline void keep(const Heads in, int head, int64_t block, uint8_t* codes, float* scales) const
+    {
+        float amax = 0.0f, zero = 0.0f;                      // a NaN or an infinity leaves no 0
+#pragma clang loop unroll(disable)
+        for (int u = 0; u < T; ++u) {
+            if (!has(u)) continue;
+            float x[8];
+            row<KEY>(in, head, u, x);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[u][i] = over(x[u][i]);
-            if (has(u)) put_codes<FP8, KEY>(to, dim, first + u, d, x[u]);
+            for (int i = 0; i < 8; ++i) {
+                amax = fmaxf(amax, fabsf(x[i]));
+                zero = __builtin_fmaf(x[i], 0.0f, zero);
+            }
+        }
+        uint8_t* const to = codes + block * (int64_t(16) * dim);
+        const Divide over(block < 0 ? 0.0f : this->template rescale<FP8, KEY>(amax, zero, block, to, scales));
+#pragma clang loop unroll(disable)
+        for (int u = 0; u < T; ++u) {
+            if (!has(u)) continue;
+            float x[8];
+            row<KEY>(in, head, u, x);
+            if (KEY && k_out.p) this->put(k_out, head, u, x);        // which may be the row that was read
+            if (block < 0) continue;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = over(x[i]);
+            put_codes<FP8, KEY>(to, dim, first + u, d, x);
         }
     }
 };
@@ -390,32 +482,28 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(AppendArgs a, int e
     const int64_t i1 = number * 16 + 16 - before < sp.n ? number * 16 + 16 - before : sp.n;
     if (i0 >= i1) return;
     const Place at{sp.first + int(i0), int(i1 - i0), int((before + i0) & 15), number * 16};
-    const int kv = a.kv_heads, units = 2 * kv + a.q_heads;
+    const int units = 2 * a.kv_heads + a.q_heads;
     int unit = int(blockIdx.y) * kWaves * each + same(threadIdx.x >> 6);
     const int stop = unit + kWaves * each < units ? unit + kWaves * each : units;
     if (unit >= stop) return;
+    // a wave's heads: keys, values, queries
+    const int kv = a.kv_heads, blocks = 1 << a.c.page_shift;
     const int page = used && a.c.k ? same(page_of(a.c, it.seq, number)) : -1;
-    const int blocks = 1 << a.c.page_shift;
-    const Append<FP8, T, TURN> work(a.r, a.k_out, a.dim, at);
-    // key heads, value heads, query heads
-    for (; unit < stop; unit += kWaves) {
-        Rows<T> rows;
-        if (unit >= 2 * kv) {
-            const int head = unit - 2 * kv;
-            work.ask(a.q, head, true, rows);
-            work.head_out(a.q, a.q_out, head, used, rows);
-            continue;
+    auto place = [&](int head) { return page < 0 ? int64_t(-1) : (int64_t(page) * kv + head) * blocks + (number & (blocks - 1)); };
+    if (at.n == 16 && a.dim == 32 * T && used) {
+        const Whole<FP8, T, TURN> work(a, at);
+        for (; unit < stop; unit += kWaves) {
+            if (unit >= 2 * kv) work.turn(a.q, a.q_out, unit - 2 * kv);
+            else if (unit < kv) work.template keep<true>(a.k, unit, place(unit), a.c.k, a.c.ks);
+            else if (page >= 0) work.template keep<false>(a.v, unit - kv, place(unit - kv), a.c.v, a.c.vs);
         }
-        const bool key = unit < kv;
-        const int head = key ? unit : unit - kv;
-        const int64_t block = page < 0 ? -1 : (int64_t(page) * kv + head) * blocks + (number & (blocks - 1));
-        if (key) {
-            work.ask(a.k, head, true, rows);
-            if (used && a.c.k) work.template block_in<true>(a.k, head, rows, block, a.c.k, a.c.ks);
-            else if (a.k_out.p) work.head_out(a.k, a.k_out, head, used, rows);
-        } else if (block >= 0) {
-            work.ask(a.v, head, false, rows);
-            work.template block_in<false>(a.v, head, rows, block, a.c.v, a.c.vs);
+    } else {
+        const Some<FP8, T, TURN> work(a, at);
+        for (; unit < stop; unit += kWaves) {
+            if (unit >= 2 * kv) work.turn(a.q, a.q_out, unit - 2 * kv, used);
+            else if (unit >= kv) { if (page >= 0) work.template keep<false>(a.v, unit - kv, place(unit - kv), a.c.v, a.c.vs); }
+            else if (used) work.template keep<true>(a.k, unit, place(unit), a.c.k, a.c.ks);
+            else if (a.k_out.p) work.turn(a.k, a.k_out, unit, false);
         }
     }
 }
