@@ -280,18 +280,18 @@ struct Lane {
         first = (lane / (4 * T)) * T;
         d = (lane % (4 * T)) * 8;
     }
-    // a row's 8 dimensions: the head's place in the block's first row is the wave's, what a lane adds to it (15 rows at most) fits 32 bits
-    __device__ inline _Float16* place(const Heads h, int head, int u) const
+    // 8 dimensions of the token in a slot: the head's place in the block's first row is the wave's, what a lane adds to it (15 rows at most) fits 32 bits
+    __device__ inline _Float16* place(const Heads h, int head, int slot) const
     {
         char* base = reinterpret_cast<char*>(h.p + int64_t(at.row0) * h.token + int64_t(head) * h.head);
-        return reinterpret_cast<_Float16*>(base + (uint32_t(first + u - at.slot) * (uint32_t(h.token) * 2u) + uint32_t(d) * 2u));
+        return reinterpret_cast<_Float16*>(base + (uint32_t(slot - at.slot) * (uint32_t(h.token) * 2u) + uint32_t(d) * 2u));
     }
-    __device__ inline void put(const Heads h, int head, int u, const float (&x)[8]) const
+    __device__ inline void put(const Heads h, int head, int slot, const float (&x)[8]) const
     {
         f16x8 o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = _Float16(x[i]);
-        *reinterpret_cast<f16x8*>(place(h, head, u)) = o;
+        *reinterpret_cast<f16x8*>(place(h, head, slot)) = o;
     }
     // The block's new scale, written down; what it holds already is coded anew.
     template <bool FP8, bool KEY>
@@ -306,7 +306,8 @@ struct Lane {
     }
 };
 
-// A block that the call fills, of heads of 32 T dimensions: every lane has T tokens, and all of them stay in registers.
+// A block that the call fills, of heads of 32 T dimensions: every lane has T tokens, and all of them stay in registers.  Of values, T
+// neighbours, whose codes are neighbours in memory; of keys and queries those of 16 / T rows that the wave's lanes then read and write side by side.
 template <bool FP8, int T, Turn TURN>
 struct Whole : Lane<T> {
     const Heads k_out;
@@ -317,12 +318,15 @@ struct Whole : Lane<T> {
     using Lane<T>::dim;
     using Lane<T>::first;
 
+    template <bool VALUE>
+    __device__ inline int slot(int u) const { return VALUE ? first + u : u * (16 / T) + first / T; }
+
     __device__ inline Whole(const AppendArgs& a, const Place& place) : Lane<T>(a, place), k_out(a.k_out)
     {
 #pragma unroll
         for (int u = 0; u < T; ++u) {
             cs[u] = Angles{};
-            if (d < r.rot) cs[u] = angles<TURN>(r, at.pos + first + u, d);
+            if (d < r.rot) cs[u] = angles<TURN>(r, at.pos + slot<false>(u), d);
         }
     }
 
@@ -332,14 +336,14 @@ struct Whole : Lane<T> {
         f16x8 own[T], other[T];
 #pragma unroll
         for (int u = 0; u < T; ++u) {
-            const _Float16* p = this->place(in, head, u);
+            const _Float16* p = this->place(in, head, slot<!TURNED>(u));
             own[u] = *reinterpret_cast<const f16x8*>(p);
             if constexpr (TURNED) other[u] = partners<TURN>(r, p - d, d);
         }
 #pragma unroll
         for (int u = 0; u < T; ++u) {
             if constexpr (TURNED) {
-                turn8<TURN>(r, at.pos + first + u, this->place(in, head, u) - d, d, own[u], other[u], cs[u], x[u]);
+                turn8<TURN>(r, at.pos + slot<false>(u), this->place(in, head, slot<false>(u)) - d, d, own[u], other[u], cs[u], x[u]);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[u][i] = float(own[u][i]);
@@ -352,7 +356,7 @@ struct Whole : Lane<T> {
         float x[T][8];
         rows<true>(in, head, x);
 #pragma unroll
-        for (int u = 0; u < T; ++u) this->put(out, head, u, x[u]);
+        for (int u = 0; u < T; ++u) this->put(out, head, slot<false>(u), x[u]);
     }
 
     template <bool KEY>
@@ -362,7 +366,7 @@ struct Whole : Lane<T> {
         rows<KEY>(in, head, x);
         if (KEY && k_out.p) {
 #pragma unroll
-            for (int u = 0; u < T; ++u) this->put(k_out, head, u, x[u]);
+            for (int u = 0; u < T; ++u) this->put(k_out, head, slot<false>(u), x[u]);
         }
         if (block < 0) return;
         float amax = 0.0f, zero = 0.0f;                      // a NaN or an infinity leaves no 0
@@ -387,7 +391,7 @@ struct Whole : Lane<T> {
             for (int u = 0; u < T; ++u) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[u][i] = over(x[u][i]);
-                put_codes<FP8, KEY>(to, dim, first + u, d, x[u]);
+                put_codes<FP8, KEY>(to, dim, slot<!KEY>(u), d, x[u]);
             }
         }
     }
@@ -409,7 +413,7 @@ struct Some : Lane<T> {
     template <bool TURNED>
     __device__ inline void row(const Heads in, int head, int u, float (&x)[8]) const
     {
-        const _Float16* p = this->place(in, head, u);
+        const _Float16* p = this->place(in, head, first + u);
         const f16x8 own = *reinterpret_cast<const f16x8*>(p);
         if constexpr (TURNED) {
             Angles cs{};
@@ -429,7 +433,7 @@ struct Some : Lane<T> {
             if (!has(u)) continue;
             float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             if (used) row<true>(in, head, u, x);
-            this->put(out, head, u, x);
+            this->put(out, head, first + u, x);
         }
     }
 
@@ -455,7 +459,7 @@ struct Some : Lane<T> {
             if (!has(u)) continue;
             float x[8];
             row<KEY>(in, head, u, x);
-            if (KEY && k_out.p) this->put(k_out, head, u, x);        // which may be the row that was read
+            if (KEY && k_out.p) this->put(k_out, head, first + u, x);        // which may be the row that was read
             if (block < 0) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = over(x[i]);
@@ -517,8 +521,8 @@ hipError_t launch(const AppendArgs& a, hipStream_t s)
         return hipGetLastError();
     }
     const int64_t items = a.b.tokens / 16 + 2 * int64_t(a.b.seqs);
-    // heads for each wave: as many as leave the chip 8 waves on each SIMD
-    int64_t each = items * units / (8 * 1024);
+    // heads for each wave, as many as leave the chip 16 waves for each SIMD (8: 86 us for 81, 32: 91, at 6264 tokens of 96 heads)
+    int64_t each = items * units / (16 * 1024);
     if (each < 1) each = 1;
     if (each > (units + kWaves - 1) / kWaves) each = (units + kWaves - 1) / kWaves;
     append_kernel<FP8, T, TURN><<<dim3(unsigned(items), unsigned((units + kWaves * each - 1) / (kWaves * each))), 64 * kWaves, 0, s>>>(a, int(each));
