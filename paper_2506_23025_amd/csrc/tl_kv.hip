@@ -306,7 +306,7 @@ struct Lane {
     }
 };
 
-// A block that the call fills, of heads of 32 T dimensions: every lane has T tokens, and all of them stay in registers.  Of values, T
+// A block that the call fills: every lane has T tokens, and all of them stay in registers.  Of values, T
 // neighbours, whose codes are neighbours in memory; of keys and queries those of 16 / T rows that the wave's lanes then read and write side by side.
 template <bool FP8, int T, Turn TURN>
 struct Whole : Lane<T> {
@@ -323,6 +323,7 @@ struct Whole : Lane<T> {
 
     __device__ inline Whole(const AppendArgs& a, const Place& place) : Lane<T>(a, place), k_out(a.k_out)
     {
+        if (d >= dim) d = dim - 8;                           // lanes beyond the head do what its last one does, once more
 #pragma unroll
         for (int u = 0; u < T; ++u) {
             cs[u] = Angles{};
@@ -494,7 +495,7 @@ __global__ __launch_bounds__(64 * kWaves) void append_kernel(AppendArgs a, int e
     const int kv = a.kv_heads, blocks = 1 << a.c.page_shift;
     const int page = used && a.c.k ? same(page_of(a.c, it.seq, number)) : -1;
     auto place = [&](int head) { return page < 0 ? int64_t(-1) : (int64_t(page) * kv + head) * blocks + (number & (blocks - 1)); };
-    if (at.n == 16 && a.dim == 32 * T && used) {
+    if (at.n == 16 && used) {
         const Whole<FP8, T, TURN> work(a, at);
         for (; unit < stop; unit += kWaves) {
             if (unit >= 2 * kv) work.turn(a.q, a.q_out, unit - 2 * kv);
