@@ -15,6 +15,7 @@
 // read on the device, so one captured launch serves every step.  Pieces of row tiles that several waves share meet in a second kernel.
 #include "tl_attn.hpp"
 
+#include <cmath>
 #include <type_traits>
 
 namespace tl {
@@ -94,6 +95,7 @@ __device__ inline u32x4 fetch(const uint8_t* p)
     else return *reinterpret_cast<const u32x4*>(p);
 }
 
+__device__ inline float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
 __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
 __device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -425,9 +427,21 @@ struct Walk {
             l[n] += __shfl_xor(l[n], 32);
         }
     }
-};
 
-__device__ inline float inverse(float l) { return l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l; }
+    // This lane's quarter of its row in block n, where the wave has seen all of it.
+    __device__ inline void write_row(const CachedArgs& a, _Float16* out, int n, int g) const
+    {
+        const float x = inverse(l[n]) * power(R[n] - finite(m[n]));
+#pragma unroll
+        for (int d = 0; d < CH; ++d) {
+            if (!EXACT && d * 16 >= a.c.dim) continue;
+            f16x4 v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = _Float16(o[n][d][j] * x);
+            *reinterpret_cast<f16x4*>(out + d * 16 + g * 4) = v;
+        }
+    }
+};
 
 __device__ inline _Float16* out_row(const CachedArgs& a, const Shape& p, int row, int head, int sub, int h)
 {
@@ -481,6 +495,30 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void short_k
 #pragma unroll
         for (int j = 0; j < 4; ++j) y[j] = _Float16(sum[j]);
         *reinterpret_cast<f16x4*>(out_row(a, p, sp.first + w.first + t, head, sub, h) + d) = y;
+    }
+}
+
+// A wave for each row tile of each key head.
+template <bool FP8, int CH, bool EXACT, int NR>
+__global__ __launch_bounds__(64 * kWaves, CH * NR > 8 ? 1 : 2) void wave_kernel(CachedArgs a, Shape p)
+{
+    const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
+    const int x = int(blockIdx.x) * kWaves + same(threadIdx.x >> 6);
+    Item it{x < a.b.seqs ? x : -1, 0};
+    if (a.b.start) it = find_item(a.b, x, p.per, 1);
+    it = {same(it.seq), same(it.i)};
+    if (it.seq < 0) return;
+    Span sp = span(a.b, it.seq);
+    sp = {same(sp.first), same(sp.n)};
+    if (it.i * p.per >= sp.n) return;
+    const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
+    Walk<FP8, CH, EXACT, NR, 1> w;
+    w.start(a, p, sp, same(cached_of(a.b, it.seq)), it.i, head, sub);
+    w.walk(a, it.seq, head, 0, int((w.most + 63) >> 6), 1);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        const int r = n * 16 + m16, t = r / p.heads, h = r - t * p.heads;
+        if (r < w.rows && h < w.heads) w.write_row(a, out_row(a, p, sp.first + w.first + t, head, sub, h), n, g);
     }
 }
 
@@ -542,16 +580,7 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
             const int r = n * 16 + m16, t = r / p.heads, h = r - t * p.heads;
             if (r >= w.rows || h >= w.heads) continue;
             if (whole) {
-                const float x = inverse(w.l[n]) * power(w.R[n] - finite(w.m[n]));
-                _Float16* out = out_row(a, p, sp.first + w.first + t, head, sub, h);
-#pragma unroll
-                for (int d = 0; d < CH; ++d) {
-                    if (d * 16 >= a.c.dim) continue;
-                    f16x4 v;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] = _Float16(w.o[n][d][j] * x);
-                    *reinterpret_cast<f16x4*>(out + d * 16 + g * 4) = v;
-                }
+                w.write_row(a, out_row(a, p, sp.first + w.first + t, head, sub, h), n, g);
             } else {
                 float* row = part_row(a, p, DP, piece, tile == 0, y, r);
 #pragma unroll
@@ -667,10 +696,19 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p
 inline int padded(int64_t dim) { return dim <= 64 ? 64 : 128; }
 
 template <bool FP8, int CH, bool EXACT, int NR>
-hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
+hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, int64_t longest, hipStream_t s)
 {
     const unsigned y = unsigned(p.ys);
     if (alone) {
+        // Tiles of the longest sequence to one wave or dealt to four: rounds of as many waves (two on each SIMD) or workgroups as the chip holds, each with 5 us before its first tile
+        // is there and 1.2 us for each further one.  Measured: 119 sequences of 5 tokens with 32 key heads
+        // of 128 32 us dealt to four, 16 with one wave each.
+        const double tiles = double((longest + 63) / 64), units = double(p.tiles) * y;
+        const double by_wave = ceil(units / 2048.0) * (5.0 + 1.2 * tiles), by_four = ceil(units / 512.0) * (5.0 + 1.2 * ceil(tiles / 4.0));
+        if (by_wave < by_four) {
+            wave_kernel<FP8, CH, EXACT, NR><<<dim3(unsigned((p.tiles + kWaves - 1) / kWaves), y), 64 * kWaves, 0, s>>>(a, p);
+            return hipGetLastError();
+        }
         short_kernel<FP8, CH, EXACT, NR, 1><<<dim3(unsigned(p.tiles), y), 64 * kWaves, 0, s>>>(a, p);
         return hipGetLastError();
     }
@@ -683,17 +721,17 @@ hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s
 }
 
 template <bool FP8, int NR>
-hipError_t launch_dim(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
+hipError_t launch_dim(const CachedArgs& a, const Shape& p, bool alone, int64_t longest, hipStream_t s)
 {
-    if (a.c.dim == 128) return launch<FP8, 8, true, NR>(a, p, alone, s);
-    if (a.c.dim == 64) return launch<FP8, 4, true, NR>(a, p, alone, s);
-    return a.c.dim < 64 ? launch<FP8, 4, false, NR>(a, p, alone, s) : launch<FP8, 8, false, NR>(a, p, alone, s);
+    if (a.c.dim == 128) return launch<FP8, 8, true, NR>(a, p, alone, longest, s);
+    if (a.c.dim == 64) return launch<FP8, 4, true, NR>(a, p, alone, longest, s);
+    return a.c.dim < 64 ? launch<FP8, 4, false, NR>(a, p, alone, longest, s) : launch<FP8, 8, false, NR>(a, p, alone, longest, s);
 }
 
 template <bool FP8>
-hipError_t launch_type(const CachedArgs& a, const Shape& p, bool alone, hipStream_t s)
+hipError_t launch_type(const CachedArgs& a, const Shape& p, bool alone, int64_t longest, hipStream_t s)
 {
-    return p.nr == 2 ? launch_dim<FP8, 2>(a, p, alone, s) : launch_dim<FP8, 1>(a, p, alone, s);
+    return p.nr == 2 ? launch_dim<FP8, 2>(a, p, alone, longest, s) : launch_dim<FP8, 1>(a, p, alone, longest, s);
 }
 
 }  // namespace
@@ -714,7 +752,7 @@ hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s)
 {
     const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group, a.c.kv_heads);
     const bool alone = longest > 0 && longest <= kAlone * 64;
-    return a.c.fp8 ? launch_type<true>(a, p, alone, s) : launch_type<false>(a, p, alone, s);
+    return a.c.fp8 ? launch_type<true>(a, p, alone, longest, s) : launch_type<false>(a, p, alone, longest, s);
 }
 
 }  // namespace tl

@@ -398,7 +398,7 @@ struct Whole : Lane<T> {
     }
 };
 
-// Any other block: a token at a time, and once more when the scale is known.
+// Any other block: 16 / T tokens at a time, and once more when the scale is known.
 template <bool FP8, int T, Turn TURN>
 struct Some : Lane<T> {
     const Heads k_out;
@@ -409,17 +409,18 @@ struct Some : Lane<T> {
     using Lane<T>::first;
 
     __device__ inline Some(const AppendArgs& a, const Place& place) : Lane<T>(a, place), k_out(a.k_out) {}
-    __device__ inline bool has(int u) const { return d < dim && first + u >= at.slot && first + u < at.slot + at.n; }
+    __device__ inline int slot(int u) const { return u * (16 / T) + first / T; }
+    __device__ inline bool has(int u) const { return d < dim && slot(u) >= at.slot && slot(u) < at.slot + at.n; }
 
     template <bool TURNED>
     __device__ inline void row(const Heads in, int head, int u, float (&x)[8]) const
     {
-        const _Float16* p = this->place(in, head, first + u);
+        const _Float16* p = this->place(in, head, slot(u));
         const f16x8 own = *reinterpret_cast<const f16x8*>(p);
         if constexpr (TURNED) {
             Angles cs{};
-            if (d < r.rot) cs = angles<TURN>(r, at.pos + first + u, d);
-            turn8<TURN>(r, at.pos + first + u, p - d, d, own, partners<TURN>(r, p - d, d), cs, x);
+            if (d < r.rot) cs = angles<TURN>(r, at.pos + slot(u), d);
+            turn8<TURN>(r, at.pos + slot(u), p - d, d, own, partners<TURN>(r, p - d, d), cs, x);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = float(own[i]);
@@ -430,11 +431,11 @@ struct Some : Lane<T> {
     __device__ inline void turn(const Heads in, const Heads out, int head, bool used) const
     {
 #pragma clang loop unroll(disable)
-        for (int u = 0; u < T; ++u) {
+        for (int u = at.slot / (16 / T); u * (16 / T) < at.slot + at.n; ++u) {
             if (!has(u)) continue;
             float x[8] = {0, 0, 0, 0, 0, 0, 0, 0};
             if (used) row<true>(in, head, u, x);
-            this->put(out, head, first + u, x);
+            this->put(out, head, slot(u), x);
         }
     }
 
@@ -443,7 +444,7 @@ struct Some : Lane<T> {
     {
         float amax = 0.0f, zero = 0.0f;                      // a NaN or an infinity leaves no 0
 #pragma clang loop unroll(disable)
-        for (int u = 0; u < T; ++u) {
+        for (int u = at.slot / (16 / T); u * (16 / T) < at.slot + at.n; ++u) {
             if (!has(u)) continue;
             float x[8];
             row<KEY>(in, head, u, x);
@@ -456,15 +457,15 @@ struct Some : Lane<T> {
         uint8_t* const to = codes + block * (int64_t(16) * dim);
         const Divide over(block < 0 ? 0.0f : this->template rescale<FP8, KEY>(amax, zero, block, to, scales));
 #pragma clang loop unroll(disable)
-        for (int u = 0; u < T; ++u) {
+        for (int u = at.slot / (16 / T); u * (16 / T) < at.slot + at.n; ++u) {
             if (!has(u)) continue;
             float x[8];
             row<KEY>(in, head, u, x);
-            if (KEY && k_out.p) this->put(k_out, head, first + u, x);        // which may be the row that was read
+            if (KEY && k_out.p) this->put(k_out, head, slot(u), x);        // which may be the row that was read
             if (block < 0) continue;
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = over(x[i]);
-            put_codes<FP8, KEY>(to, dim, first + u, d, x);
+            put_codes<FP8, KEY>(to, dim, slot(u), d, x);
         }
     }
 };
