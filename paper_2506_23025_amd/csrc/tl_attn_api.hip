@@ -8,7 +8,7 @@ namespace {
 
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
-// 64 tokens of 2^24 elements each lie within the 32-bit offsets of the kernels.
+// 128 tokens of less than 2^24 elements each lie within 32-bit offsets (without a sign) of 2-byte numbers.
 inline tl_status heads_status(const tl_heads& h, int64_t heads)
 {
     if (heads == 0) return TL_OK;

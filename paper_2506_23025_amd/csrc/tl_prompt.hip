@@ -78,6 +78,39 @@ __device__ inline Item nth_longest(const PromptArgs& a, int rows, int place)
     return {int(__builtin_ctzll(there)), lo};
 }
 
+// What a workgroup takes: a block of `rows` query rows of a sequence, and a head.
+struct Where { int seq, block, head; };
+__device__ inline Where where(const PromptArgs& a, int rows)
+{
+    // heads that share keys go to one chiplet (workgroups are dealt to the 8 of them in turn); the rows with most keys first
+    int h = int(blockIdx.x) % a.q_heads;
+    const int place = int(blockIdx.x) / a.q_heads, places = int(gridDim.x) / a.q_heads;
+    Item it{places - 1 - place, 0};
+    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, rows, place);
+    else if (a.b.start) it = find_item(a.b, places - 1 - place, rows, 1);
+    if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads >> 3) + (h >> 3);
+    return {__builtin_amdgcn_readfirstlane(it.seq), __builtin_amdgcn_readfirstlane(it.i), h};
+}
+
+// A row's queries, turned round where the scale is negative, or 0: so that the largest product is the largest score.
+template <int KK>
+__device__ inline void load_queries(const PromptArgs& a, const _Float16* from, int half, f16x8 (&q)[KK])
+{
+#pragma unroll
+    for (int k = 0; k < KK; ++k) {
+        const int c = 2 * k + half;
+        q[k] = *reinterpret_cast<const f16x8*>(from + (c < (a.dim >> 3) ? c : 0) * 8);
+        if (c >= (a.dim >> 3) || a.scale == 0.0f) q[k] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    if (a.scale < 0.0f) {
+#pragma unroll
+        for (int k = 0; k < KK; ++k) q[k] = -q[k];
+    }
+}
+
+// Two fp16: ones in the place of each that is an infinity or a NaN (whose exponent of ones carries into the sign's place).
+__device__ inline uint32_t only_finite(uint32_t two) { return ((((two & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15) * 0xffffu; }
+
 template <int DP, int NW, int NB>
 __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
 {
@@ -91,18 +124,12 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    // heads that share keys go to one chiplet (workgroups are dealt to the 8 of them in turn); the rows with most keys first
-    int h = int(blockIdx.x) % a.q_heads;
-    const int place = int(blockIdx.x) / a.q_heads, places = int(gridDim.x) / a.q_heads;
-    Item it{places - 1 - place, 0};
-    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, 32 * NW, place);
-    else if (a.b.start) it = find_item(a.b, places - 1 - place, 32 * NW, 1);
-    if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads >> 3) + (h >> 3);
-    const int seq = __builtin_amdgcn_readfirstlane(it.seq);
+    const Where where_ = where(a, 32 * NW);
+    const int seq = where_.seq, h = where_.head;
     if (seq < 0) return;
     const Span sp = span(a.b, seq);
     const int n = __builtin_amdgcn_readfirstlane(sp.n), first = __builtin_amdgcn_readfirstlane(sp.first);
-    const int q0 = __builtin_amdgcn_readfirstlane(it.i) * (32 * NW);
+    const int q0 = where_.block * (32 * NW);
     if (q0 >= n) return;
     const int g = h / a.group;
     const int row0 = q0 + wave * 32, row = row0 + l32;       // this lane's query in the sequence
@@ -157,19 +184,7 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
 #pragma unroll
     for (int u = 0; u < NB - 1; ++u) fetch(u, u);
     f16x8 q[KK];
-    {
-        const _Float16* from = a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head;
-#pragma unroll
-        for (int k = 0; k < KK; ++k) {
-            const int c = 2 * k + half;
-            q[k] = *reinterpret_cast<const f16x8*>(from + (c < pieces ? c : 0) * 8);
-            if (c >= pieces || a.scale == 0.0f) q[k] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
-        }
-        if (a.scale < 0.0f) {
-#pragma unroll
-            for (int k = 0; k < KK; ++k) q[k] = -q[k];
-        }
-    }
+    load_queries<KK>(a, a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head, half, q);
     f32x16 o[DT];
 #pragma unroll
     for (int d = 0; d < DT; ++d)
@@ -268,13 +283,9 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
                 for (int u = 0; u < 4; ++u)
 #pragma unroll
                     for (int d = 0; d < DT; ++d) {
-                        // an exponent of ones carries into the sign's place
                         union { f16x8 v; uint32_t w[4]; } x{values(u, d)};
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t bad = (((x.w[i] & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15;
-                            x.w[i] &= ~(bad * 0xffffu);
-                        }
+                        for (int i = 0; i < 4; ++i) x.w[i] &= ~only_finite(x.w[i]);
                         o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.v, w[u], o[d], 0, 0, 0);
                     }
                 return;
@@ -381,13 +392,210 @@ __global__ __launch_bounds__(64 * NW, 2) void prompt_kernel(PromptArgs a)
     }
 }
 
+// The same for 64 query rows a workgroup, 32 a wave, S waves for each of them, which deal tiles of 32 keys among themselves and join their sums in LDS at the end: for few rows
+// with many keys (S = 4), where workgroups of 128 rows with all their keys leave most of the chip idle, and for many sequences of a few tokens (S = 1), where they are idle themselves.
+// Bound: one chain of products, softmax and products again a wave, with two waves on a SIMD at S = 4 (DP = 128): it takes 0.9 us a round of 4 tiles, whatever is in LDS in advance.
+template <int DP, int S>
+__global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(PromptArgs a)
+{
+    constexpr int R = 2, kKeys = 32 * S, kRow = DP * 2, kPieces = DP / 8, kBytes = kKeys * kRow, kSteps = kBytes / (R * S * 1024), kRows1 = 1024 / kRow;
+    constexpr int KK = DP / 16, DT = DP / 32;
+    constexpr int kSum = DP + 4;                             // a row's sums in LDS, so that rows begin in different banks
+    constexpr int kLds = R * S * 32 * kSum * 4 > 4 * kBytes ? R * S * 32 * kSum * 4 : 4 * kBytes;
+    __shared__ __attribute__((aligned(1024))) unsigned char lds[kLds];
+    __shared__ float stats[S][32 * R][2];
+    __shared__ int strange[R];                               // whether values that only some of the rows see hold an infinity or a NaN
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int l32 = lane & 31, half = lane >> 5, rw = wave % R, kw = wave / R;
+    const Where at = where(a, 32 * R);
+    if (at.seq < 0) return;
+    const Span sp = span(a.b, at.seq);
+    const int n = __builtin_amdgcn_readfirstlane(sp.n), first = __builtin_amdgcn_readfirstlane(sp.first), h = at.head, g = h / a.group;
+    const int q0 = at.block * (32 * R), own = at.block * R + rw, row = own * 32 + l32, pieces = a.dim >> 3;
+    if (q0 >= n) return;
+    const int whole = (n + 31) / 32, tiles = (at.block + 1) * R < whole ? (at.block + 1) * R : whole, rounds = (tiles + S - 1) / S;
+    const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);
+    if (pieces < kPieces) {                                  // dimensions beyond the head are never transferred
+        for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 64 * R * S) reinterpret_cast<u32x4*>(lds)[i] = u32x4{0, 0, 0, 0};
+        __syncthreads();
+    }
+    const char* const kbase = reinterpret_cast<const char*>(a.k.p + int64_t(first) * a.k.token + int64_t(g) * a.k.head);
+    const char* const vbase = reinterpret_cast<const char*>(a.v.p + int64_t(first) * a.v.token + int64_t(g) * a.v.head);
+    const uint32_t kstride = uint32_t(a.k.token) * 2u, vstride = uint32_t(a.v.token) * 2u;
+    const uint32_t base = lds_address(lds);
+    auto fetch = [&](int round, int buf) {
+        const char* const kb = kbase + int64_t(round) * kKeys * kstride;
+        const char* const vb = vbase + int64_t(round) * kKeys * vstride;
+        const int last = n - 1 - round * kKeys;
+#pragma unroll
+        for (int i = 0; i < kSteps; ++i) {
+            int r = (wave * kSteps + i) * kRows1 + lane / kPieces;
+            const int c = piece<DP>(r, lane % kPieces);
+            if (r > last) r = last;                          // tokens behind the sequence are masked: the last one again, no NaN that is not there
+            if (c < pieces) {
+                transfer(kb, uint32_t(r) * kstride + c * 16, base + buf * 2 * kBytes + (wave * kSteps + i) * 1024);
+                transfer(vb, uint32_t(r) * vstride + c * 16, base + (buf * 2 + 1) * kBytes + (wave * kSteps + i) * 1024);
+            }
+        }
+    };
+    fetch(0, 0);
+    f16x8 q[KK];
+    load_queries<KK>(a, a.q.p + int64_t(first + (row < n ? row : n - 1)) * a.q.token + int64_t(h) * a.q.head, half, q);
+    const uint32_t mine = base + kw * 32 * kRow;
+    uint32_t ka[KK], va[DT][2];
+#pragma unroll
+    for (int k = 0; k < KK; ++k) ka[k] = mine + l32 * kRow + piece<DP>(l32, 2 * k + half) * 16;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = e * 8 + half * 4 + ((lane & 15) >> 2), c = d * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            va[d][e] = mine + kBytes + r * kRow + piece<DP>(r, c) * 16 + (lane & 1) * 8;
+        }
+    f32x16 o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[d][i] = 0.0f;
+    float m = -kInf, l = 0.0f;
+    bool left_out = false;
+    auto work = [&](int t, auto buf) {
+        constexpr int AT = decltype(buf)::value * 2 * kBytes;
+        f32x16 s;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = 0.0f;
+#pragma unroll
+        for (int k = 0; k < KK; ++k) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_f16x8*)(ka[k] + AT), q[k], s, 0, 0, 0);
+        bool odd = false;
+        if (t == own) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (8 * (i >> 2) + 4 * half + (i & 3) > l32) s[i] = -kInf;
+            f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+            for (int i = 0; i < 32 * kRow / 1024; ++i) zero += *(const lds_f16x8*)(mine + kBytes + AT + i * 1024 + lane * 16) * _Float16(0.0f);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) odd |= !(zero[i] == _Float16(0.0f));
+            odd = __any(odd);
+            left_out = odd;
+        }
+        float mx = -kInf;
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
+        mx = mx == -kInf ? mx : mx * scale;
+        if (__any(mx > m + kSlack)) {
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            const float to = mx > m + kSlack ? mx : m;
+            const float f = power(m - finite(to));
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] *= f;
+            m = to;
+        }
+        const float mb = finite(m);
+        f16x8 w[2];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i >> 3][i & 7] = _Float16(power(__builtin_fmaf(s[i], scale, -mb)));
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) l = __builtin_amdgcn_fdot2(f16x2{w[u][i], w[u][i + 1]}, f16x2{_Float16(1.0f), _Float16(1.0f)}, l, false);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int d = 0; d < DT; ++d) {
+                union { f16x8 v; i16x4 h[2]; uint32_t w[4]; } x;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) x.h[e] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(va[d][e] + (AT + u * 16 * kRow)));
+                if (odd) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x.w[i] &= ~only_finite(x.w[i]);
+                }
+                o[d] = __builtin_amdgcn_mfma_f32_32x32x16_f16(x.v, w[u], o[d], 0, 0, 0);
+            }
+    };
+    auto turn = [&](int round, auto buf) {
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+        __syncthreads();                                     // these keys are there, and nobody reads from the other buffer any more
+        if (round + 1 < rounds) fetch(round + 1, decltype(buf)::value ^ 1);
+        const int t = round * S + kw;
+        if (t <= own) work(t, buf);
+    };
+    for (int round = 0; round < rounds; round += 2) {
+        turn(round, std::integral_constant<int, 0>{});
+        if (round + 1 < rounds) turn(round + 1, std::integral_constant<int, 1>{});
+    }
+    l += __shfl_xor(l, 32);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __syncthreads();
+    // The waves' sums meet in LDS, where keys and values were.
+    float* const sums = reinterpret_cast<float*>(lds);
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<f32x4*>(sums + ((kw * R + rw) * 32 + l32) * kSum + d * 32 + i * 8 + half * 4) =
+                f32x4{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+    if (half == 0) {
+        stats[kw][rw * 32 + l32][0] = m;
+        stats[kw][rw * 32 + l32][1] = l;
+    }
+    if (own % S == kw && lane == 0) strange[rw] = left_out;  // the wave of the keys that are masked for some
+    __syncthreads();
+    for (int i = threadIdx.x; i < 32 * R * kPieces; i += 64 * R * S) {
+        const int r = i / kPieces, c = i % kPieces;
+        if (q0 + r >= n || c >= pieces) continue;
+        float M = -kInf, L = 0.0f;
+#pragma unroll
+        for (int v = 0; v < S; ++v) M = fmaxf(M, stats[v][r][0]);
+        M = finite(M);
+        f32x4 x[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int v = 0; v < S; ++v) {
+            const float f = power(stats[v][r][0] - M);
+            const float* from = sums + (v * R * 32 + r) * kSum + c * 8;
+            L += stats[v][r][1] * f;
+            x[0] += *reinterpret_cast<const f32x4*>(from) * f;
+            x[1] += *reinterpret_cast<const f32x4*>(from + 4) * f;
+        }
+        const float f = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
+        f16x8 y;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            float sum = x[j >> 2][j & 3];
+            if (strange[r >> 5]) {
+                // values of the tokens that only some rows see, once more: an infinity or a NaN goes to the rows that see it
+                for (int key = q0 + (r & ~31); key <= q0 + r; ++key) {
+                    const float v = float(reinterpret_cast<const _Float16*>(vbase)[int64_t(key) * a.v.token + c * 8 + j]);
+                    if (!(fabsf(v) < kInf)) sum += v;
+                }
+            }
+            y[j] = _Float16(sum * f);
+        }
+        *reinterpret_cast<f16x8*>(a.out.p + int64_t(first + q0 + r) * a.out.token + int64_t(h) * a.out.head + c * 8) = y;
+    }
+}
+
 }  // namespace
 
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
 {
-    const auto grid = [&](int rows) { return unsigned((a.b.start ? a.b.tokens / rows + a.b.seqs : a.b.seqs) * a.q_heads); };
-    if (a.dim <= 64) prompt_kernel<64, 4, 2><<<grid(128), 256, 0, s>>>(a);
-    else prompt_kernel<128, 4, 2><<<grid(128), 256, 0, s>>>(a);
+    const auto grid = [&](int rows) { return (a.b.start ? a.b.tokens / rows + a.b.seqs : a.b.seqs) * a.q_heads; };
+    const unsigned small = unsigned(grid(64)), large = unsigned(grid(128));
+    // about as many of 64 rows have work
+    const int64_t busy = a.b.start ? (a.b.tokens + 32 * int64_t(a.b.seqs)) / 64 * a.q_heads : small;
+    if (a.b.tokens <= 40 * int64_t(a.b.seqs) || (a.b.tokens <= 80 * int64_t(a.b.seqs) && busy > 1024)) {
+        // Sequences that mostly need no more than 64 rows, and no split of their keys.  34 of 2 tokens with 32 heads of 128: 19 us with 128 rows, 11 with 64; 200 of 10 on average: 79 and 42;
+        // 60 of 64: 33 and 28, but 8 of 64, which all fit at once, 7.6 and 10; 60 of 96: 44 and 45.
+        if (a.dim <= 64) narrow_kernel<64, 1><<<small, 128, 0, s>>>(a);
+        else narrow_kernel<128, 1><<<small, 128, 0, s>>>(a);
+    } else if (busy <= (a.dim <= 64 ? 512 : 256)) {
+        // All fit on the chip at once, two to a compute unit or one.  One head of 64, 14587 tokens: 198 us with 128 rows and all their keys, 97 with 64 rows and keys dealt to four waves;
+        // 8 heads of 128, 2048 tokens: 40 and 29.  With 16 heads of 128, twice as many as fit: 42 and 46.
+        if (a.dim <= 64) narrow_kernel<64, 4><<<small, 512, 0, s>>>(a);
+        else narrow_kernel<128, 4><<<small, 512, 0, s>>>(a);
+    } else if (a.dim <= 64) prompt_kernel<64, 4, 2><<<large, 256, 0, s>>>(a);
+    else prompt_kernel<128, 4, 2><<<large, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -525,6 +525,70 @@ def test_prompt_strides_streams_and_rows_of_no_sequence():
     check_prompt(q, k0, v, st, prompt(q, k0, v, st, 0.2, views=(by_head[0], one, by_head[2])), 0.2)
 
 
+# Few rows, whose keys are dealt to several waves; many rows; many sequences of a few tokens; more than 64 sequences.
+KINDS_OF_CALL = {"few": ((0, 300, 77, 2, 130, 1, 257), 3), "many": ((0, 300, 77, 2, 130, 1, 257, 400), 24),
+                 "short": ((1, 2, 64, 0, 33, 32, 31, 65, 150, 3, 63, 7, 0) * 3, 32), "sequences": (tuple(range(60, 95)) * 2, 8)}
+
+
+def some_rows(rng, st, count):
+    return set(rng.integers(0, st[-1], count)) | set(np.maximum(st - 1, 0)) | set(np.minimum(st, st[-1] - 1)) | {x + o for x in st[:-1] for o in (31, 32, 63, 64, 127, 128)}
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
+@pytest.mark.parametrize("D", [128, 64, 80, 16])
+def test_prompt_kinds_of_calls(call, D):
+    n, H = KINDS_OF_CALL[call]
+    rng = np.random.default_rng(D)
+    st = starts(*n)
+    HK = H if H == 3 else H // 8
+    q, k, v = f16(rng, st[-1], H, D, scale=2.0), f16(rng, st[-1], HK, D), f16(rng, st[-1], HK, D)
+    got = prompt(q, k, v, st, D ** -0.5, extra=3)
+    check_prompt(q, k, v, st, got, D ** -0.5, some_rows(rng, st, 40))
+    assert np.array_equal(got, prompt(q, k, v, st, D ** -0.5))
+    check_prompt(q, k, v, st, prompt(q, k, v, st, -3.0), -3.0, some_rows(rng, st, 5))
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
+@pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
+def test_prompt_kinds_of_calls_show_nothing_unseen(call, what):
+    n, H = KINDS_OF_CALL[call]
+    rng = np.random.default_rng(31)
+    st = starts(*n)
+    q, k, v = f16(rng, st[-1], H, 64), f16(rng, st[-1], H, 64), f16(rng, st[-1], H, 64)
+    clean = prompt(q, k, v, st, 0.1)
+    longest = int(np.argmax(np.diff(st)))
+    first, end = int(st[longest]), int(st[longest + 1])
+    for at in (first, first + 40, end - 1):
+        v2 = v.copy()
+        v2[at, 1, 17] = what
+        got = prompt(q, k, v2, st, 0.1)
+        touched = np.zeros(got.shape, bool)
+        touched[at:end, 1, 17] = True
+        assert np.array_equal(got[~touched], clean[~touched]), at
+        assert (np.isnan(got[touched]) if np.isnan(what) else got[touched] == what).all(), at
+        k2 = k.copy()
+        k2[at, 1, 17] = np.nan
+        got = prompt(q, k2, v, st, 0.1)
+        touched[at:end, 1] = True
+        assert np.array_equal(got[~touched], clean[~touched]) and np.isnan(got[touched]).all(), at
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
+def test_prompt_kinds_of_calls_take_strides_and_streams(call):
+    import torch
+    n, H = KINDS_OF_CALL[call]
+    rng = np.random.default_rng(32)
+    st = starts(*n) + 5
+    T = int(st[-1]) + 6
+    q, k, v = f16(rng, T, H, 64), f16(rng, T, H, 64), f16(rng, T, H, 64)
+    by_head = [torch.from_numpy(np.ascontiguousarray(x.transpose(1, 0, 2))).cuda().transpose(0, 1) for x in (q, k, v)]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = prompt(q, k, v, st, 0.2, views=by_head, stream=side)
+    check_prompt(q, k, v, st, got, 0.2, some_rows(rng, st, 5))
+    assert (got[:5] == 77).all() and (got[T - 6:] == 77).all()
+
+
 def test_outputs_may_take_the_place_of_queries():
     import torch
     rng = np.random.default_rng(18)
