@@ -22,9 +22,8 @@ namespace tl {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kWavesAll = 2048;           // waves that share a call's tiles: two on each SIMD of 256 CUs
+constexpr int kWavesAll = 2048;           // waves that share a call's tiles: two on each SIMD of 256 CUs, or one where a row tile is of 32 rows
 constexpr int kFewRows = 1024;            // up to so many rows a workgroup joins the parts of each, beyond a wave
-constexpr int kAlone = 16;                // up to so many tiles a sequence is left to one workgroup: the second kernel would cost more than it saves
 
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;            // log2 of how far a weight may pass its reference (fp16 holds 2^15)
@@ -51,11 +50,14 @@ inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group, int kv_
     p.per = one ? 1 : most / p.heads;
     p.rows = p.per * p.heads;
     p.ys = kv_heads * p.subs;
-    p.pieces = kWavesAll / p.ys;
+    p.pieces = kWavesAll / p.nr / p.ys;
     if (p.pieces < 1) p.pieces = 1;
     p.tiles = one ? seqs : tokens / p.per + seqs;
     return p;
 }
+
+// Row tiles of all key heads, where sequences of several tokens end anywhere in one.
+inline double likely_tiles(int seqs, int tokens, const Shape& p) { return (p.per == 1 ? double(tokens) : double(tokens) / p.per + 0.5 * seqs) * p.ys; }
 
 constexpr int kExtra = 4;                 // floats beside a row's sums: m, l, R
 
@@ -700,11 +702,10 @@ hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, int64_t longe
 {
     const unsigned y = unsigned(p.ys);
     if (alone) {
-        // Tiles of the longest sequence to one wave or dealt to four: rounds of as many waves (two on each SIMD) or workgroups as the chip holds, each with 5 us before its first tile
-        // is there and 1.2 us for each further one.  Measured: 119 sequences of 5 tokens with 32 key heads
-        // of 128 32 us dealt to four, 16 with one wave each.
-        const double tiles = double((longest + 63) / 64), units = double(p.tiles) * y;
-        const double by_wave = ceil(units / 2048.0) * (5.0 + 1.2 * tiles), by_four = ceil(units / 512.0) * (5.0 + 1.2 * ceil(tiles / 4.0));
+        // Tiles of the longest sequence to one wave or dealt to four: rounds of as many waves as the chip holds, each with 5 us before its first tile is there and `step` for each
+        // further one.  Measured: 119 sequences of 5 tokens with 32 key heads of 128 32 us dealt to four, 16 with one wave each.
+        const double tiles = double((longest + 63) / 64), units = likely_tiles(a.b.seqs, a.b.tokens, p), waves = CH * NR > 8 ? 1024.0 : 2048.0, step = NR == 1 ? 1.2 : CH > 4 ? 2.3 : 1.4;
+        const double by_wave = fmax(units / waves, 1.0) * (5.0 + step * tiles), by_four = fmax(units * kWaves / waves, 1.0) * (5.0 + step * ceil(tiles / kWaves));
         if (by_wave < by_four) {
             wave_kernel<FP8, CH, EXACT, NR><<<dim3(unsigned((p.tiles + kWaves - 1) / kWaves), y), 64 * kWaves, 0, s>>>(a, p);
             return hipGetLastError();
@@ -751,7 +752,12 @@ size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t k
 hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s)
 {
     const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group, a.c.kv_heads);
-    const bool alone = longest > 0 && longest <= kAlone * 64;
+    // Up to so many tiles a sequence is left to one workgroup: the partial sums and the second kernel would cost more than a finer split saves, and more so with many row tiles of 32 rows.
+    // 2 sequences of 64 tokens with 16 heads of 128 on 2 key heads: 16 tiles 16 us and 20 with pieces, 32 tiles 24 and 26; 6 of 45 with 32 heads of 64 on 8: 40 tiles 21 and 27, 64
+    // tiles 30 and 33.  4 of 16 with 16 heads on 4: 32 tiles 22 and 18.  One token each, 4 with 16 heads on 4: 24 tiles 14 and 10.
+    const bool many = p.nr == 2 && likely_tiles(a.b.seqs, a.b.tokens, p) >= 32.0;
+    const int64_t alone_tiles = !many ? 16 : a.c.dim <= 64 ? 56 : 32;
+    const bool alone = longest > 0 && longest <= alone_tiles * 64;
     return a.c.fp8 ? launch_type<true>(a, p, alone, longest, s) : launch_type<false>(a, p, alone, longest, s);
 }
 

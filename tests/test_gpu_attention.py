@@ -278,6 +278,40 @@ def test_cached_long(kind, past, H, HK):
     assert np.array_equal(got, cached(st, q, 128 ** -0.5))
 
 
+def some_of(rng, st, count):
+    return set(rng.integers(0, st.T, count)) | {int(x) for x in st.start[:-1] if x < st.T} | {int(x) - 1 for x in st.start[1:]}
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("D,past", [(64, 2500), (128, 1700), (80, 1700), (64, 4000), (128, 2600)])
+def test_cached_several_tokens_and_many_heads(kind, D, past):
+    rng = np.random.default_rng(past + D)
+    st = Setup(past, [45, 1, 20, 0, 33], [past, 5, past // 3, 9, 70], 16, 8, D, 32, kind)
+    q = f16(rng, st.T, 16, D)
+    rows = some_of(rng, st, 8)
+    got = cached(st, q, D ** -0.5)
+    check_cached(st, q, got, D ** -0.5, rows)
+    assert np.array_equal(got, cached(st, q, D ** -0.5))
+    check_cached(st, q, cached(st, q, D ** -0.5, longest=0), D ** -0.5, rows)
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("most", [1, 2, 17])
+@pytest.mark.parametrize("D", [64, 128, 96])
+def test_cached_many_short_sequences(kind, most, D):
+    rng = np.random.default_rng(most + D)
+    n = np.ones(75, int) if most == 1 else rng.integers(0, most + 1, 75)
+    past = rng.integers(0, 120, 75)
+    past[[3, 70]] = -1
+    st = Setup(most * D, n, past, 32, 16, D, 16, kind)
+    q = f16(rng, st.T, 32, D)
+    rows = some_of(rng, st, 30)
+    got = cached(st, q, D ** -0.5, extra=1)
+    check_cached(st, q, got, D ** -0.5, rows)
+    assert np.array_equal(got, cached(st, q, D ** -0.5))
+    check_cached(st, q, cached(st, q, D ** -0.5, longest=0), D ** -0.5, rows)
+
+
 def test_cached_sharp_and_flat_scores():
     rng = np.random.default_rng(8)
     st = Setup(21, [1, 1, 1, 3], [700, 65, 300, 90], 4, 2, 128, 64, "int8")
