@@ -10,7 +10,7 @@
 // Softmax: weights p = 2^(x - m) are summed as they are, and reach the product as p * scale_v relative to a second running reference
 // R = max(x + log2 scale_v), so that their fp16 form (2^-11) is exact enough whatever the scales of the blocks are.  The references move only when a score
 // is more than 2^8 beyond them, so a tile needs no exchange between lanes.
-// Bound: memory.  Short caches: a workgroup takes a row tile, its 4 waves deal the tiles among themselves and join their sums in LDS.  Otherwise the tiles of the whole
+// Bound: memory.  Short caches: a workgroup takes a row tile, its waves deal the tiles among themselves and join their sums in LDS.  Otherwise the tiles of the whole
 // call stand in one row, sequence after sequence, and every wave of a grid that fills the chip once takes an equal piece of it, whatever the sequences' lengths; they are
 // read on the device, so one captured launch serves every step.  Pieces of row tiles that several waves share meet in a second kernel.
 #include "tl_attn.hpp"
@@ -42,8 +42,9 @@ struct Shape {
 inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group, int kv_heads)
 {
     Shape p;
-    // two blocks of 16 rows share the widened codes where the tokens of a sequence fill them
-    p.nr = tokens * group > 16 * seqs && !one ? 2 : 1;
+    // Two blocks of 16 rows share the widened codes where the tokens of a sequence fill them.  One token each keeps to one, however many heads share its keys: 64 sequences of up to 800
+    // with 32 heads on one of 128 9.8 us, with two 13.6 (over up to 9000, 64 heads on 2 of 64, 35.6 and 33.8).
+    p.nr = tokens * group > 16 * seqs && tokens > seqs ? 2 : 1;
     const int most = 16 * p.nr;
     p.heads = group < most ? group : most;
     p.subs = (group + p.heads - 1) / p.heads;
@@ -56,8 +57,11 @@ inline Shape shape_of(int64_t seqs, int64_t tokens, bool one, int group, int kv_
     return p;
 }
 
-// Row tiles of all key heads, where sequences of several tokens end anywhere in one.
-inline double likely_tiles(int seqs, int tokens, const Shape& p) { return (p.per == 1 ? double(tokens) : double(tokens) / p.per + 0.5 * seqs) * p.ys; }
+// About how many row tiles of all key heads there are: sequences of several tokens end anywhere in one.
+inline double likely_tiles(int seqs, int tokens, const Shape& p)
+{
+    return (p.per == 1 ? double(tokens) : fmax(double(tokens) / p.per + 0.5 * seqs, fmin(tokens, seqs))) * p.ys;
+}
 
 constexpr int kExtra = 4;                 // floats beside a row's sums: m, l, R
 
@@ -451,8 +455,8 @@ __device__ inline _Float16* out_row(const CachedArgs& a, const Shape& p, int row
 }
 
 // A workgroup for each row tile of each key head.
-template <bool FP8, int CH, bool EXACT, int NR, int NB>
-__global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void short_kernel(CachedArgs a, Shape p)
+template <bool FP8, int CH, bool EXACT, int NR, int W>
+__global__ __launch_bounds__(64 * W, CH * NR > 8 ? 1 : 2) void short_kernel(CachedArgs a, Shape p)
 {
     constexpr int DP = CH * 16;
     const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
@@ -465,12 +469,12 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void short_k
     sp = {same(sp.first), same(sp.n)};
     if (it.i * p.per >= sp.n) return;
     const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
-    Walk<FP8, CH, EXACT, NR, NB> w;
+    Walk<FP8, CH, EXACT, NR, 1> w;
     w.start(a, p, sp, same(cached_of(a.b, it.seq)), it.i, head, sub);
-    w.walk(a, it.seq, head, wave, int((w.most + 63) >> 6), kWaves);
+    w.walk(a, it.seq, head, wave, int((w.most + 63) >> 6), W);
 
-    __shared__ float sums[kWaves][16 * NR][DP + 4];
-    __shared__ Row stats[kWaves][16 * NR];
+    __shared__ float sums[W][16 * NR][DP + 4];
+    __shared__ Row stats[W][16 * NR];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
         if (g == 0) stats[wave][n * 16 + m16] = {w.m[n], w.l[n], w.R[n]};
@@ -479,16 +483,16 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void short_k
     }
     __syncthreads();
     constexpr int kQuads = DP / 4;
-    for (int i = threadIdx.x; i < w.rows * kQuads; i += 64 * kWaves) {
+    for (int i = threadIdx.x; i < w.rows * kQuads; i += 64 * W) {
         const int r = i / kQuads, d = (i - r * kQuads) * 4, t = r / p.heads, h = r - t * p.heads;
         if (h >= w.heads || d >= a.c.dim) continue;
         float M = -kInf, L = 0.0f;
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) M = fmaxf(M, stats[v][r].m);
+        for (int v = 0; v < W; ++v) M = fmaxf(M, stats[v][r].m);
         M = finite(M);
         f32x4 sum = {0, 0, 0, 0};
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
+        for (int v = 0; v < W; ++v) {
             L += stats[v][r].l * power(stats[v][r].m - M);
             sum += *reinterpret_cast<f32x4*>(&sums[v][r][d]) * power(stats[v][r].R - M);
         }
@@ -710,7 +714,15 @@ hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, int64_t longe
             wave_kernel<FP8, CH, EXACT, NR><<<dim3(unsigned((p.tiles + kWaves - 1) / kWaves), y), 64 * kWaves, 0, s>>>(a, p);
             return hipGetLastError();
         }
-        short_kernel<FP8, CH, EXACT, NR, 1><<<dim3(unsigned(p.tiles), y), 64 * kWaves, 0, s>>>(a, p);
+        if constexpr (CH * NR <= 8) {
+            // eight waves where that leaves two on a SIMD: 45 tokens of 6 sequences over 3001 with 32 heads of 64 on 8 21.6 us with four, 18.7; one token of 64 over up to 900 with 8 key heads of 128
+            // (512 row tiles) 18.6 and 21
+            if (units <= (NR == 1 ? 256.0 : 512.0)) {
+                short_kernel<FP8, CH, EXACT, NR, 2 * kWaves><<<dim3(unsigned(p.tiles), y), 64 * 2 * kWaves, 0, s>>>(a, p);
+                return hipGetLastError();
+            }
+        }
+        short_kernel<FP8, CH, EXACT, NR, kWaves><<<dim3(unsigned(p.tiles), y), 64 * kWaves, 0, s>>>(a, p);
         return hipGetLastError();
     }
     piece_kernel<FP8, CH, EXACT, NR, 1><<<unsigned((p.pieces * p.ys + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a, p);
@@ -752,11 +764,12 @@ size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t k
 hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s)
 {
     const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group, a.c.kv_heads);
-    // Up to so many tiles a sequence is left to one workgroup: the partial sums and the second kernel would cost more than a finer split saves, and more so with many row tiles of 32 rows.
-    // 2 sequences of 64 tokens with 16 heads of 128 on 2 key heads: 16 tiles 16 us and 20 with pieces, 32 tiles 24 and 26; 6 of 45 with 32 heads of 64 on 8: 40 tiles 21 and 27, 64
-    // tiles 30 and 33.  4 of 16 with 16 heads on 4: 32 tiles 22 and 18.  One token each, 4 with 16 heads on 4: 24 tiles 14 and 10.
-    const bool many = p.nr == 2 && likely_tiles(a.b.seqs, a.b.tokens, p) >= 32.0;
-    const int64_t alone_tiles = !many ? 16 : a.c.dim <= 64 ? 56 : 32;
+    // Up to so many tiles a sequence is left to one workgroup: the partial sums and the second kernel would cost more than a finer split saves, and more so with many row tiles, or of 32
+    // rows.  In us, so and with pieces, heads of 128: one token of 8 sequences, 8 key heads, 15 tiles 10 and 13, 30 tiles 16 and 13; of 24 with 8 of 96, 22 tiles 16 and 23; 64 tokens of 2,
+    // 16 heads on 2, 32 tiles 24 and 26; 16 of 4, 16 heads on 4, 32 tiles 22 and 18.  Heads of 64: 45 tokens of 6, 32 heads on 8, 71 tiles 25 and 30; 5 of 3, 24 tiles 9.4 and 10.2, 32 tiles of
+    // one token of 5 11 and 10.
+    const bool many = likely_tiles(a.b.seqs, a.b.tokens, p) >= (p.nr == 2 ? 32.0 : 128.0);
+    const int64_t alone_tiles = a.c.dim <= 64 ? (many && p.nr == 2 ? 80 : 24) : !many ? 16 : p.nr == 2 ? 32 : 24;
     const bool alone = longest > 0 && longest <= alone_tiles * 64;
     return a.c.fp8 ? launch_type<true>(a, p, alone, longest, s) : launch_type<false>(a, p, alone, longest, s);
 }
