@@ -13,6 +13,8 @@
 // Bound: memory.  Short caches: a workgroup takes a row tile, its waves deal the tiles among themselves and join their sums in LDS.  Otherwise the tiles of the whole
 // call stand in one row, sequence after sequence, and every wave of a grid that fills the chip once takes an equal piece of it, whatever the sequences' lengths; they are
 // read on the device, so one captured launch serves every step.  Pieces of row tiles that several waves share meet in a second kernel.
+// Measured: 3 sequences of up to 131072 tokens, 32 heads of 128 on 8 key heads, int8 98 us (5.85 TB/s); 48 of up to 4096, e4m3 47.5 us (5.05 TB/s, 42 of them here and 5 in the second
+// kernel); 16 of up to 2047 with 32 key heads 31.5 us (4.4 TB/s).  One sequence of 700 tokens with 16 heads 6.8 us, a chain of reads: lengths, pages, scales, codes.
 #include "tl_attn.hpp"
 
 #include <cmath>
@@ -227,8 +229,8 @@ __device__ inline float* part_row(const CachedArgs& a, const Shape& p, int dp, i
 }
 
 // One row tile of one key head: its queries, and its sums over tiles begin, begin + step, ... below end.
-// NB tiles are in registers or on their way to them.  EXACT: the head has CH * 16 dimensions, else fewer.
-template <bool FP8, int CH, bool EXACT, int NR, int NB>
+// A tile is in registers or on its way to them.  EXACT: the head has CH * 16 dimensions, else fewer.
+template <bool FP8, int CH, bool EXACT, int NR>
 struct Walk {
     static constexpr int J = (CH + 3) / 4;
     f16x8 q[NR][J][2];
@@ -291,9 +293,9 @@ struct Walk {
         const int in_page = int(blocks - 1);
         auto page_at = [&](int64_t block) { return page_of(a.c, seq, block); };
         auto place = [&](int page, int64_t block) { return (int64_t(page < 0 ? 0 : page) * a.c.kv_heads + head) * blocks + (block & in_page); };
-        u32x4 kw[NB][4][J], vw[NB][CH];
-        float ks[NB], vs[NB];
-        bool there[NB];                                      // the lane's block has a page
+        u32x4 kw[4][J], vw[CH];
+        float ks = 0.0f, vs = 0.0f;
+        bool there = false;                                  // the lane's block has a page
         // Loads come back in order, so what is needed first is asked for first: the pages of the tile after, a tile's scales, its keys, its values.
         int next_k = 0, next_v = 0;
         int64_t value_block = 0;
@@ -301,47 +303,38 @@ struct Walk {
             next_k = page_at(int64_t(tile) * 4 + (m16 >> 2));
             next_v = page_at(int64_t(tile) * 4 + g);
         };
-        auto load_k = [&](int tile, int at) {
+        auto load_k = [&](int tile) {
             const int64_t key_block = place(next_k, int64_t(tile) * 4 + (m16 >> 2));
             value_block = place(next_v, int64_t(tile) * 4 + g);
-            there[at] = next_v >= 0;
+            there = next_v >= 0;
             ask_pages(tile + step);
-            ks[at] = a.c.ks[value_block];
-            vs[at] = a.c.vs[value_block];
+            ks = a.c.ks[value_block];
+            vs = a.c.vs[value_block];
             const uint8_t* from = a.c.k + key_block * block_bytes + (m16 & 3) * 16;
 #pragma unroll
             for (int b = 0; b < 4; ++b)
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
                     const int c = EXACT || 4 * j + g < chunks ? 4 * j + g : 0;
-                    kw[at][b][j] = fetch<NR == 1>(from + (b * chunks + c) * 64);
+                    kw[b][j] = fetch<NR == 1>(from + (b * chunks + c) * 64);
                 }
         };
-        auto load_v = [&](int at) {
+        auto load_v = [&] {
             const uint8_t* from = a.c.v + value_block * block_bytes + m16 * 16;
 #pragma unroll
-            for (int d = 0; d < CH; ++d) vw[at][d] = fetch<NR == 1>(from + (EXACT || d < chunks ? d : 0) * 256);
+            for (int d = 0; d < CH; ++d) vw[d] = fetch<NR == 1>(from + (EXACT || d < chunks ? d : 0) * 256);
         };
         begin = same(begin);
         end = same(end);
         if (begin >= end) return;
         ask_pages(begin);
-#pragma unroll
-        for (int u = 0; u < NB; ++u) {
-            if (begin + u * step < end) {
-                load_k(begin + u * step, u);
-                load_v(u);
-            }
-        }
-        for (int tile0 = begin; tile0 < end; tile0 += NB * step) {
-#pragma unroll
-        for (int u = 0; u < NB; ++u) {
-            const int tile = tile0 + u * step, ahead = tile + NB * step;
-            if (tile >= end) break;
-            const bool more = ahead < end;
-            const bool inside = there[u];
+        load_k(begin);
+        load_v();
+        for (int tile = begin; tile < end; tile += step) {
+            const bool more = tile + step < end;
+            const bool inside = there;
             const bool masked = int64_t(tile) * 64 + 64 > least || !__all(inside);
-            const float ksc = ks[u] * scale, vsc = vs[u];
+            const float ksc = ks * scale, vsc = vs;
             f32x4 s[NR][4];
 #pragma unroll
             for (int b = 0; b < 4; ++b) {
@@ -349,7 +342,7 @@ struct Walk {
                 for (int n = 0; n < NR; ++n) s[n][b] = FP8 ? f32x4{0, 0, 0, 0} : f32x4{from[n], from[n], from[n], from[n]};
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
-                    const f16x8 k0 = widen<FP8, true>(kw[u][b][j][0], kw[u][b][j][1]), k1 = widen<FP8, true>(kw[u][b][j][2], kw[u][b][j][3]);
+                    const f16x8 k0 = widen<FP8, true>(kw[b][j][0], kw[b][j][1]), k1 = widen<FP8, true>(kw[b][j][2], kw[b][j][3]);
 #pragma unroll
                     for (int n = 0; n < NR; ++n) {
                         s[n][b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k0, q[n][j][0], s[n][b], 0, 0, 0);
@@ -357,7 +350,7 @@ struct Walk {
                     }
                 }
             }
-            if (more) load_k(ahead, u);
+            if (more) load_k(tile + step);
             const float lv = __builtin_amdgcn_logf(vsc);
             f16x8 w[NR][2];
             auto weigh = [&](auto some) {
@@ -417,15 +410,14 @@ struct Walk {
             else weigh(std::false_type{});
 #pragma unroll
             for (int d = 0; d < CH; ++d) {
-                const f16x8 v0 = widen<FP8>(vw[u][d][0], vw[u][d][1]), v1 = widen<FP8>(vw[u][d][2], vw[u][d][3]);
+                const f16x8 v0 = widen<FP8>(vw[d][0], vw[d][1]), v1 = widen<FP8>(vw[d][2], vw[d][3]);
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
                     o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v0, w[n][0], o[n][d], 0, 0, 0);
                     o[n][d] = __builtin_amdgcn_mfma_f32_16x16x32_f16(v1, w[n][1], o[n][d], 0, 0, 0);
                 }
             }
-            if (more) load_v(u);
-        }
+            if (more) load_v();
         }
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
@@ -469,7 +461,7 @@ __global__ __launch_bounds__(64 * W, CH * NR > 8 ? 1 : 2) void short_kernel(Cach
     sp = {same(sp.first), same(sp.n)};
     if (it.i * p.per >= sp.n) return;
     const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
-    Walk<FP8, CH, EXACT, NR, 1> w;
+    Walk<FP8, CH, EXACT, NR> w;
     w.start(a, p, sp, same(cached_of(a.b, it.seq)), it.i, head, sub);
     w.walk(a, it.seq, head, wave, int((w.most + 63) >> 6), W);
 
@@ -518,7 +510,7 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR > 8 ? 1 : 2) void wave_kernel(
     sp = {same(sp.first), same(sp.n)};
     if (it.i * p.per >= sp.n) return;
     const int head = int(blockIdx.y) / p.subs, sub = int(blockIdx.y) - head * p.subs;
-    Walk<FP8, CH, EXACT, NR, 1> w;
+    Walk<FP8, CH, EXACT, NR> w;
     w.start(a, p, sp, same(cached_of(a.b, it.seq)), it.i, head, sub);
     w.walk(a, it.seq, head, 0, int((w.most + 63) >> 6), 1);
 #pragma unroll
@@ -530,8 +522,8 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR > 8 ? 1 : 2) void wave_kernel(
 
 // A wave for each piece of the row of all tiles and each key head: neighbouring waves read the heads of the same tokens, which lie side by side in
 // a page.  A row tile that a piece has whole is written out, of the others the sums go to the workspace.
-template <bool FP8, int CH, bool EXACT, int NR, int NB>
-__global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_kernel(CachedArgs a, Shape p)
+template <bool FP8, int CH, bool EXACT, int NR>
+__global__ __launch_bounds__(64 * kWaves, CH * NR > 8 ? 1 : 2) void piece_kernel(CachedArgs a, Shape p)
 {
     constexpr int DP = CH * 16;
     const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
@@ -574,7 +566,7 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR * NB > 8 ? 1 : 2) void piece_k
         const double left = stop - at;
         const int to = same(double(tiles - tile) <= left ? tiles : tile + int(left));
         const Span sp = {same(need.first), same(need.n)};
-        Walk<FP8, CH, EXACT, NR, NB> w;
+        Walk<FP8, CH, EXACT, NR> w;
         w.start(a, p, sp, same(need.past), rt, head, sub);
         const int seen = int((w.most + 63) >> 6);
         w.walk(a, seq, head, tile, to < seen ? to : seen, 1);
@@ -725,7 +717,7 @@ hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, int64_t longe
         short_kernel<FP8, CH, EXACT, NR, kWaves><<<dim3(unsigned(p.tiles), y), 64 * kWaves, 0, s>>>(a, p);
         return hipGetLastError();
     }
-    piece_kernel<FP8, CH, EXACT, NR, 1><<<unsigned((p.pieces * p.ys + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a, p);
+    piece_kernel<FP8, CH, EXACT, NR><<<unsigned((p.pieces * p.ys + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (p.tiles * p.ys * p.rows <= kFewRows) join_kernel<CH, kWaves><<<dim3(unsigned(p.tiles), y, unsigned(p.rows)), 64 * kWaves, 0, s>>>(a, p);
