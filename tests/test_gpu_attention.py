@@ -651,3 +651,68 @@ def test_prompt_and_cache_agree():
     again = cached(st, q, D ** -0.5)
     off = np.abs(whole.astype(np.float64) - again)
     assert off.max() < 0.1 and off.mean() < 0.01
+
+
+# ---- beyond 32 bits ------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 3, 1]])
+def test_a_cache_of_more_than_4_gigabytes(kind, new):
+    """The same calls with pages at the beginning of a small cache and near the end of a large one: the same codes and outputs."""
+    import torch
+    rng = np.random.default_rng(41)
+    H, HK, D, page, past = 16, 8, 128, 64, [900, 17, 300]
+    pages, each = 75000, 16                                   # 64 KiB a page
+    T = sum(new)
+    q, k, v = f16(rng, T, H, D), f16(rng, T, HK, D), f16(rng, T, HK, D)
+    start, pastd = to_dev(starts(*new)), to_dev(np.array(past, np.int32))
+    rope = tl.make_rope(to_dev(tl.tl_rope_table(1000, D)), D)
+    codes = torch.from_numpy(rng.integers(0, 100, (2, 3 * each, HK, page * D), dtype=np.uint8)).cuda()
+    scales = torch.from_numpy(rng.uniform(0.01, 0.02, (2, 3 * each, HK, page // 16)).astype(np.float32)).cuda()
+    got = []
+    for count in (3 * each, pages):
+        at = torch.from_numpy(rng.permutation(3 * each)).cuda() + (count - 3 * each)
+        kv, sc = [], []
+        for i in range(2):
+            kv.append(torch.empty((count, HK, page * D), dtype=torch.uint8, device="cuda"))
+            sc.append(torch.empty((count, HK, page // 16), dtype=torch.float32, device="cuda"))
+            kv[i][at], sc[i][at] = codes[i], scales[i]
+        table = at.to(torch.int32).view(3, each)
+        cache = tl.make_kv_cache(*kv, *sc, table, page, D, KINDS[kind])
+        batch = tl.make_batch(None if T == 3 else start, pastd, 3, T)
+        qd, out = on(q), blank(T, H, D)
+        tl.tl_kv_append(tl.make_append_job(qd, on(k), on(v), qd, None, batch, cache, rope))
+        outs = []
+        for longest in (0, 1000):
+            space = torch.empty(tl.tl_attn_cached_workspace(3, T, H, HK, D), dtype=torch.uint8, device="cuda")
+            tl.tl_attn_cached(tl.make_cached_job(qd, out, batch, cache, 0.1, longest, space))
+            outs.append(taken(out).copy())
+        assert np.isfinite(outs[0]).all()
+        got.append([x[at].cpu().numpy() for x in kv + sc] + outs)
+        del kv, sc, cache
+    for a, b in zip(*got):
+        assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("T,H", [(300, 2), (300, 64), (100, 64)])
+def test_rows_further_apart_than_32_bits_reach(T, H):
+    """Tokens 2^23 + 8 numbers apart: the whole is 5 GB; the same bits as side by side."""
+    import torch
+    rng = np.random.default_rng(42)
+    stride, D = 2 ** 23 + 8, 64
+    flat = torch.empty(T * stride, dtype=torch.float16, device="cuda")
+    q, k, v = f16(rng, T, H, D), f16(rng, T, H, D), f16(rng, T, H, D)
+    wide = [torch.as_strided(flat, (T, H, D), (stride, D, 1), i * H * D) for i in range(4)]
+    for t, x in zip(wide, (q, k, v)):
+        t.copy_(torch.from_numpy(x))
+    st = starts(T) if T > 100 else starts(*[2] * (T // 2))
+    batch = tl.make_batch(to_dev(st), None, len(st) - 1, T)
+    tl.tl_attn_prompt(tl.make_prompt_job(*wide, batch, 0.1))
+    torch.cuda.synchronize()
+    assert np.array_equal(wide[3].cpu().numpy(), prompt(q, k, v, st, 0.1))
+    rope = tl.make_rope(to_dev(tl.tl_rope_table(T, D)), D)
+    near = [blank(T, H, D) for _ in range(2)]
+    tl.tl_kv_append(tl.make_append_job(on(q), on(k), None, *near, batch, None, rope))
+    tl.tl_kv_append(tl.make_append_job(wide[0], wide[1], None, wide[0], wide[1], batch, None, rope))
+    for a, b in zip(near, wide):
+        assert np.array_equal(taken(a), b.cpu().numpy())
