@@ -12,7 +12,7 @@
 // Bound: the matrix pipes and, beside them, the softmax's vector instructions; two workgroups on a CU, so that one's products run beside the other's softmax.
 // Rounding: scores, statistics and sums in 32 bits; weights become fp16 (2^-11 of each) for the second product, and their sum is of the rounded ones, so that weights add up to 1.
 // Measured: 16384 tokens, 32 heads of 128 on 8 key heads 2.01 to 2.16 ms from card to card, 1.02 to 1.09 PFLOP/s: the matrix pipes are busy 61 % of the time and the chip's power sets the clock (1.75 GHz; the same
-// on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 59 to 63 us, the matrix pipes busy 33 %.
+// on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 54 to 58 us.
 #include "tl_attn.hpp"
 
 #include <type_traits>
@@ -55,7 +55,7 @@ __device__ inline int piece(int r, int c)
 
 // Blocks of `rows` query rows of all sequences (64 at most), those with most keys before others: the one in that place.  What is heavy begins early, so that the chip is
 // full until the end; where all fit at once, two to a compute unit, the second half comes in the opposite order, so that a heavy one shares its unit with a light one.
-__device__ inline Item nth_longest(const PromptArgs& a, int rows, int place)
+__device__ inline Item nth_longest(const PromptArgs& a, int rows, int heads, int place)
 {
     const int lane = threadIdx.x & 63;
     const int n = lane < a.b.seqs ? span(a.b, lane).n : 0, blocks = (n + rows - 1) / rows;
@@ -64,8 +64,8 @@ __device__ inline Item nth_longest(const PromptArgs& a, int rows, int place)
     };
     const int all = from(0);
     if (place >= all) return {-1, 0};
-    const int half = 256 / a.q_heads;
-    if (int64_t(all) * a.q_heads <= 512 && place >= half) place = all - 1 - (place - half);
+    const int half = 256 / heads;
+    if (int64_t(all) * heads <= 512 && place >= half) place = all - 1 - (place - half);
     if (a.b.seqs == 1) return {0, all - 1 - place};
     // the largest number j with more than `place` blocks from j on
     int lo = 0, hi = 1;
@@ -81,17 +81,17 @@ __device__ inline Item nth_longest(const PromptArgs& a, int rows, int place)
     return {int(__builtin_ctzll(there)), lo};
 }
 
-// What a workgroup takes: a block of `rows` query rows of a sequence, and a head.
+// What a workgroup takes: a block of `rows` query rows of a sequence, and one of `heads` heads or groups of heads.
 struct Where { int seq, block, head; };
-__device__ inline Where where(const PromptArgs& a, int rows)
+__device__ inline Where where(const PromptArgs& a, int rows, int heads)
 {
     // heads that share keys go to one chiplet (workgroups are dealt to the 8 of them in turn); the rows with most keys first
-    int h = int(blockIdx.x) % a.q_heads;
-    const int place = int(blockIdx.x) / a.q_heads, places = int(gridDim.x) / a.q_heads;
+    int h = int(blockIdx.x) % heads;
+    const int place = int(blockIdx.x) / heads, places = int(gridDim.x) / heads;
     Item it{places - 1 - place, 0};
-    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, rows, place);
+    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, rows, heads, place);
     else if (a.b.start) it = find_item(a.b, places - 1 - place, rows, 1);
-    if (a.q_heads % 8 == 0) h = (h & 7) * (a.q_heads >> 3) + (h >> 3);
+    if (heads % 8 == 0) h = (h & 7) * (heads >> 3) + (h >> 3);
     return {__builtin_amdgcn_readfirstlane(it.seq), __builtin_amdgcn_readfirstlane(it.i), h};
 }
 
@@ -114,8 +114,8 @@ __device__ inline void load_queries(const PromptArgs& a, const _Float16* from, i
 // Two fp16: ones in the place of each that is an infinity or a NaN (whose exponent of ones carries into the sign's place).
 __device__ inline uint32_t only_finite(uint32_t two) { return ((((two & 0x7c007c00u) + 0x04000400u) & 0x80008000u) >> 15) * 0xffffu; }
 
-// 128 query rows a workgroup.
-template <int DP>
+// 128 query rows a workgroup: of one head, or 64 or 32 of each of two or four HEADS that share their keys, which leaves fewer rows behind a sequence's end and less of the last tiles masked.
+template <int DP, int HEADS>
 __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
 {
     constexpr int NW = 4;                                    // waves, 32 rows each
@@ -123,21 +123,21 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
     constexpr int kSteps = kBytes / (NW * 1024);             // transfers of a wave for keys, and as many for values
     constexpr int kRows1 = 1024 / kRow;                      // tokens of a transfer
     constexpr int KK = DP / 16, DT = DP / 32;
-    static_assert(32 * NW % (2 * kTile) == 0, "both buffers are used equally before a workgroup's rows");
+    constexpr int kRows = 32 * NW / HEADS;                   // of a head
     __shared__ __attribute__((aligned(1024))) unsigned char lds[2][2][kBytes];
     __shared__ int strange[2][NW];                           // whether the values that a wave brought hold an infinity or a NaN
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const Where where_ = where(a, 32 * NW);
-    const int seq = where_.seq, h = where_.head;
+    const Where where_ = where(a, kRows, a.q_heads / HEADS);
+    const int seq = where_.seq, h = where_.head * HEADS + wave % HEADS;
     if (seq < 0) return;
     const Span sp = span(a.b, seq);
     const int n = __builtin_amdgcn_readfirstlane(sp.n), first = __builtin_amdgcn_readfirstlane(sp.first);
-    const int q0 = where_.block * (32 * NW);
+    const int q0 = where_.block * kRows;
     if (q0 >= n) return;
     const int g = h / a.group;
-    const int row0 = q0 + wave * 32, row = row0 + l32;       // this lane's query in the sequence
+    const int row0 = q0 + wave / HEADS * 32, row = row0 + l32;       // this lane's query in the sequence
     const int pieces = a.dim >> 3;
     const float scale = a.scale == 0.0f ? 1.0f : fabsf(a.scale);      // with queries that are turned round, or 0: the largest product is the largest score
 
@@ -145,8 +145,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
         for (int i = threadIdx.x; i < 4 * kBytes / 16; i += 64 * NW) reinterpret_cast<u32x4*>(&lds[0][0][0])[i] = u32x4{0, 0, 0, 0};
         __syncthreads();
     }
-    const int most = q0 + 32 * NW < n ? q0 + 32 * NW : n;    // keys that the workgroup sees
-    const int tiles = (most + kTile - 1) / kTile;
+    const int most = q0 + kRows < n ? q0 + kRows : n;        // keys that the workgroup sees
+    const int tiles = (most + kTile - 1) / kTile, full = q0 / kTile & ~1;     // the first ones without a mask, both buffers as often
     const char* const kbase = reinterpret_cast<const char*>(a.k.p + int64_t(first) * a.k.token + int64_t(g) * a.k.head);
     const char* const vbase = reinterpret_cast<const char*>(a.v.p + int64_t(first) * a.v.token + int64_t(g) * a.v.head);
     const uint32_t kstride = uint32_t(a.k.token) * 2u, vstride = uint32_t(a.v.token) * 2u;
@@ -319,7 +319,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
         odd = __any(odd);
         if (lane == 0) strange[buf][wave] = odd;
     };
-    if (q0 == 0) look(0);
+    if (full == 0) look(0);
     arrived();
     // Tiles that all rows of the workgroup see, two at a time; while a tile is worked on, the next is on its way.
     int t = 0;
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
         fetch(t + 1, B ^ 1);
         work(t, std::integral_constant<int, B * 2 * kBytes>{}, std::false_type{});
         ++t;
-        if (B == 1 && t == q0 / kTile) look(0);
+        if (B == 1 && t == full) look(0);
         arrived();
     };
     // tiles that some row does not see, or not all of
@@ -341,18 +341,20 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
         if (t < tiles) look(B ^ 1);
         arrived();
     };
-    auto round = [&](auto step) {
-        step(std::integral_constant<int, 0>{});
-        step(std::integral_constant<int, 1>{});
-    };
-    while (t < q0 / kTile) round(whole);
-    round(last);
+    constexpr std::integral_constant<int, 0> kFirst{};
+    constexpr std::integral_constant<int, 1> kSecond{};
+    while (t < full) {
+        whole(kFirst);
+        whole(kSecond);
+    }
+    last(kFirst);
+    last(kSecond);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     __syncthreads();
 
     if (left_out) {
         // values of the tokens that only some rows see, once more: an infinity or a NaN goes to the rows that see it
-        for (int key = q0; key < most; ++key) {
+        for (int key = full * kTile; key < most; ++key) {
             const _Float16* v = reinterpret_cast<const _Float16*>(vbase) + int64_t(key) * a.v.token;
 #pragma unroll
             for (int d = 0; d < DT; ++d)
@@ -408,7 +410,7 @@ __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(Promp
     __shared__ int strange[R];                               // whether values that only some of the rows see hold an infinity or a NaN
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5, rw = wave % R, kw = wave / R;
-    const Where at = where(a, 32 * R);
+    const Where at = where(a, 32 * R, a.q_heads);
     if (at.seq < 0) return;
     const Span sp = span(a.b, at.seq);
     const int n = __builtin_amdgcn_readfirstlane(sp.n), first = __builtin_amdgcn_readfirstlane(sp.first), h = at.head, g = h / a.group;
@@ -582,21 +584,36 @@ __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(Promp
 hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
 {
     const auto grid = [&](int rows) { return (a.b.start ? a.b.tokens / rows + a.b.seqs : a.b.seqs) * a.q_heads; };
-    const unsigned small = unsigned(grid(64)), large = unsigned(grid(128));
+    const unsigned small = unsigned(grid(64));
     // about as many of 64 rows have work
     const int64_t busy = a.b.start ? (a.b.tokens + 32 * int64_t(a.b.seqs)) / 64 * a.q_heads : small;
-    if (a.b.tokens <= 40 * int64_t(a.b.seqs) || (a.b.tokens <= 80 * int64_t(a.b.seqs) && busy > 1024)) {
-        // Sequences that mostly need no more than 64 rows, and no split of their keys.  34 of 2 tokens with 32 heads of 128: 19 us with 128 rows, 11 with 64; 200 of 10 on average: 79 and 42;
-        // 60 of 64: 33 and 28, but 8 of 64, which all fit at once, 7.6 and 10; 60 of 96: 44 and 45.
-        if (a.dim <= 64) narrow_kernel<64, 1><<<small, 128, 0, s>>>(a);
-        else narrow_kernel<128, 1><<<small, 128, 0, s>>>(a);
-    } else if (busy <= (a.dim <= 64 ? 512 : 256)) {
+    const auto heads_together = [&](auto n) {
+        constexpr int N = decltype(n)::value;
+        const unsigned groups = unsigned(grid(128 / N) / N);
+        if (a.dim <= 64) prompt_kernel<64, N><<<groups, 256, 0, s>>>(a);
+        else prompt_kernel<128, N><<<groups, 256, 0, s>>>(a);
+    };
+    const bool brief = a.b.tokens <= 40 * int64_t(a.b.seqs) || (a.b.tokens <= 80 * int64_t(a.b.seqs) && busy > 1024);
+    if (!brief && busy <= (a.dim <= 64 ? 512 : 256)) {
         // All fit on the chip at once, two to a compute unit or one.  One head of 64, 14587 tokens: 198 us with 128 rows and all their keys, 97 with 64 rows and keys dealt to four waves;
         // 8 heads of 128, 2048 tokens: 40 and 29.  With 16 heads of 128, twice as many as fit: 42 and 46.
         if (a.dim <= 64) narrow_kernel<64, 4><<<small, 512, 0, s>>>(a);
         else narrow_kernel<128, 4><<<small, 512, 0, s>>>(a);
-    } else if (a.dim <= 64) prompt_kernel<64><<<large, 256, 0, s>>>(a);
-    else prompt_kernel<128><<<large, 256, 0, s>>>(a);
+    } else if (a.group % 4 == 0 && !(brief && busy <= 128)) {
+        // 60 of up to 200 tokens with 32 heads of 64 on 8 33.8 us with 128 rows of one head, 25.0 with 32 of four; 60 of 96 with heads of 128 44 and 35; 200 of 10 on average 79, with 64 rows
+        // of one head 43, 31 with 32 of four; 11 of up to 1500 with heads of 64 66 and 63; one of 16384 2.06 ms both ways.
+        // One of 12 with 8 heads of 64 on one 5.2 us, 4.6 with 64 rows of one head
+        heads_together(std::integral_constant<int, 4>{});
+    } else if (brief) {
+        // Sequences that mostly need no more than 64 rows, and no split of their keys, also where two heads share them (200 of 5 with 32 heads of 128 on 16 39 us, 44 with 64 rows of two).
+        // 34 of 2 with 32 heads of 128: 19 us with 128 rows, 11 with 64; 8 of 64, which all fit at once, 7.6 and 10; 60 of 96 44 and 45
+        if (a.dim <= 64) narrow_kernel<64, 1><<<small, 128, 0, s>>>(a);
+        else narrow_kernel<128, 1><<<small, 128, 0, s>>>(a);
+    } else if (a.group % 2 == 0) {
+        heads_together(std::integral_constant<int, 2>{});
+    } else {
+        heads_together(std::integral_constant<int, 1>{});
+    }
     return hipGetLastError();
 }
 

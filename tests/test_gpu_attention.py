@@ -583,6 +583,42 @@ def test_prompt_kinds_of_calls(call, D):
 
 
 @pytest.mark.parametrize("call", KINDS_OF_CALL)
+@pytest.mark.parametrize("D", [128, 64, 80])
+@pytest.mark.parametrize("group", [2, 3, 4, 12])
+def test_prompt_heads_that_share_keys(call, D, group):
+    n, H = KINDS_OF_CALL[call]
+    rng = np.random.default_rng(D + group)
+    st = starts(*n)
+    H = 24 if H == 3 else H // 24 * 24 + 24                 # from 24 heads on a call of few rows has many
+    q, k, v = f16(rng, st[-1], H, D, scale=2.0), f16(rng, st[-1], H // group, D), f16(rng, st[-1], H // group, D)
+    got = prompt(q, k, v, st, D ** -0.5, extra=3)
+    check_prompt(q, k, v, st, got, D ** -0.5, some_rows(rng, st, 10))
+    assert np.array_equal(got, prompt(q, k, v, st, D ** -0.5))
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
+@pytest.mark.parametrize("group", [2, 4])
+def test_prompt_heads_that_share_keys_show_nothing_unseen(call, group):
+    n, H = KINDS_OF_CALL[call]
+    rng = np.random.default_rng(33)
+    st = starts(*n)
+    H = 24 if H == 3 else H // 24 * 24 + 24
+    q, k, v = f16(rng, st[-1], H, 64), f16(rng, st[-1], H // group, 64), f16(rng, st[-1], H // group, 64)
+    clean = prompt(q, k, v, st, 0.1)
+    longest = int(np.argmax(np.diff(st)))
+    first, end = int(st[longest]), int(st[longest + 1])
+    for at in (first, (first + end) // 2, end - 1):
+        touched = np.zeros(clean.shape, bool)
+        touched[at:end, group:2 * group, 17] = True
+        for what in (np.nan, np.inf):
+            v2 = v.copy()
+            v2[at, 1, 17] = what
+            got = prompt(q, k, v2, st, 0.1)
+            assert np.array_equal(got[~touched], clean[~touched]), at
+            assert (np.isnan(got[touched]) if np.isnan(what) else got[touched] == what).all(), at
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
 @pytest.mark.parametrize("what", [np.nan, np.inf, -np.inf])
 def test_prompt_kinds_of_calls_show_nothing_unseen(call, what):
     n, H = KINDS_OF_CALL[call]
