@@ -1,6 +1,6 @@
 // Causal attention over packed prompts.
 //
-// A workgroup takes 32 * NW query rows of one head, a wave 32 of them, and walks the keys 64 at a time.  Keys and values go to LDS
+// A workgroup takes 128 query rows, a wave 32 of them, and walks the keys 64 at a time.  Keys and values go to LDS
 // by LDS-DMA (no registers), the next tile's while this one is worked on.  Products are v_mfma_f32_32x32x16_f16:
 //   scores  S^T = K Q^T: A = keys from LDS, B = queries, which stay in registers.  Lane (column q, half h) receives the scores of its query
 //           with keys 8 i + 4 h .. + 3, which packed to fp16 are the B operand of the second product as they stand
@@ -12,7 +12,7 @@
 // Bound: the matrix pipes and, beside them, the softmax's vector instructions; two workgroups on a CU, so that one's products run beside the other's softmax.
 // Rounding: scores, statistics and sums in 32 bits; weights become fp16 (2^-11 of each) for the second product, and their sum is of the rounded ones, so that weights add up to 1.
 // Measured: 16384 tokens, 32 heads of 128 on 8 key heads 2.01 to 2.16 ms from card to card, 1.02 to 1.09 PFLOP/s: the matrix pipes are busy 61 % of the time and the chip's power sets the clock (1.75 GHz; the same
-// on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 54 to 58 us.
+// on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 57 us.
 #include "tl_attn.hpp"
 
 #include <type_traits>
