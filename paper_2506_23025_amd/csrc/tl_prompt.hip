@@ -12,7 +12,7 @@
 // Bound: the matrix pipes and, beside them, the softmax's vector instructions; two workgroups on a CU, so that one's products run beside the other's softmax.
 // Rounding: scores, statistics and sums in 32 bits; weights become fp16 (2^-11 of each) for the second product, and their sum is of the rounded ones, so that weights add up to 1.
 // Measured: 16384 tokens, 32 heads of 128 on 8 key heads 2.01 to 2.16 ms from card to card, 1.02 to 1.09 PFLOP/s: the matrix pipes are busy 61 % of the time and the chip's power sets the clock (1.75 GHz; the same
-// on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 57 us.
+// on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 55 to 57 us.
 #include "tl_attn.hpp"
 
 #include <type_traits>
@@ -54,8 +54,8 @@ __device__ inline int piece(int r, int c)
 }
 
 // Blocks of `rows` query rows of all sequences (64 at most), those with most keys before others: the one in that place.  What is heavy begins early, so that the chip is
-// full until the end; where all fit at once, two to a compute unit, the second half comes in the opposite order, so that a heavy one shares its unit with a light one.
-__device__ inline Item nth_longest(const PromptArgs& a, int rows, int heads, int place)
+// full until the end; with `two` to a compute unit, where all fit at once, the second half comes in the opposite order, so that a heavy one shares its unit with a light one.
+__device__ inline Item nth_longest(const PromptArgs& a, int rows, int heads, bool two, int place)
 {
     const int lane = threadIdx.x & 63;
     const int n = lane < a.b.seqs ? span(a.b, lane).n : 0, blocks = (n + rows - 1) / rows;
@@ -65,7 +65,7 @@ __device__ inline Item nth_longest(const PromptArgs& a, int rows, int heads, int
     const int all = from(0);
     if (place >= all) return {-1, 0};
     const int half = 256 / heads;
-    if (int64_t(all) * heads <= 512 && place >= half) place = all - 1 - (place - half);
+    if (two && int64_t(all) * heads <= 512 && place >= half) place = all - 1 - (place - half);
     if (a.b.seqs == 1) return {0, all - 1 - place};
     // the largest number j with more than `place` blocks from j on
     int lo = 0, hi = 1;
@@ -83,13 +83,13 @@ __device__ inline Item nth_longest(const PromptArgs& a, int rows, int heads, int
 
 // What a workgroup takes: a block of `rows` query rows of a sequence, and one of `heads` heads or groups of heads.
 struct Where { int seq, block, head; };
-__device__ inline Where where(const PromptArgs& a, int rows, int heads)
+__device__ inline Where where(const PromptArgs& a, int rows, int heads, bool two)
 {
     // heads that share keys go to one chiplet (workgroups are dealt to the 8 of them in turn); the rows with most keys first
     int h = int(blockIdx.x) % heads;
     const int place = int(blockIdx.x) / heads, places = int(gridDim.x) / heads;
     Item it{places - 1 - place, 0};
-    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, rows, heads, place);
+    if (a.b.start && a.b.seqs <= 64) it = nth_longest(a, rows, heads, two, place);
     else if (a.b.start) it = find_item(a.b, places - 1 - place, rows, 1);
     if (heads % 8 == 0) h = (h & 7) * (heads >> 3) + (h >> 3);
     return {__builtin_amdgcn_readfirstlane(it.seq), __builtin_amdgcn_readfirstlane(it.i), h};
@@ -129,7 +129,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5;
 
-    const Where where_ = where(a, kRows, a.q_heads / HEADS);
+    const Where where_ = where(a, kRows, a.q_heads / HEADS, true);
     const int seq = where_.seq, h = where_.head * HEADS + wave % HEADS;
     if (seq < 0) return;
     const Span sp = span(a.b, seq);
@@ -410,7 +410,7 @@ __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(Promp
     __shared__ int strange[R];                               // whether values that only some of the rows see hold an infinity or a NaN
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int l32 = lane & 31, half = lane >> 5, rw = wave % R, kw = wave / R;
-    const Where at = where(a, 32 * R, a.q_heads);
+    const Where at = where(a, 32 * R, a.q_heads, DP == 64);
     if (at.seq < 0) return;
     const Span sp = span(a.b, at.seq);
     const int n = __builtin_amdgcn_readfirstlane(sp.n), first = __builtin_amdgcn_readfirstlane(sp.first), h = at.head, g = h / a.group;
@@ -594,9 +594,11 @@ hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
         else prompt_kernel<128, N><<<groups, 256, 0, s>>>(a);
     };
     const bool brief = a.b.tokens <= 40 * int64_t(a.b.seqs) || (a.b.tokens <= 80 * int64_t(a.b.seqs) && busy > 1024);
-    if (!brief && busy <= (a.dim <= 64 ? 512 : 256)) {
-        // All fit on the chip at once, two to a compute unit or one.  One head of 64, 14587 tokens: 198 us with 128 rows and all their keys, 97 with 64 rows and keys dealt to four waves;
-        // 8 heads of 128, 2048 tokens: 40 and 29.  With 16 heads of 128, twice as many as fit: 42 and 46.
+    const bool lengthy = a.b.tokens >= 1500 * int64_t(a.b.seqs);
+    if (!brief && busy <= (a.dim <= 64 ? 512 : 256) * (lengthy ? 2 : 1)) {
+        // All fit on the chip at once, two to a compute unit or one, or where sequences are long half of them: the second half goes where the shorter ones of the first have been, and 128 rows
+        // with all their keys leave a unit alone with one for long.  One head of 64, 14587 tokens: 198 us with 128 rows, 97 with 64 rows and keys dealt to four waves; 8 heads of 128, 2048
+        // tokens 40 and 29, 4096 75 and 67; 4 heads, 8000 133 and 109; but 16 heads, 3000 59 and 75, and 32 heads, 1024 25 and 27.
         if (a.dim <= 64) narrow_kernel<64, 4><<<small, 512, 0, s>>>(a);
         else narrow_kernel<128, 4><<<small, 512, 0, s>>>(a);
     } else if (a.group % 4 == 0 && !(brief && busy <= 128)) {

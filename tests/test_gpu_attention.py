@@ -496,6 +496,16 @@ def test_prompt_long(n, H, HK, D):
     assert np.array_equal(got, prompt(q, k, v, [0, n], D ** -0.5))
 
 
+@pytest.mark.parametrize("n,H,HK,D", [((4200,), 6, 3, 128), ((3900, 0, 1000, 130), 12, 12, 64), ((4200,), 6, 6, 80), ((2500, 2500, 1), 5, 1, 112)])
+def test_prompt_long_with_few_heads(n, H, HK, D):
+    rng = np.random.default_rng(n[0] + D)
+    st = starts(*n)
+    q, k, v = f16(rng, st[-1], H, D, scale=2.0), f16(rng, st[-1], HK, D), f16(rng, st[-1], HK, D)
+    got = prompt(q, k, v, st, D ** -0.5)
+    check_prompt(q, k, v, st, got, D ** -0.5, some_rows(rng, st, 30))
+    assert np.array_equal(got, prompt(q, k, v, st, D ** -0.5))
+
+
 def test_prompt_of_one_token_each_gives_the_values():
     rng = np.random.default_rng(14)
     q, k, v = f16(rng, 70, 4, 128), f16(rng, 70, 2, 128), f16(rng, 70, 2, 128)
