@@ -13,7 +13,7 @@
 // Bound: memory.  Short caches: a workgroup takes a row tile, its waves deal the tiles among themselves and join their sums in LDS.  Otherwise the tiles of the whole
 // call stand in one row, sequence after sequence, and every wave of a grid that fills the chip once takes an equal piece of it, whatever the sequences' lengths; they are
 // read on the device, so one captured launch serves every step.  Pieces of row tiles that several waves share meet in a second kernel.
-// Measured: 3 sequences of up to 131072 tokens, 32 heads of 128 on 8 key heads, int8 98 us (5.85 TB/s); 48 of up to 4096, e4m3 47.5 us (5.05 TB/s, 42 of them here and 5 in the second
+// Measured: 3 sequences of up to 131072 tokens, 32 heads of 128 on 8 key heads, int8 97 us (5.9 TB/s); 48 of up to 4096, e4m3 47.5 us (5.05 TB/s, 42 of them here and 5 in the second
 // kernel); 16 of up to 2047 with 32 key heads 32 us (4.3 TB/s).  One sequence of 700 tokens with 16 heads 6.8 us, a chain of reads: lengths, pages, scales, codes.
 #include "tl_attn.hpp"
 
@@ -25,7 +25,7 @@ namespace {
 
 constexpr int kWaves = 4;
 constexpr int kWavesAll = 2048;           // waves that share a call's tiles: two on each SIMD of 256 CUs, or one where a row tile is of 32 rows
-constexpr int kFewRows = 1024;            // up to so many rows a workgroup joins the parts of each, beyond a wave
+constexpr int kFewRows = 1024;            // up to so many rows a workgroup joins the parts of each, of 8 waves up to a quarter of it; beyond a wave
 
 constexpr float kInf = __builtin_inff();
 constexpr float kSlack = 8.0f;            // log2 of how far a weight may pass its reference (fp16 holds 2^15)
@@ -599,11 +599,11 @@ __global__ __launch_bounds__(64 * kWaves, CH * NR > 8 ? 1 : 2) void piece_kernel
     }
 }
 
-// Joins the pieces of row tiles that several waves share.  A row is a wave's, or the four waves' of a workgroup (W = 4) where there are so few rows that the
+// Joins the pieces of row tiles that several waves share.  A row is a wave's, or of W = 4 or 8 of a workgroup where there are so few rows that the
 // parts of each are worth dealing out.  Four dimensions are a lane's, and the parts go round among the lanes that have the same ones; the sums of the first
 // are asked for before it is known how they weigh.
 template <int CH, int W>
-__global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p)
+__global__ __launch_bounds__(64 * (W == 1 ? kWaves : W)) void join_kernel(CachedArgs a, Shape p)
 {
     constexpr int DP = CH * 16, kQuads = DP / 4, kGroups = 64 * W / kQuads, kAhead = 8;
     const int lane = threadIdx.x & 63, wave = same(threadIdx.x >> 6);
@@ -640,13 +640,13 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p
     float M = stat[0];
     for (int c = tid + 64 * W; c < parts; c += 64 * W) M = fmaxf(M, row_of(c)[DP]);
     for (int k = 32; k; k >>= 1) M = fmaxf(M, __shfl_xor(M, k));
-    __shared__ float most[kWaves], total[kWaves];
-    __shared__ f32x4 sums[W == 1 ? 1 : kWaves][kQuads];
+    __shared__ float most[W], total[W];
+    __shared__ f32x4 sums[W][kQuads];
     if constexpr (W > 1) {
         if (lane == 0) most[wave] = M;
         __syncthreads();
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) M = fmaxf(M, most[v]);
+        for (int v = 0; v < W; ++v) M = fmaxf(M, most[v]);
     }
     M = finite(M);
     float L = 0.0f;
@@ -677,7 +677,7 @@ __global__ __launch_bounds__(64 * kWaves) void join_kernel(CachedArgs a, Shape p
         L = 0.0f;
         x = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int v = 0; v < kWaves; ++v) {
+        for (int v = 0; v < W; ++v) {
             L += total[v];
             x += sums[v][quad];
         }
@@ -720,7 +720,11 @@ hipError_t launch(const CachedArgs& a, const Shape& p, bool alone, int64_t longe
     piece_kernel<FP8, CH, EXACT, NR><<<unsigned((p.pieces * p.ys + kWaves - 1) / kWaves), 64 * kWaves, 0, s>>>(a, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.tiles * p.ys * p.rows <= kFewRows) join_kernel<CH, kWaves><<<dim3(unsigned(p.tiles), y, unsigned(p.rows)), 64 * kWaves, 0, s>>>(a, p);
+    // Waves for a row: one token over 23827, 3 heads (up to 373 parts a row) 16.7 us with four, 14.4 with eight, 14.2 with sixteen; 3 over up to 131072, 32 heads 98.4, 96.9 and 97; 24 over
+    // up to 2500, 16 heads on 2 10.8 and 11.7; 128 over up to 4000, 32 heads 116 with one and four
+    const int64_t all_rows = p.tiles * p.ys * p.rows;
+    if (all_rows <= kFewRows / 4) join_kernel<CH, 2 * kWaves><<<dim3(unsigned(p.tiles), y, unsigned(p.rows)), 64 * 2 * kWaves, 0, s>>>(a, p);
+    else if (all_rows <= kFewRows) join_kernel<CH, kWaves><<<dim3(unsigned(p.tiles), y, unsigned(p.rows)), 64 * kWaves, 0, s>>>(a, p);
     else join_kernel<CH, 1><<<dim3(unsigned(p.tiles), y, unsigned((p.rows + kWaves - 1) / kWaves)), 64 * kWaves, 0, s>>>(a, p);
     return hipGetLastError();
 }
