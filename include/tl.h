@@ -397,6 +397,7 @@ tl_status tl_kv_append(const tl_append_job* job, void* stream);
  *     out[t][h] = sum_p softmax_p(scale * q[t][h] . k[p][g]) v[p][g],   g = h / (q_heads / kv_heads).
  * A query that sees no position (all its pages missing) gives 0.  A block whose scale is NaN makes NaN of every query that sees a token of it, and of no other.
  *   q, out      q_heads heads of cache->head_dim dimensions; out may be q itself with the same strides, and may not overlap it otherwise
+ *   scale       any sign; TL_ERR_VALUE where scale * log2(e) is not finite in fp32
  *   longest     an upper bound of cached[s] + the tokens of s over all sequences, 0 if not known: it spares the second
  *               launch that joins the parts of long sequences where none can be cut in parts.  Results are right also where it is exceeded
  *   workspace   device, 16-byte aligned, tl_attn_cached_workspace bytes at least; written and read within the call alone
@@ -420,7 +421,7 @@ tl_status tl_attn_cached(const tl_cached_job* job, void* stream);
  * Attention of whole prompts, causal: token i of a sequence sees tokens 0 .. i of the same sequence among this call's rows
  * (batch.cached is not read), with fp16 keys and values:
  *     out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j][g]) v[j][g],   g = h / (q_heads / kv_heads).
- * head_dim is a multiple of 16 up to 128; (seqs + tokens / 32) * q_heads is below 2^24.  An infinity or a NaN in a key or value shows in the tokens that see it and in no others.  out may be
+ * head_dim is a multiple of 16 up to 128; (seqs + tokens / 32) * q_heads is below 2^24; scale as in tl_cached_job.  An infinity or a NaN in a key or value shows in the tokens that see it and in no others.  out may be
  * q itself with the same strides, and may not overlap q, k or v otherwise.  Deterministic.
  */
 typedef struct tl_prompt_job {

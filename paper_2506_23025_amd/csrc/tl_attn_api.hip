@@ -50,7 +50,7 @@ inline tl_status cache_status(const tl_kv_cache& c)
     if (c.kv_heads < 1 || c.kv_heads > kMaxHeads || !dim_ok(c.head_dim)) return TL_ERR_SHAPE;
     const int64_t lim = int64_t(1) << 31;
     if (c.page_tokens < 16 || c.page_tokens > 1024 || (c.page_tokens & (c.page_tokens - 1))) return TL_ERR_SHAPE;
-    if (c.pages < 1 || c.pages >= lim || c.pages_per_seq < 1 || c.pages_per_seq * c.page_tokens >= lim) return TL_ERR_SHAPE;
+    if (c.pages < 1 || c.pages >= lim || c.pages_per_seq < 1 || c.pages_per_seq > (lim - 1) / c.page_tokens) return TL_ERR_SHAPE;
     if (!aligned(c.k, 16) || !aligned(c.v, 16) || !aligned(c.k_scale, 4) || !aligned(c.v_scale, 4) || !aligned(c.page_table, 4)) return TL_ERR_ALIGN;
     return TL_OK;
 }
@@ -159,7 +159,7 @@ tl_status tl_attn_cached(const tl_cached_job* job, void* stream)
     if (e != TL_OK || (e = cache_status(*j.cache)) != TL_OK) return e;
     if ((e = heads_number_status(j.q_heads, j.cache->kv_heads)) != TL_OK) return e;
     if (j.longest < 0) return TL_ERR_SHAPE;
-    if (!std::isfinite(j.scale)) return TL_ERR_VALUE;
+    if (!std::isfinite(j.scale * kLog2e)) return TL_ERR_VALUE;
     if ((e = heads_status(j.q, j.q_heads)) != TL_OK || (e = heads_status(j.out, j.q_heads)) != TL_OK) return e;
     if (!j.workspace) return TL_ERR_NULL;
     if (!aligned(j.workspace, 16)) return TL_ERR_ALIGN;
@@ -179,7 +179,7 @@ tl_status tl_attn_prompt(const tl_prompt_job* job, void* stream)
     if (e != TL_OK || (e = heads_number_status(j.q_heads, j.kv_heads)) != TL_OK) return e;
     if (!dim_ok(j.head_dim)) return TL_ERR_SHAPE;
     if ((j.batch.seqs + j.batch.tokens / 32) * j.q_heads >= kMaxGroups) return TL_ERR_SHAPE;
-    if (!std::isfinite(j.scale)) return TL_ERR_VALUE;
+    if (!std::isfinite(j.scale * kLog2e)) return TL_ERR_VALUE;
     if ((e = heads_status(j.q, j.q_heads)) != TL_OK || (e = heads_status(j.k, j.kv_heads)) != TL_OK || (e = heads_status(j.v, j.kv_heads)) != TL_OK ||
         (e = heads_status(j.out, j.q_heads)) != TL_OK) return e;
     if (j.batch.tokens == 0) return TL_OK;

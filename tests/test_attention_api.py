@@ -175,3 +175,15 @@ def test_binding_looks_at_tensors_before_it_takes_their_addresses():
         tl.make_batch(None, torch.zeros(2, dtype=torch.int32), 2, 2)           # on the host
     with pytest.raises(tl.TlError):
         tl.tl_rope_table(4, 3)
+
+
+def test_numbers_at_the_ends_of_their_ranges():
+    """Sizes whose products would not fit 64 bits, and a scale that overflows on its way to powers of 2."""
+    for pages in (1 << 59, (1 << 63) - 1, (1 << 31) // 64):
+        assert cached(c=cache(pages_per_seq=pages)) == append(c=cache(pages_per_seq=pages)) == tl.TL_ERR_SHAPE, pages
+    assert cached(c=cache(pages_per_seq=(1 << 31) // 64 - 1)) == tl.TL_OK
+    assert cached(scale=3e38) == prompt(scale=-3e38) == tl.TL_ERR_VALUE
+    assert cached(scale=2e38) == prompt(scale=2e38) == tl.TL_OK
+    for big in (1 << 62, (1 << 63) - 1):
+        assert prompt(b=batch(seqs=big)) == prompt(b=batch(tokens=big)) == tl.TL_ERR_SHAPE
+        assert tl.raw().tl_attn_cached_workspace(big, 1, 4, 2, 128) == tl.raw().tl_attn_cached_workspace(1, 1, big, big, 128) == 0
