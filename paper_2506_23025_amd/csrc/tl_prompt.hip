@@ -396,8 +396,8 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
 
 // The same for 64 query rows a workgroup, 32 a wave, S waves for each of them, which deal tiles of 32 keys among themselves and join their sums in LDS at the end: for few rows
 // with many keys (S = 4), where workgroups of 128 rows with all their keys leave most of the chip idle, and for many sequences of a few tokens (S = 1), where they are idle themselves.
-// Bound: with heads of 64 a round (64 rows, 128 keys) takes 0.80 us, 0.58 of it without the transfers and 0.60 without the products: the one barrier a round lets them overlap little,
-// and more rounds in LDS ahead did not help.  Measured: one head of 64, 14587 tokens 97 us; 8 of 128, 2048 tokens 29 us.
+// Bound: with heads of 64 a round (64 rows, 128 keys) takes 0.77 us, 0.58 of it without the transfers and 0.60 without the products: the one barrier a round lets them overlap little,
+// and more rounds in LDS ahead did not help.  Measured: one head of 64, 14587 tokens 92 us; 8 of 128, 2048 tokens 29 us.
 template <int DP, int S>
 __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(PromptArgs a)
 {
@@ -469,6 +469,9 @@ __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(Promp
         for (int i = 0; i < 16; ++i) s[i] = 0.0f;
 #pragma unroll
         for (int k = 0; k < KK; ++k) s = __builtin_amdgcn_mfma_f32_32x32x16_f16(*(const lds_f16x8*)(ka[k] + AT), q[k], s, 0, 0, 0);
+        // all reads before the products: 97 us for the one head, 92
+        __builtin_amdgcn_sched_group_barrier(0x100, KK, 0);
+        __builtin_amdgcn_sched_group_barrier(0x8, KK, 0);
         bool odd = false;
         if (t == own) {
 #pragma unroll
@@ -597,8 +600,8 @@ hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
     const bool lengthy = a.b.tokens >= 1500 * int64_t(a.b.seqs);
     if (!brief && busy <= (a.dim <= 64 ? 512 : 256) * (lengthy ? 2 : 1)) {
         // All fit on the chip at once, two to a compute unit or one, or where sequences are long half of them: the second half goes where the shorter ones of the first have been, and 128 rows
-        // with all their keys leave a unit alone with one for long.  One head of 64, 14587 tokens: 198 us with 128 rows, 97 with 64 rows and keys dealt to four waves; 8 heads of 128, 2048
-        // tokens 40 and 29, 4096 75 and 67; 4 heads, 8000 133 and 109; but 16 heads, 3000 59 and 75, and 32 heads, 1024 25 and 27.
+        // with all their keys leave a unit alone with one for long.  One head of 64, 14587 tokens: 198 us with 128 rows, 92 with 64 rows and keys dealt to four waves; 8 heads of 128, 2048
+        // tokens 40 and 29, 4096 75 and 66; 4 heads, 8000 133 and 109; but 16 heads, 3000 59 and 75, and 32 heads, 1024 25 and 27.
         if (a.dim <= 64) narrow_kernel<64, 4><<<small, 512, 0, s>>>(a);
         else narrow_kernel<128, 4><<<small, 512, 0, s>>>(a);
     } else if (a.group % 4 == 0 && !(brief && busy <= 128)) {
