@@ -406,8 +406,22 @@ struct Walk {
                     w[n][1] = c.v[1];
                 }
             };
-            if (masked) weigh(std::true_type{});
-            else weigh(std::false_type{});
+            if (masked) {
+                weigh(std::true_type{});
+                // A weight of 0 does not take a NaN out of a sum, and bytes that no token of the sequence was written to, or those read in place of a page that is missing, may be codes
+                // that stand for one (whole numbers have none): they become 0.
+                if constexpr (FP8) {
+                    const int64_t x = most - int64_t(tile) * 64 - g * 16;
+                    const int held = !inside || x < 0 ? 0 : x > 16 ? 16 : int(x);
+                    u32x4 keep;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) keep[i] = held >= 4 * i + 4 ? ~0u : held > 4 * i ? (1u << (held - 4 * i) * 8) - 1 : 0u;
+#pragma unroll
+                    for (int d = 0; d < CH; ++d) vw[d] &= keep;
+                }
+            } else {
+                weigh(std::false_type{});
+            }
 #pragma unroll
             for (int d = 0; d < CH; ++d) {
                 const f16x8 v0 = widen<FP8>(vw[d][0], vw[d][1]), v1 = widen<FP8>(vw[d][2], vw[d][3]);

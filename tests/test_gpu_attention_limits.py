@@ -1,0 +1,95 @@
+"""The attention part where its promises end: memory that nobody wrote, numbers at the ends of their ranges, lengths beyond the pages, calls of no tokens."""
+import numpy as np
+import pytest
+
+import attention as ref
+import paper_2506_23025_amd as tl
+from parity import to_dev
+from test_gpu_attention import KINDS, Setup, blank, cached, check_cached, f16, on, some_of, taken
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- memory that nobody wrote ------------------------------------------------------------------
+
+def fill(st):
+    """Brings the device's codes and scales in line with the twin's."""
+    for n, codes, scale in (("k", st.kd, st.ksd), ("v", st.vd, st.vsd)):
+        codes.copy_(to_dev(ref.to_layout(st.cache.codes[n], n == "k").reshape(tuple(codes.shape))))
+        scale.copy_(to_dev(st.cache.scale[n]))
+
+
+def leave_page_0(st):
+    """Page 0, which stands in for pages that are missing, belongs to no sequence."""
+    free = next(p for p in range(st.cache.pages) if not (st.table == p).any())
+    for d in (st.cache.codes, st.cache.scale):
+        for n in "kv":
+            d[n][free] = d[n][0]
+    st.table[st.table == 0] = free
+    st.td.copy_(to_dev(st.table))
+
+
+def spoil(st, byte):
+    """Every code that no token of a sequence was written to."""
+    written = np.zeros((st.cache.pages, st.cache.page), bool)
+    for s, (n, p) in enumerate(zip(st.new, st.past)):
+        for at in range(int(p + n) if p >= 0 else 0):
+            page = st.cache.page_of(st.table, s, at)
+            if page >= 0:
+                written[page, at % st.cache.page] = True
+    w = written.reshape(st.cache.pages, 1, st.cache.page // 16, 16)
+    for n in "kv":
+        c = st.cache.codes[n]
+        c[np.broadcast_to(~w, c.shape[:-1])] = byte
+    fill(st)
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("call", ["one", "several", "many", "many of several"])
+def test_cached_codes_that_nobody_wrote_do_not_show(kind, D, call):
+    """Ends inside a block, a tile and a page, pages that are missing, every kernel: the bits are those of a cache of zeros."""
+    rng = np.random.default_rng(51)
+    new, past, H, HK = {"one": (np.ones(8, int), np.array([0, 5, 15, 16, 62, 200, 700, -1]), 8, 2), "several": (np.array([5, 1, 70, 0, 33, 3]), np.array([0, 3, 61, 9, 250, -1]), 8, 2),
+                        "many": (np.ones(75, int), rng.integers(0, 120, 75), 32, 16), "many of several": (rng.integers(1, 18, 75), rng.integers(0, 120, 75), 32, 16)}[call]
+    st = Setup(52, new, past, H, HK, D, 32, kind, more_pages=3, missing=((2, 0), (4, 1), (5, 0)))
+    leave_page_0(st)
+    q = f16(rng, st.T, H, D)
+    rows = some_of(rng, st, 20)
+    spoil(st, 0)
+    clean = {longest: cached(st, q, D ** -0.5, longest=longest) for longest in (None, 0)}
+    for byte in (0x7f, 0xff):
+        spoil(st, byte)
+        for longest, want in clean.items():
+            got = cached(st, q, D ** -0.5, longest=longest)
+            assert np.isfinite(got).all(), (byte, longest)
+            assert np.array_equal(got, want), (byte, longest)
+    check_cached(st, q, got, D ** -0.5, rows)
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [1, 17, 30, 65]])
+def test_a_cache_of_unset_memory(kind, new):
+    """First tokens into pages of any bytes and scales, then attention over them: as with pages of zeros."""
+    import torch
+    rng = np.random.default_rng(53)
+    H, HK, D, page = 4, 2, 64, 32
+    T, S = sum(new), len(new)
+    q, k, v = f16(rng, T, H, D), f16(rng, T, HK, D), f16(rng, T, HK, D)
+    start, none = to_dev(np.concatenate([[0], np.cumsum(new)]).astype(np.int32)), to_dev(np.zeros(S, np.int32))
+    table = to_dev(np.concatenate([[[-1, -1, -1]], 1 + np.arange(3 * S - 3).reshape(-1, 3)]).astype(np.int32))       # the first has no pages
+    outs = []
+    for byte, scale in ((0, 0.0), (0x7f, np.nan), (0xff, np.inf)):
+        kd, vd = (torch.full((3 * S, HK, page * D), byte, dtype=torch.uint8, device="cuda") for _ in range(2))
+        ks, vs = (torch.full((3 * S, HK, page // 16), scale, dtype=torch.float32, device="cuda") for _ in range(2))
+        handle = tl.make_kv_cache(kd, vd, ks, vs, table, page, D, KINDS[kind])
+        batch = tl.make_batch(None if T == S else start, none, S, T)
+        tl.tl_kv_append(tl.make_append_job(None, on(k), on(v), None, None, batch, handle))
+        for longest in (65, 0):
+            out = blank(T, H, D)
+            space = torch.empty(tl.tl_attn_cached_workspace(S, T, H, HK, D), dtype=torch.uint8, device="cuda")
+            tl.tl_attn_cached(tl.make_cached_job(on(q), out, batch, handle, 0.125, longest, space))
+            outs.append(taken(out).copy())
+    for got, want in zip(outs, outs[:2] * 3):
+        assert np.isfinite(got).all() and np.array_equal(got, want)
+    assert (outs[0][0] == 0).all() and (outs[0][1:] != 0).any()
