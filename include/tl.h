@@ -308,8 +308,8 @@ typedef struct tl_batch {
  *                     key's dimension d of token t is byte ((t / 4) * (head_dim / 16) + d / 16) * 64 + (t % 4) * 16 + d % 16, a value's
  *                     (d / 16) * 256 + (d % 16) * 16 + t: the orders in which the matrix instructions take them
  *   k_scale, v_scale  device, fp32 [pages][kv_heads][page_tokens / 16]
- *   page_table        device, int32 [seqs][pages_per_seq].  An entry outside [0, pages) stands for no page: what would
- *                     go there is dropped, and attention does not see it
+ *   page_table        device, int32 [seqs][pages_per_seq].  An entry outside [0, pages) stands for no page, and positions beyond
+ *                     page_tokens * pages_per_seq have none: what would go there is dropped, and attention does not see it
  * Memory of pages need not be set to anything before they are used.  The cache belongs to the caller, and two calls
  * that write or read and write the same page have to be on one stream or ordered by the caller.
  */

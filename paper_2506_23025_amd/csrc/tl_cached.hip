@@ -108,6 +108,9 @@ __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
 __device__ inline float max3(float a, float b, float c) { return fmaxf(fmaxf(a, b), c); }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// Positions that a sequence's pages hold.
+__device__ inline int64_t room(const Cache& c) { return c.pages_per_seq << (c.page_shift + 4); }
+
 // A sequence: its tokens in the call, those before them, and the tiles and row tiles that it needs.
 struct Need {
     int first, n, past, tiles, rts;
@@ -121,8 +124,7 @@ __device__ inline Need need_of(const CachedArgs& a, const Shape& p, int s)
     Need need{sp.first, sp.n, past, 0, 0};
     if (sp.n == 0) return need;
     int64_t len = past < 0 ? 0 : int64_t(past) + sp.n;
-    const int64_t room = a.c.pages_per_seq << (a.c.page_shift + 4);
-    if (len > room) len = room;
+    if (len > room(a.c)) len = room(a.c);
     need.tiles = int((len + 63) >> 6);
     need.rts = p.per == 1 ? sp.n : (sp.n + p.per - 1) / p.per;
     return need;
@@ -234,7 +236,7 @@ template <bool FP8, int CH, bool EXACT, int NR>
 struct Walk {
     static constexpr int J = (CH + 3) / 4;
     f16x8 q[NR][J][2];
-    int64_t sees[NR], least, most;        // positions that this lane's rows see; the fewest and most of the tile
+    int64_t sees[NR], least, most;        // positions that this lane's rows see; the fewest of the tile, and the most, within the pages
     f32x4 o[NR][CH];
     float m[NR], l[NR], R[NR];
     float from[NR];                       // where a score's sum begins: it takes off what the raised keys add
@@ -249,6 +251,7 @@ struct Walk {
         rows = tokens * p.heads;                             // those of heads beyond the group are computed and dropped
         least = past < 0 ? 0 : int64_t(past) + first + 1;
         most = past < 0 ? 0 : int64_t(past) + first + tokens;
+        if (most > room(a.c)) most = room(a.c);              // a length beyond the pages asks for no tiles that cannot be there
 #pragma unroll
         for (int n = 0; n < NR; ++n) {
             // row r is token r / p.heads, head r % p.heads

@@ -93,3 +93,27 @@ def test_a_cache_of_unset_memory(kind, new):
     for got, want in zip(outs, outs[:2] * 3):
         assert np.isfinite(got).all() and np.array_equal(got, want)
     assert (outs[0][0] == 0).all() and (outs[0][1:] != 0).any()
+
+
+# ---- lengths beyond the pages --------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("new", [[1, 1, 1], [5, 1, 40]])
+def test_lengths_beyond_the_pages(kind, new):
+    """What is seen is what the pages hold, and no time goes into places that they cannot hold, however far beyond them a length is."""
+    rng = np.random.default_rng(64)
+    st = Setup(65, new, [150, 40, 300], 4, 2, 64, 32, kind)
+    st.table = np.ascontiguousarray(st.table[:, :3])       # of 96 positions
+    st.td = to_dev(st.table)
+    st.handle = tl.make_kv_cache(st.kd, st.vd, st.ksd, st.vsd, st.td, 32, 64, KINDS[kind])
+    q = f16(rng, st.T, 4, 64)
+    want = {longest: cached(st, q, 0.125, longest=longest) for longest in (96, 0)}
+    check_cached(st, q, want[96], 0.125)
+    for far in (1 << 20, (1 << 31) - 1):
+        st.pastd.copy_(to_dev(np.array([far, 40, far], np.int32)))
+        for longest in (96, 0):
+            assert np.array_equal(cached(st, q, 0.125, longest=longest), want[longest]), (far, longest)
+    k, v = f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64)
+    st.past = np.array([(1 << 31) - 1, 40, 1 << 20])
+    st.pastd.copy_(to_dev(st.past.astype(np.int32)))
+    st.append(q, k, v, tl.tl_rope_table(200, 64), 64, False)      # dropped there, and beyond the table
