@@ -378,6 +378,7 @@ tl_status tl_rope_table(float* table, int64_t positions, int64_t rot_dim, double
  * What goes into the cache is coded from the fp32 rotated key and from the fp16 value.  A block's scale is that of the
  * tokens it holds before the call (0 if it holds none) or, if larger, the call's largest magnitude in it divided by 127 (448); where it grows, the
  * earlier codes are coded anew, round(code * (old scale / new scale)).  Places behind the last token keep what they hold.
+ * A scale below 2^-80 becomes 0, and the call's codes in that block with it.
  * A block that takes a NaN or an infinity gets the scale NaN, and stands for NaN until its first token is written again.
  * Two sequences may not share a page that the call writes.
  */

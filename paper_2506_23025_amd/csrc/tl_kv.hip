@@ -35,7 +35,8 @@ template <bool FP8>
 __device__ inline uint32_t two_codes(float a, float b) { return four_codes<FP8>(a, b, 0.0f, 0.0f) & 0xffffu; }
 
 // Quotients by one number b, rounded as a division rounds them: with the rounded reciprocal, the remainder of the first guess sets it right (Markstein, IBM
-// Journal of Research and Development 34, 1990).  0 for all where b is 0 or NaN.  Magnitudes here stay far from both ends of the range.
+// Journal of Research and Development 34, 1990).  0 for all where b is 0 or NaN.  b is a scale, kSmallest at least and an amax / 127 or / 448: it and its reciprocal
+// are ordinary numbers, and so is the remainder of every quotient that is not coded as 0.
 struct Divide {
     float b, inv;
     bool any;
@@ -166,12 +167,14 @@ __device__ inline void recode(uint8_t* to, int dim, int slots, float ratio, int 
     }
 }
 
-// The scale of a block that takes tokens with magnitudes up to amax (or an infinity or a NaN: odd) and had `was` (0 if it held nothing).
+// The scale of a block that takes tokens with magnitudes up to amax (or an infinity or a NaN: odd) and had `was` (0 if it held nothing).  Rotated keys are coded from
+// 32 bits, and a table of tiny numbers could make a scale whose reciprocal is no number, or that is itself so coarse that a magnitude is more than the top of it.
+constexpr float kSmallest = 0x1p-80f;
 template <bool FP8>
 __device__ inline float scale_of(float was, float amax, bool odd)
 {
     const float now = fmaxf(was, amax / top<FP8>());
-    return odd || !(was == was) ? __builtin_nanf("") : now;
+    return odd || !(was == was) ? __builtin_nanf("") : now < kSmallest ? 0.0f : now;
 }
 
 // One token's codes of 8 dimensions from d on.

@@ -117,3 +117,35 @@ def test_lengths_beyond_the_pages(kind, new):
     st.past = np.array([(1 << 31) - 1, 40, 1 << 20])
     st.pastd.copy_(to_dev(st.past.astype(np.int32)))
     st.append(q, k, v, tl.tl_rope_table(200, 64), 64, False)      # dropped there, and beyond the table
+
+
+# ---- numbers at the ends of their ranges ---------------------------------------------------------
+
+class Bounded(ref.Cache):
+    """Scales below 2^-80 become 0: what the block held stays as it is, and the new codes are 0."""
+
+    def put(self, name, x, table, s, past):
+        was = self.codes[name].copy()
+        super().put(name, x, table, s, past)
+        for b in range(past // 16, (past + len(x) - 1) // 16 + 1):
+            lo, hi = max(past, 16 * b), min(past + len(x), 16 * b + 16)
+            page, blk = self.page_of(table, s, lo), 16 * b % self.page // 16
+            for h in range(self.heads):
+                if self.scale[name][page, h, blk] < 2.0 ** -80:
+                    self.scale[name][page, h, blk] = 0
+                    self.codes[name][page, h, blk] = was[page, h, blk]
+                    self.codes[name][page, h, blk, lo % 16:lo % 16 + hi - lo] = 0
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("new,past", [([1, 1, 1], [0, 5, 31]), ([3, 20, 40], [0, 5, 31])])
+def test_append_scales_at_the_ends_of_their_range(kind, new, past):
+    """Rotated keys are coded from 32 bits, so a table of tiny or large numbers reaches scales whose reciprocals are no numbers."""
+    rng = np.random.default_rng(54)
+    for i, magnitude in enumerate((1e-20, 1e-22, 1e-23, 1e-25, 1e-33, 1e-36, 1e-38, 1e-40, 1e-43, 1e-38, 1e30, 3e37)):
+        st = Setup(55 + i, new, past, 2, 2, 64, 32, kind)
+        st.cache.__class__ = Bounded
+        st.cache.scale["k"] *= np.float32(magnitude * 0.01)
+        fill(st)
+        table = tl.tl_rope_table(80, 64, magnitude=magnitude)
+        st.append(f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), table, 64, i % 2 == 0)
