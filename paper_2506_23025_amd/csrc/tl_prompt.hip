@@ -33,6 +33,8 @@ typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
 
 __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
+// What a row's sums are multiplied by.  Every row sees a key, so its weights add up to 1 at least, unless all its scores are -infinity, whose softmax is 0 / 0.
+__device__ inline float share(float l) { return l > 0.0f ? 1.0f / l : __builtin_nanf(""); }
 
 __device__ inline uint32_t lds_address(const void* p)
 {
@@ -369,7 +371,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
         }
     }
     l += __shfl_xor(l, 32);
-    const float f = l > 0.0f ? 1.0f / l : l == 0.0f ? 0.0f : l;
+    const float f = share(l);
     // Through LDS, which nobody reads any more, so that whole rows are written at once.  A row has 16 bytes beside it: rows begin in different banks.
     constexpr int kOut = kRow + 16;
     static_assert(NW * 32 * kOut <= 4 * kBytes, "a workgroup's rows in LDS");
@@ -564,7 +566,7 @@ __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(Promp
             x[0] += *reinterpret_cast<const f32x4*>(from) * f;
             x[1] += *reinterpret_cast<const f32x4*>(from + 4) * f;
         }
-        const float f = L > 0.0f ? 1.0f / L : L == 0.0f ? 0.0f : L;
+        const float f = share(L);
         f16x8 y;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {

@@ -5,7 +5,7 @@ import pytest
 import attention as ref
 import paper_2506_23025_amd as tl
 from parity import to_dev
-from test_gpu_attention import KINDS, Setup, blank, cached, check_cached, f16, on, some_of, taken
+from test_gpu_attention import KINDS, KINDS_OF_CALL, Setup, blank, cached, check_cached, f16, on, prompt, some_of, starts, taken
 
 pytestmark = pytest.mark.gpu
 
@@ -149,3 +149,27 @@ def test_append_scales_at_the_ends_of_their_range(kind, new, past):
         fill(st)
         table = tl.tl_rope_table(80, 64, magnitude=magnitude)
         st.append(f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), table, 64, i % 2 == 0)
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
+@pytest.mark.parametrize("D,group", [(64, 1), (128, 1), (128, 4)])
+def test_prompt_rows_whose_scores_are_all_lost(call, D, group):
+    """Scores of -infinity at all that a row sees: their softmax is 0 / 0.  A row that sees one more is an ordinary one."""
+    n, H = KINDS_OF_CALL[call]
+    H = 24 if H == 3 else H
+    rng = np.random.default_rng(56)
+    st = starts(*n)
+    q, k, v = f16(rng, st[-1], H, D), f16(rng, st[-1], H // group, D), f16(rng, st[-1], H // group, D)
+    q[:, :, 5] = 1
+    for s in st[:-1]:
+        if s < st[-1]:
+            k[s:s + 3, 0, 5] = -np.inf
+    got = prompt(q, k, v, st, 0.1)
+    for a, b in zip(st[:-1], st[1:]):
+        lost = min(3, b - a)
+        assert np.isnan(got[a:a + lost, :group]).all(), a
+        assert np.isfinite(got[a + lost:b]).all() and np.isfinite(got[a:b, group:]).all(), a
+        if b - a > 3 and b - a < 100:
+            k0, v0 = k[a + 3:b, 0].astype(np.float64), v[a + 3:b, 0].astype(np.float64)
+            y, tol = ref.attend(q[b - 1, 0].astype(np.float64), k0, v0, np.ones(b - a - 3, bool), float(np.float32(0.1)))
+            assert (np.abs(got[b - 1, 0] - y) <= tol).all()
