@@ -396,7 +396,8 @@ tl_status tl_kv_append(const tl_append_job* job, void* stream);
  * Attention of a call's tokens over the cache, which holds them already (tl_kv_append first): the query of token i of sequence s sees
  * positions 0 .. cached[s] + i, and
  *     out[t][h] = sum_p softmax_p(scale * q[t][h] . k[p][g]) v[p][g],   g = h / (q_heads / kv_heads).
- * A query that sees no position (all its pages missing) gives 0.  A block whose scale is NaN makes NaN of every query that sees a token of it, and of no other.
+ * A query that sees no position (all its pages missing) gives 0.  One with an infinity or a NaN in it gives NaN otherwise.
+ * A block whose scale is NaN makes NaN of every query that sees a token of it, and of no other.
  *   q, out      q_heads heads of cache->head_dim dimensions; out may be q itself with the same strides, and may not overlap it otherwise
  *   scale       any sign; TL_ERR_VALUE where scale * log2(e) is not finite in fp32
  *   longest     an upper bound of cached[s] + the tokens of s over all sequences, 0 if not known: it spares the second

@@ -288,6 +288,30 @@ struct Walk {
         }
     }
 
+    // A query with an infinity: its scores are infinities of both signs or NaN, and their softmax NaN.  All negative, they would look unseen: all of the query becomes NaN.  (Raised
+    // codes and what takes the raise off make NaN of such scores by themselves.)
+    __device__ inline void look_at_queries()
+    {
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+            f16x8 zero = {0, 0, 0, 0, 0, 0, 0, 0};           // an infinity or a NaN leaves no 0
+#pragma unroll
+            for (int j = 0; j < J; ++j) zero += q[n][j][0] * _Float16(0.0f) + q[n][j][1] * _Float16(0.0f);
+            bool odd = false;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) odd |= !(zero[e] == _Float16(0.0f));
+            if (__any(odd)) {
+                float x = odd ? __builtin_nanf("") : 0.0f;
+                x += __shfl_xor(x, 16);
+                x += __shfl_xor(x, 32);
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) q[n][j][i] += _Float16(x);
+            }
+        }
+    }
+
     __device__ inline void walk(const CachedArgs& a, int seq, int head, int begin, int end, int step)
     {
         const int m16 = threadIdx.x & 15, g = (threadIdx.x & 63) >> 4, chunks = EXACT ? CH : a.c.dim >> 4;
@@ -333,6 +357,7 @@ struct Walk {
         ask_pages(begin);
         load_k(begin);
         load_v();
+        if constexpr (FP8) look_at_queries();                // while the first tile is on its way
         for (int tile = begin; tile < end; tile += step) {
             const bool more = tile + step < end;
             const bool inside = there;

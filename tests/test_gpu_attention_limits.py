@@ -173,3 +173,29 @@ def test_prompt_rows_whose_scores_are_all_lost(call, D, group):
             k0, v0 = k[a + 3:b, 0].astype(np.float64), v[a + 3:b, 0].astype(np.float64)
             y, tol = ref.attend(q[b - 1, 0].astype(np.float64), k0, v0, np.ones(b - a - 3, bool), float(np.float32(0.1)))
             assert (np.abs(got[b - 1, 0] - y) <= tol).all()
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("new", [[1, 1, 1, 1], [5, 1, 40, 3]])
+def test_cached_queries_that_are_no_numbers(kind, new):
+    """An infinity in a query makes infinities of all its scores, and NaN of its softmax whatever their signs; a row that sees nothing is 0 all the same."""
+    rng = np.random.default_rng(57)
+    st = Setup(58, new, [700, 5, 90, 20], 4, 2, 64, 32, kind, missing=((3, 0),))
+    c = st.cache.codes["k"]
+    c[..., 7] = 40                                         # of one sign
+    fill(st)
+    q = f16(rng, st.T, 4, 64)
+    bad = q.copy()
+    rows = [0, int(st.start[2]), st.T - 1]
+    for what in (np.inf, -np.inf, np.nan):
+        for r in rows:
+            bad[r, 1, 7] = what
+        for scale in (0.125, -0.125, 0.0):
+            for longest in (None, 0):
+                clean, got = (cached(st, x, scale, longest=longest) for x in (q, bad))
+                for r in rows[:2]:
+                    assert np.isnan(got[r, 1]).all(), (what, scale, longest, r)
+                    got[r, 1] = clean[r, 1]
+                assert np.array_equal(got, clean), (what, scale, longest)
+                if new[3] == 1:
+                    assert (got[-1] == 0).all()
