@@ -424,7 +424,7 @@ tl_status tl_attn_cached(const tl_cached_job* job, void* stream);
  * (batch.cached is not read), with fp16 keys and values:
  *     out[t][h] = sum_j softmax_j(scale * q[t][h] . k[j][g]) v[j][g],   g = h / (q_heads / kv_heads).
  * head_dim is a multiple of 16 up to 128; (seqs + tokens / 32) * q_heads is below 2^24; scale as in tl_cached_job.  An infinity or a NaN in a key or value shows in the tokens that see it and in no others.  A token
- * whose scores are all -infinity gives NaN.  out may be
+ * whose scores are all -infinity gives NaN, and so does one with an infinity or a NaN in its query.  out may be
  * q itself with the same strides, and may not overlap q, k or v otherwise.  Deterministic.
  */
 typedef struct tl_prompt_job {

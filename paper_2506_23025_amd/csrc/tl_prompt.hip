@@ -105,7 +105,11 @@ __device__ inline void load_queries(const PromptArgs& a, const _Float16* from, i
     for (int k = 0; k < KK; ++k) {
         const int c = 2 * k + half;
         q[k] = *reinterpret_cast<const f16x8*>(from + (c < (a.dim >> 3) ? c : 0) * 8);
-        if (c >= (a.dim >> 3) || a.scale == 0.0f) q[k] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+        if (c >= (a.dim >> 3)) q[k] = f16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    }
+    if (a.scale == 0.0f) {
+#pragma unroll
+        for (int k = 0; k < KK; ++k) q[k] *= _Float16(0.0f);              // an infinity or a NaN stays one
     }
     if (a.scale < 0.0f) {
 #pragma unroll

@@ -199,3 +199,26 @@ def test_cached_queries_that_are_no_numbers(kind, new):
                 assert np.array_equal(got, clean), (what, scale, longest)
                 if new[3] == 1:
                     assert (got[-1] == 0).all()
+
+
+@pytest.mark.parametrize("call", KINDS_OF_CALL)
+@pytest.mark.parametrize("D", [64, 128])
+def test_prompt_queries_that_are_no_numbers(call, D):
+    """Also with a scale of 0, which takes no infinity and no NaN away."""
+    n, H = KINDS_OF_CALL[call]
+    rng = np.random.default_rng(59)
+    st = starts(*n)
+    q, k, v = f16(rng, st[-1], H, D), f16(rng, st[-1], H, D), f16(rng, st[-1], H, D)
+    longest = int(np.argmax(np.diff(st)))
+    rows = [int(st[longest]), int(st[longest]) + 20, int(st[longest + 1]) - 1]
+    for scale in (0.1, -0.1, 0.0):
+        clean = prompt(q, k, v, st, scale)
+        for what in (np.inf, -np.inf, np.nan):
+            bad = q.copy()
+            for r in rows:
+                bad[r, 1, 7] = what
+            got = prompt(bad, k, v, st, scale)
+            for r in rows:
+                assert np.isnan(got[r, 1]).all(), (what, scale, r)
+                got[r, 1] = clean[r, 1]
+            assert np.array_equal(got, clean), (what, scale)
