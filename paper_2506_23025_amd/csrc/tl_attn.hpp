@@ -56,6 +56,10 @@ struct PromptArgs {
     float scale;
 };
 
+// Weights go into the second product in fp16, as powers of 2 relative to a running reference.  kSlack: log2 of how far a row's largest may pass its reference before that moves; kLift: log2 of what a weight at the
+// reference is in fp16.  Their sum is what fp16 holds (up to 2^15); with the lift at that, a weight is off by 2^-11 of itself down to 2^-21 of the reference, and below by 2^-32 of it.
+constexpr float kSlack = 8.0f, kLift = 7.0f;
+
 hipError_t launch_append(const AppendArgs& a, hipStream_t s);
 hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s);
 size_t cached_workspace(int64_t seqs, int64_t tokens, int64_t q_heads, int64_t kv_heads, int64_t dim);

@@ -8,7 +8,7 @@
 //   output  O^T = V^T P^T: A = values, dimension by token
 // Both layouts of the cache are made for this: every load is 16 bytes a lane and 256 contiguous bytes for 16 lanes, and nothing passes through LDS.
 // Softmax: weights p = 2^(x - m) are summed as they are, and reach the product as p * scale_v relative to a second running reference
-// R = max(x + log2 scale_v), so that their fp16 form (2^-11) is exact enough whatever the scales of the blocks are.  The references move only when a score
+// R = max(x + log2 scale_v) - kLift, so that their fp16 form (2^-11) is exact enough whatever the scales of the blocks are.  The references move only when a score
 // is more than 2^8 beyond them, so a tile needs no exchange between lanes.
 // Bound: memory.  Short caches: a workgroup takes a row tile, its waves deal the tiles among themselves and join their sums in LDS.  Otherwise the tiles of the whole
 // call stand in one row, sequence after sequence, and every wave of a grid that fills the chip once takes an equal piece of it, whatever the sequences' lengths; they are
@@ -28,7 +28,6 @@ constexpr int kWavesAll = 2048;           // waves that share a call's tiles: tw
 constexpr int kFewRows = 1024;            // up to so many rows a workgroup joins the parts of each, of 8 waves up to a quarter of it; beyond a wave
 
 constexpr float kInf = __builtin_inff();
-constexpr float kSlack = 8.0f;            // log2 of how far a weight may pass its reference (fp16 holds 2^15)
 
 struct Shape {
     int per;                              // tokens of a row tile
@@ -397,7 +396,7 @@ struct Walk {
 #pragma unroll
                     for (int i = 0; i < 16; i += 2) mx = max3(mx, s[n][i >> 2][i & 3], s[n][i >> 2][(i & 3) + 1]);
                     if (!MASKED || mx != -kInf) mx *= ksc;
-                    const float top = MASKED && mx == -kInf ? -kInf : mx + lv;
+                    const float top = MASKED && mx == -kInf ? -kInf : mx + (lv - kLift);
                     if (__any(mx > m[n] + kSlack || top > R[n] + kSlack)) {
                         // each row by itself: what one row sees does not change how another is rounded
                         float a1 = mx, a2 = top;

@@ -10,7 +10,8 @@
 // Softmax: powers of 2 relative to a row's reference, which moves only when a score is more than 2^8 beyond it (fp16 holds the weights all the same), so most tiles need
 // no exchange between lanes and no scaling of the sums.
 // Bound: the matrix pipes and, beside them, the softmax's vector instructions; two workgroups on a CU, so that one's products run beside the other's softmax.
-// Rounding: scores, statistics and sums in 32 bits; weights become fp16 (2^-11 of each) for the second product, and their sum is of the rounded ones, so that weights add up to 1.
+// Rounding: scores, statistics and sums in 32 bits; weights become fp16 for the second product, whose matrix instructions take no more (2^-11 of each, or 2^-32 of the reference where that is
+// more: at the reference a weight is 2^7, so that fp16 has its range where weights are), and their sum is of the rounded ones, so that weights add up to 1.
 // Measured: 16384 tokens, 32 heads of 128 on 8 key heads 2.01 to 2.16 ms from card to card, 1.02 to 1.09 PFLOP/s: the matrix pipes are busy 61 % of the time and the chip's power sets the clock (1.75 GHz; the same
 // on zeros 1.48 ms).  2048 tokens with 32 heads of 128 47 to 52 us; 11 packed prompts of up to 1500 with 32 heads of 64 on 8 55 to 57 us.
 #include "tl_attn.hpp"
@@ -21,7 +22,6 @@ namespace tl {
 namespace {
 
 constexpr float kInf = __builtin_inff();
-constexpr float kSlack = 8.0f;
 constexpr int kTile = 64;                 // keys
 
 // LDS addresses are 32-bit numbers here
@@ -33,7 +33,7 @@ typedef __attribute__((address_space(3))) f16x8 lds_f16x8;
 
 __device__ inline float finite(float x) { return x == -kInf ? 0.0f : x; }
 __device__ inline float power(float x) { return __builtin_amdgcn_exp2f(x); }
-// What a row's sums are multiplied by.  Every row sees a key, so its weights add up to 1 at least, unless all its scores are -infinity, whose softmax is 0 / 0.
+// What a row's sums are multiplied by.  Every row sees a key, so its weights add up to 2^kLift at least, unless all its scores are -infinity, whose softmax is 0 / 0.
 __device__ inline float share(float l) { return l > 0.0f ? 1.0f / l : __builtin_nanf(""); }
 
 __device__ inline uint32_t lds_address(const void* p)
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256, 2) void prompt_kernel(PromptArgs a)
         for (int b = 0; b < 2; ++b)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[b][i]), s[b][i + 1]);
-        mx = mx == -kInf ? mx : mx * scale;
+        mx = mx == -kInf ? mx : __builtin_fmaf(mx, scale, -kLift);
         if (__any(mx > m + kSlack)) {
             // each row by itself: what one row sees does not change how another is rounded
             mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -494,7 +494,7 @@ __global__ __launch_bounds__(128 * S, DP == 64 ? 4 : 2) void narrow_kernel(Promp
         float mx = -kInf;
 #pragma unroll
         for (int i = 0; i < 16; i += 2) mx = fmaxf(fmaxf(mx, s[i]), s[i + 1]);
-        mx = mx == -kInf ? mx : mx * scale;
+        mx = mx == -kInf ? mx : __builtin_fmaf(mx, scale, -kLift);
         if (__any(mx > m + kSlack)) {
             mx = fmaxf(mx, __shfl_xor(mx, 32));
             const float to = mx > m + kSlack ? mx : m;

@@ -222,3 +222,58 @@ def test_prompt_queries_that_are_no_numbers(call, D):
                 assert np.isnan(got[r, 1]).all(), (what, scale, r)
                 got[r, 1] = clean[r, 1]
             assert np.array_equal(got, clean), (what, scale)
+
+
+SHARES = [0.7 * 2.0 ** -24, 1.3 * 2.0 ** -27, 0.9 * 2.0 ** -21, 2.0 ** -16]
+
+
+def tail(n, share, value):
+    """What n weights of `share` each beside one of 1 make of `value` beside 0, and what that may be off by.
+
+    A weight is held in fp16 as 2^7 times what it is relative to the row's first and largest score, so that it is off by 2^-11 of itself or 2^-25 / 2^7; scores
+    of a few units, products with whole numbers, make it off by 2^-20 of itself; sums of a tile's weights of n in 32 bits by 2^-23 of the sum each; the output by 2^-11 of itself or by half of fp16's smallest step."""
+    y = n * share / (1 + n * share)
+    return value * y, value * (y * (2.0 ** -10 + 2.0 ** -20 + n / 64 * 2.0 ** -23) + n * 2.0 ** -32) + 2.0 ** -25
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("share", SHARES)
+@pytest.mark.parametrize("call", ["one", "several", "many"])
+def test_cached_many_small_weights_beside_a_large_one(kind, share, call):
+    """The first token takes nearly all of the weight, as first tokens do; hundreds of others share the rest."""
+    new, n, H, HK = {"one": ([1, 1], 1400, 2, 1), "several": ([1, 20], 1000, 2, 1), "many": ([1] * 75, 500, 32, 16)}[call]
+    D = 64
+    st = Setup(60, new, [n] * len(new), H, HK, D, 64, kind)
+    one = ref.encode(np.float32([4.0]), kind)[0]
+    first = st.table[:, 0]
+    for s in "kv":
+        st.cache.codes[s][:] = 0 if s == "k" else one
+        st.cache.scale[s][:] = 0.25 if s == "k" else 64
+    st.cache.codes["k"][first, :, 0, 0, 3] = one           # 1
+    st.cache.codes["v"][first, :, 0, 0] = 0                # and 256 elsewhere
+    fill(st)
+    q = np.zeros((st.T, H, D), np.float16)
+    q[:, :, 3] = 16.0
+    scale = -np.log(share) / 16.0
+    share = np.exp(-16.0 * float(np.float32(scale)))
+    for longest in (None, 0):
+        got = cached(st, q, scale, longest=longest).astype(np.float64)
+        for s in range(len(new)):
+            for i in range(new[s]):
+                y, tol = tail(n + i, share, 256.0)
+                off = np.abs(got[st.start[s] + i] - y).max()
+                assert off <= tol, (s, i, longest, off, y, tol)
+
+
+@pytest.mark.parametrize("H,HK,D,n", [(1, 1, 64, 20000), (4, 1, 128, 9000), (12, 12, 64, 9000), (16, 4, 128, 9000)])
+@pytest.mark.parametrize("share", SHARES)
+def test_prompt_many_small_weights_beside_a_large_one(H, HK, D, n, share):
+    q, k, v = np.zeros((n, H, D), np.float16), np.zeros((n, HK, D), np.float16), np.full((n, HK, D), 256, np.float16)
+    q[:, :, 3], k[0, :, 3], v[0] = 16.0, 1.0, 0.0
+    scale = -np.log(share) / 16.0
+    share = np.exp(-16.0 * float(np.float32(scale)))
+    got = prompt(q, k, v, [0, n], scale).astype(np.float64)
+    for r in (0, 1, 100, 1000, n // 2, n - 1):
+        y, tol = tail(r, share, 256.0)
+        off = np.abs(got[r] - y).max()
+        assert off <= tol, (r, off, y, tol)
