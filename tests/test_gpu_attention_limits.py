@@ -277,3 +277,51 @@ def test_prompt_many_small_weights_beside_a_large_one(H, HK, D, n, share):
         y, tol = tail(r, share, 256.0)
         off = np.abs(got[r] - y).max()
         assert off <= tol, (r, off, y, tol)
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("D", [64, 80, 128])
+@pytest.mark.parametrize("tokens", [1, 5])
+def test_cached_scores_of_queries_with_a_large_common_part(kind, D, tokens):
+    """Queries of 16 to 17 in steps of 2^-6 and keys of small whole numbers: products and sums are exact in 32 bits, in any order.  Two keys that differ in two places by 1 share the weight
+    by a difference of scores below 1, which is what is left of sums of hundreds.
+
+    A score in powers of 2 is off by 2^-23 of itself twice (the scale, its product), a weight and the output by 2^-11 each."""
+    rng = np.random.default_rng(66)
+    S, H, HK = 6, 8, 2
+    st = Setup(67, [tokens] * S, [64] * S, H, HK, D, 64, kind)
+    for n in "kv":
+        st.cache.codes[n][:] = 0
+        st.cache.scale[n][:] = 1
+    unit = ref.encode(np.arange(-15, 16).astype(np.float32), kind)
+    want = np.zeros((st.T, H))
+    off = np.zeros((st.T, H))
+    q = (16 + rng.integers(0, 64, (st.T, H, D)) / 64).astype(np.float16)
+    for s in range(S):
+        page, later = st.table[s, 0], st.table[s, 1]
+        for g in range(HK):
+            a = rng.integers(-14, 15, D)
+            while a.sum() != 0:
+                i = rng.integers(0, D)
+                a[i] = np.clip(a[i] - np.sign(a.sum()), -14, 14)
+            b = a.copy()
+            i, j = rng.permutation(D)[:2]
+            b[i], b[j] = b[i] + 1, b[j] - 1
+            ahead = np.sign(a)                             # what the other tokens are is far behind
+            st.cache.codes["k"][page, g], st.cache.codes["k"][later, g] = (unit[-a + 15] for _ in range(2))
+            st.cache.codes["k"][page, g, 0, 3], st.cache.codes["k"][page, g, 2, 9] = unit[a + 15], unit[b + 15]
+            st.cache.codes["v"][page, g, 2, 9] = unit[1 + 15]
+            for r in range(st.start[s], st.start[s + 1]):
+                for h in range(g * H // HK, (g + 1) * H // HK):
+                    # the signs of the deviations are the key's, so that its score is large
+                    q[r, h] = (16.5 + ahead * (np.abs(q[r, h].astype(np.float64) - 16.5))).astype(np.float16)
+                    x = q[r, h].astype(np.float64)
+                    scores = x @ a, x @ b
+                    assert min(scores) > 60 and x @ -a < 0
+                    want[r, h] = 1 / (1 + np.exp(scores[0] - scores[1]))
+                    off[r, h] = want[r, h] * (2 * 2.0 ** -11 + 2 * max(scores) * 1.45 * 2.0 ** -23) + 2.0 ** -24
+    fill(st)
+    for longest in (None, 0):
+        got = cached(st, q, 1.0, longest=longest).astype(np.float64)
+        worst = np.abs(got - want[:, :, None]).max(2)
+        assert (worst <= off).all(), (longest, (worst / off).max())
