@@ -403,6 +403,10 @@ def _wants(t, what, dtype, dims, dense=True):
     return t.data_ptr()
 
 
+# torch gives a tensor of no elements no address; a call of no tokens asks for one all the same, and reads and writes nothing there.
+_NOWHERE = 16
+
+
 def _heads(t, what, like=None):
     """fp16 [tokens][heads][dim], strides as they are along the first two."""
     if t is None:
@@ -412,6 +416,8 @@ def _heads(t, what, like=None):
         raise ValueError(f"{what}: the dimensions of a head have to stand side by side")
     if like is not None and t.shape != like:
         raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(like)}")
+    if t.numel() == 0:
+        p = _NOWHERE
     return tl_heads(p, t.stride(0) if t.shape[0] > 1 else 0, t.stride(1) if t.shape[1] > 1 else 0)
 
 

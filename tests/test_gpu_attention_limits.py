@@ -325,3 +325,18 @@ def test_cached_scores_of_queries_with_a_large_common_part(kind, D, tokens):
         got = cached(st, q, 1.0, longest=longest).astype(np.float64)
         worst = np.abs(got - want[:, :, None]).max(2)
         assert (worst <= off).all(), (longest, (worst / off).max())
+
+
+# ---- calls of no tokens ---------------------------------------------------------------------------
+
+def test_calls_of_no_tokens_do_nothing():
+    import torch
+    st = Setup(61, [0, 0], [5, 70], 4, 2, 64, 32, "int8")
+    q, k = (torch.empty((0, h, 64), dtype=torch.float16, device="cuda") for h in (4, 2))
+    rope = tl.make_rope(to_dev(tl.tl_rope_table(100, 64)), 64)
+    batch = tl.make_batch(st.startd, st.pastd, 2, 0)
+    tl.tl_kv_append(tl.make_append_job(q, k, k.clone(), q, k, batch, st.handle, rope))
+    space = torch.empty(tl.tl_attn_cached_workspace(2, 0, 4, 2, 64), dtype=torch.uint8, device="cuda")
+    tl.tl_attn_cached(tl.make_cached_job(q, q.clone(), batch, st.handle, 0.1, 0, space))
+    tl.tl_attn_prompt(tl.make_prompt_job(q, k, k.clone(), q.clone(), batch, 0.1))
+    st.check_cache()
