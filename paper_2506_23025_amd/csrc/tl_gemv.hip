@@ -1529,7 +1529,7 @@ gemv_longk_kernel(Args b)
     auto dma16 = [&](gbytes src, uint32_t lds_base) {       // lane l: 16 bytes from src (per lane) to lds_base + 16 l
         const uint32_t base = __builtin_amdgcn_readfirstlane(lds_base);
         // s_nop: the wait state that a transfer needs behind a scalar write of M0
-        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(base) : "memory");
+        asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" : : "v"(src), "s"(base) : "memory", "m0");
     };
     u32x4 xv[ROWS ? ROWS : 1];
     auto stage_x = [&](int p) {

@@ -78,7 +78,7 @@ __device__ __forceinline__ void lds_barrier3()
 // before later LDS accesses.
 __device__ __forceinline__ void dma16(uint32_t voff, const void* sbase, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(voff), "s"(sbase), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
 
 // 8 * (byte B of w): the offset of that byte's table entry, in one instruction (the shift

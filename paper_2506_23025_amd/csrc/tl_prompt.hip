@@ -44,7 +44,7 @@ __device__ inline uint32_t lds_address(const void* p)
 // 16 bytes a lane from base + off to LDS, the lanes' side by side.
 __device__ inline void transfer(const void* base, uint32_t off, uint32_t lds)
 {
-    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory");
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(base), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
 
 // Where piece c (16 bytes) of token r stands in its row.

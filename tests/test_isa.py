@@ -187,3 +187,17 @@ def test_operands_of_a_pass_are_built_in_one_place(tmp_path):
             elif kernel and "v_mfma" in line:
                 counts[kernel] += 1
     assert len(counts) >= 8 and set(counts.values()) == {64}, counts
+
+
+def test_assembly_that_writes_m0_says_so():
+    """A transfer's LDS address goes through M0, which the compiler may hold for transfers of its own unless the assembly names it among what it writes."""
+    folder = os.path.join(os.path.dirname(tl.__file__), "csrc")
+    count = 0
+    for name in sorted(os.listdir(folder)):
+        with open(os.path.join(folder, name)) as f:
+            text = f.read()
+        for m in re.finditer(r"\basm\s+volatile\s*\((.*?)\)\s*;", text, re.S):
+            if "s_mov_b32 m0" in m[1]:
+                count += 1
+                assert re.search(r'"m0"', m[1].rsplit(":", 1)[1]), f"{name}: {m[0]}"
+    assert count >= 5
