@@ -5,7 +5,7 @@ import pytest
 import attention as ref
 import paper_2506_23025_amd as tl
 from parity import to_dev
-from test_gpu_attention import KINDS, KINDS_OF_CALL, Setup, blank, cached, check_cached, f16, on, prompt, some_of, starts, taken
+from test_gpu_attention import KINDS, KINDS_OF_CALL, Setup, blank, cached, check_cached, f16, on, prompt, rope_table, some_of, starts, taken
 
 pytestmark = pytest.mark.gpu
 
@@ -340,3 +340,36 @@ def test_calls_of_no_tokens_do_nothing():
     tl.tl_attn_cached(tl.make_cached_job(q, q.clone(), batch, st.handle, 0.1, 0, space))
     tl.tl_attn_prompt(tl.make_prompt_job(q, k, k.clone(), q.clone(), batch, 0.1))
     st.check_cache()
+
+
+# ---- single tokens -------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("D,rot,pairs,page", [(128, 128, False, 64), (128, 64, True, 32), (128, 64, False, 16), (16, 16, False, 16), (32, 32, True, 128), (64, 32, False, 16), (80, 40, False, 64),
+                                               (80, 40, True, 16), (96, 48, True, 32), (96, 96, False, 256), (112, 2, True, 1024), (112, 22, False, 32), (48, 0, False, 64)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_one_token_each_of_any_head(kind, D, rot, pairs, page, in_place):
+    rng = np.random.default_rng(D + rot)
+    past = np.array([0, 1, 9, 15, 16, 17, 30, 31, -1, 100, 127])
+    st = Setup(D * 11 + rot, np.ones(len(past), int), past, 5, 5, D, page, kind)
+    for size in (1.0, 30.0):                               # the second call codes what the blocks hold anew
+        st.append(f16(rng, st.T, 5, D), f16(rng, st.T, 5, D, scale=size), f16(rng, st.T, 5, D, scale=3 * size), rope_table(128, rot), rot, pairs, extra=3, in_place=in_place)
+
+
+@pytest.mark.parametrize("kind", ["int8", "fp8"])
+@pytest.mark.parametrize("rot,pairs", [(64, False), (64, True), (36, False), (0, False)])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_append_one_token_each_of_zeros_infinities_and_missing_pages(kind, rot, pairs, in_place):
+    rng = np.random.default_rng(62)
+    past = np.array([0, 7, 15, 16, 40, 3, 20, 33, -2, 64, 90])
+    st = Setup(63, np.ones(len(past), int), past, 2, 2, 64, 16, kind, missing=((2, 0), (6, 1)))
+    q, k, v = f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64)
+    k[0] = v[1] = v[0, 1] = 0
+    k[3, 1, 7], k[4, 0, 3], v[5, 1, 63], v[2, 0, 1], v[7, 0] = np.nan, np.inf, -np.inf, np.nan, 65504
+    st.append(q, k, v, rope_table(60, rot), rot, pairs, in_place=in_place)      # the last two are beyond the table
+    for n in "kv":                                        # and a block that stands for NaN takes another token, as does one that is begun again
+        st.cache.scale[n][st.table[1, 0]] = np.nan
+        st.cache.scale[n][st.table[0, 0]] = np.nan
+    fill(st)
+    st.append(f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), f16(rng, st.T, 2, 64), rope_table(128, rot), rot, pairs, in_place=in_place)
+    assert not np.isnan(st.cache.scale["k"][st.table[0, 0]]).any() and np.isnan(st.cache.scale["k"][st.table[1, 0]]).all()
