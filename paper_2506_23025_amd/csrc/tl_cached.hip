@@ -14,7 +14,7 @@
 // call stand in one row, sequence after sequence, and every wave of a grid that fills the chip once takes an equal piece of it, whatever the sequences' lengths; they are
 // read on the device, so one captured launch serves every step.  Pieces of row tiles that several waves share meet in a second kernel.
 // Measured: 3 sequences of up to 131072 tokens, 32 heads of 128 on 8 key heads, int8 97 us (5.9 TB/s); 48 of up to 4096, e4m3 47.5 us (5.05 TB/s, 42 of them here and 5 in the second
-// kernel); 16 of up to 2047 with 32 key heads 32 us (4.3 TB/s).  One sequence of 700 tokens with 16 heads 6.8 us, a chain of reads: lengths, pages, scales, codes.
+// kernel); 16 of up to 2047 with 32 key heads 32 us (4.3 TB/s).  One sequence of 700 tokens with 16 heads 7.2 us, a chain of reads: lengths, pages, scales, codes.
 #include "tl_attn.hpp"
 
 #include <cmath>
@@ -788,9 +788,10 @@ hipError_t launch_cached(const CachedArgs& a, int64_t longest, hipStream_t s)
 {
     const Shape p = shape_of(a.b.seqs, a.b.tokens, !a.b.start, a.group, a.c.kv_heads);
     // Up to so many tiles a sequence is left to one workgroup: the partial sums and the second kernel would cost more than a finer split saves, and more so with many row tiles, or of 32
-    // rows.  In us, so and with pieces, heads of 128: one token of 8 sequences, 8 key heads, 15 tiles 10 and 13, 30 tiles 16 and 13; of 24 with 8 of 96, 22 tiles 16 and 23; of 64 with
-    // 8, 32 tiles 32 and 36, of 16 with 32, 32 tiles 46 and 51, of 40 with 8, 47 tiles 35 and 33; 64 tokens of 2, 16 heads on 2, 32 tiles 24 and 26; 16 of 4, 16 heads on 4, 32 tiles 22
-    // and 18.  Heads of 64: 45 tokens of 6, 32 heads on 8, 71 tiles 25 and 30; 5 of 3, 24 tiles 9.4 and 10.2; one token of 5, 32 tiles 11 and 10.
+    // rows.  In us, so and with pieces, sequences of one length, int8, 32 query heads of 128: one token of 8, 8 key heads, 15 tiles 8.6 and 11.3, 30 tiles 14.2 and 14.2; of 24 with 8 heads of 96, 22
+    // tiles 13 and 19; of 64 with 8, 32 tiles 42 and 48; of 16 with 32, 32 tiles 41 and 47; of 40 with 8, 47 tiles 44 and 47; 64 tokens of 2, 16 heads on 2, 32 tiles 23 and 26; 16 of 4, 16 heads
+    // on 4, 32 tiles 23 and 24.  Heads of 64: 45 tokens of 6, 71 tiles 52 and 49 (e4m3 47 and 47); 5 of 3, 24 tiles 12 and 13; one token of 5, 32 tiles 10.3 and 10.8.  Where lengths differ a
+    // workgroup has the longest to itself while others are done, which is why the limits lie below where the two meet here: one token of 40 with 8 key heads over up to 47 tiles 35 and 33.
     const bool many = likely_tiles(a.b.seqs, a.b.tokens, p) >= (p.nr == 2 ? 32.0 : 128.0);
     const int64_t alone_tiles = a.c.dim <= 64 ? (many && p.nr == 2 ? 80 : 24) : !many ? 16 : p.nr == 2 ? 32 : 36;
     const bool alone = longest > 0 && longest <= alone_tiles * 64;

@@ -5,7 +5,8 @@
 // dimensions (16 bytes) of T consecutive tokens, T = 4, 2 or 1 for heads of up to 128, 64 or 32 dimensions, so that a value's codes of T tokens, neighbours in memory,
 // are written together.  Query heads take the same way without the cache.
 // Bound: memory for prompts; for a step of a few sequences the chain of dependent reads (length, page, scale).
-// Measured: 7 prompts of up to 2048 tokens (6264 in all) with 96 heads of 128 79 us (3.9 TB/s of reads and writes); one token of 192 sequences with 48 heads 5.1 us; of one sequence 4.0 us.
+// Measured: 7 prompts of up to 2048 tokens (6264 in all) with 96 heads of 128 79 us (3.9 TB/s of reads and writes), 92 where pairs are half a head
+// apart (the angles of 4 tokens take 64 registers: two waves a SIMD in place of three), the same for both types of codes; one token of 192 sequences with 48 heads 5.1 us; of one sequence 4.0 us.
 #include "tl_attn.hpp"
 
 namespace tl {

@@ -612,7 +612,7 @@ hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
         else narrow_kernel<128, 4><<<small, 512, 0, s>>>(a);
     } else if (a.group % 4 == 0 && !(brief && busy <= 128)) {
         // 60 of up to 200 tokens with 32 heads of 64 on 8 33.8 us with 128 rows of one head, 25.0 with 32 of four; 60 of 96 with heads of 128 44 and 35; 200 of 10 on average 79, with 64 rows
-        // of one head 43, 31 with 32 of four; 11 of up to 1500 with heads of 64 66 and 63; one of 16384 2.06 ms both ways.
+        // of one head 43, 31 with 32 of four; 11 of up to 1500 with heads of 64 61 and 57; one of 16384 2.09 ms both ways.
         // One of 12 with 8 heads of 64 on one 5.2 us, 4.6 with 64 rows of one head
         heads_together(std::integral_constant<int, 4>{});
     } else if (brief) {
