@@ -607,7 +607,9 @@ hipError_t launch_prompt(const PromptArgs& a, hipStream_t s)
     if (!brief && busy <= (a.dim <= 64 ? 512 : 256) * (lengthy ? 2 : 1)) {
         // All fit on the chip at once, two to a compute unit or one, or where sequences are long half of them: the second half goes where the shorter ones of the first have been, and 128 rows
         // with all their keys leave a unit alone with one for long.  One head of 64, 14587 tokens: 198 us with 128 rows, 92 with 64 rows and keys dealt to four waves; 8 heads of 128, 2048
-        // tokens 40 and 29, 4096 75 and 66; 4 heads, 8000 133 and 109; but 16 heads, 3000 59 and 75, and 32 heads, 1024 25 and 27.
+        // tokens 40 and 29, 4096 75 and 66; 4 heads, 8000 133 and 100; but 16 heads, 3000 59 and 75, and 32 heads, 1024 25 and 27.  Between
+        // one workgroup a place and two: 1500 tokens, 16 heads 32 and 25, 20 heads 32 and 31, two of 1500, 10 heads 32 and 32; but two of 1000, 16 heads 24 and 27, one of 800, 32 heads 20 and 21; with twice
+        // the heads of 64 instead 27 and 24, 27 and 27, 28 and 28; 21 and 23, 17 and 18.
         if (a.dim <= 64) narrow_kernel<64, 4><<<small, 512, 0, s>>>(a);
         else narrow_kernel<128, 4><<<small, 512, 0, s>>>(a);
     } else if (a.group % 4 == 0 && !(brief && busy <= 128)) {
