@@ -437,6 +437,147 @@ typedef struct tl_prompt_job {
 tl_status tl_attn_prompt(const tl_prompt_job* job, void* stream);
 
 /*
+ * ---- Rows in 8 bits: the norms and gates of a block that make them, ternary products that take them ----
+ *
+ * Between its products a block adds to its residual, takes a norm of it, and weighs the up product by the gate.  Those steps can leave their rows in
+ * 8 bits with a scale for each row, and the ternary products then run on whole numbers: exactly, with half the bytes of activations, and at twice
+ * the matrix rate.
+ *
+ * Rows of numbers: element (row r, place d) at ptr + r * stride + d, fp16 unless said otherwise.  ptr is 16-byte aligned; the stride is in elements, a
+ * multiple of 16 bytes, not negative and below 2^40; rows that a call writes are at least as far apart as they are long (one row alone: any stride).
+ */
+typedef struct tl_rows {
+    void* ptr;                /* device */
+    int64_t stride;
+} tl_rows;
+
+/*
+ * Rows of 8-bit codes, -127 .. 127: place d of row r stands for scales[r] * code.  In each block of 16 places, place 4 i + s is byte 4 s + i (i, s = 0 .. 3): the order
+ * in which two bits of every byte of a packed word's bits meet them.  A row's last block is filled with 0; bytes behind it are
+ * neither read nor written.
+ *   codes    device, 16-byte aligned; rows are `stride` bytes apart, a multiple of 16 of at least ceil(places / 16) * 16 and below 2^40 (one row alone: any such multiple or 0)
+ *   scales   device, fp32 [rows], 4-byte aligned
+ * A row v becomes codes by its largest magnitude t: scale t / 127, code round(v * (127 / t)), quotients, product and rounding (to the nearest, ties
+ * to even) each as IEEE fp32 has them.  With t below 2^-100 scale and codes are 0; with an infinity or a NaN in v the scale is NaN and the codes are 0.
+ */
+typedef struct tl_rows8 {
+    int8_t* codes;
+    float* scales;
+    int64_t stride;
+} tl_rows8;
+
+typedef enum tl_real {
+    TL_REAL_FP16 = 0,
+    TL_REAL_FP32 = 1,
+    TL_REAL_INT_RANGE_ = 0x7fffffff /* not a type (see TL_FMT_INT_RANGE_) */
+} tl_real;
+
+/*
+ * The residual's addition and a root-mean-square norm:
+ *     s = residual + x                         rounded to `real`, kept in sum
+ *     v = (s * r) * weight,   r = 1 / sqrt(mean(s^2) + eps)
+ *     y = v in fp16,  out = v in 8 bits
+ * mean, root and quotient are taken in fp64 and r rounded to fp32; both products are fp32, each rounded by itself.
+ *   x         fp16
+ *   residual  `real`; ptr NULL: s = x, and sum is not written.  sum may be residual itself with the same stride, and x where real is TL_REAL_FP16; no other overlap with what
+ *             is read, here and below
+ *   sum       `real`; ptr NULL: not wanted
+ *   weight    device, fp16 [dim], 16-byte aligned; NULL: 1
+ *   y         ptr NULL: not wanted (it may be x with the same stride);  out: codes NULL: not wanted
+ *   rows >= 0 below 2^31 (0: the call does nothing), 1 <= dim <= 65536, eps >= 0 and finite (a row of zeros with eps 0 gives NaN)
+ * Deterministic.  TL_ERR_NULL where none of sum, y and out is wanted.
+ */
+typedef struct tl_norm_job {
+    tl_rows x, residual, sum, y;
+    tl_rows8 out;
+    const void* weight;
+    int64_t rows, dim;
+    float eps;
+    tl_real real;             /* of residual and sum */
+} tl_norm_job;
+
+tl_status tl_norm(const tl_norm_job* job, void* stream);
+
+/*
+ * The gate between the up and the down product, or (gate.ptr NULL) rows as they are, into fp16 and / or 8 bits:
+ *     v = gate / (1 + exp(-gate)) * up         in fp64, rounded to fp32 once;   or v = up
+ *     y = v in fp16,  out = v in 8 bits
+ * gate and up may lie side by side in the rows that one product writes.  y may be gate or up with the same stride.  rows and dim as in tl_norm.  Deterministic.
+ * TL_ERR_NULL where neither y nor out is wanted.
+ */
+typedef struct tl_gate_job {
+    tl_rows gate, up, y;
+    tl_rows8 out;
+    int64_t rows, dim;
+} tl_gate_job;
+
+tl_status tl_gate(const tl_gate_job* job, void* stream);
+
+/*
+ * Ternary products over 8-bit rows:
+ *     y[m][n] = fp16_rne( float(sum_k code[m][k] * w[n][k]) * (scale[m] * float(gamma)) ),
+ * the sum exact (rounded once to fp32 where it is beyond 2^24), products fp32.  Wpacked, gamma and y as for tl_ternary_gemm; x: M rows of K places.  Any M and N as there, K
+ * below 2^24.  A scale that is infinite or NaN shows in its row of y and in no other (0 codes with a scale of NaN give NaN).  Codes of -128 are taken as they are.  What a row's
+ * bytes behind place K - 1 hold does not matter.  Deterministic: the sums are whole numbers.
+ * tl_ternary_gemm_rows8_grouped: several independent products in one call, in as few launches as possible; jobs must not alias each other's
+ * outputs; `jobs` is host memory, read before the call returns.
+ */
+typedef struct tl_gemm_rows8_job {
+    tl_rows8 x;
+    const void* Wpacked;      /* device, TL_FMT_2BIT   */
+    void* y;                  /* device, fp16 [M][N]   */
+    int64_t M, N, K;
+    uint16_t gamma_fp16_bits;
+} tl_gemm_rows8_job;
+
+tl_status tl_ternary_gemm_rows8(const tl_gemm_rows8_job* job, void* stream);
+tl_status tl_ternary_gemm_rows8_grouped(const tl_gemm_rows8_job* jobs, int64_t count, void* stream);
+
+/*
+ * ---- 4-bit weights with group scales: for the layers that ternary weights do not serve, the head first ----
+ *
+ * A weight is scales[g][n] * (c - z): code c in 0 .. 15, g = k / group, z = zeros[g][n] or 8.  The paper's 4-bit family keeps one
+ * scale per 128 weights of a row (Sec. 3.3 compares with it).
+ *
+ * Packed form: a row's codes in blocks of 128 (the last filled with code 0), 16 words of 32 bits each.  Word w holds weights 8 w .. 8 w + 7 of the block
+ * and stands at place 4 (w % 4) + w / 4; in it weight 2 j has bits 4 j .. 4 j + 3 and weight 2 j + 1 bits 4 j + 16 .. 4 j + 19: a lane's 16 bytes are its operands
+ * of four matrix instructions, and one mask takes two neighbours.  Rows are tl_row_stride_4bit(K) = 64 ceil(K / 128) bytes apart (0 for K < 1).
+ *
+ * tl_quantize_4bit: codes of a trained matrix, host.  Without zeros scale = fp16(max|w| / 7) over the group and c = 8 + round(w / scale), held in 0 .. 15; with zeros
+ * lo = min(0, w), hi = max(0, w), scale = fp16((hi - lo) / 15), z = round(-lo / scale), c = z + round(w / scale), both held in 0 .. 15.  Quotients in fp64, ties to even; a
+ * scale of 0 gives codes 8 (z = 8).
+ *   W host, float [N][K], finite;  codes host, uint8 [N][K];  scales host, fp16 bits [ceil(K / group)][N];  zeros host, uint8 of the same shape, or NULL
+ * TL_ERR_VALUE if W holds a NaN or an infinity, or a group's scale is beyond fp16; group as for tl_gemm_4bit.
+ * tl_pack_4bit (TL_ERR_VALUE on a code above 15), tl_unpack_4bit: host, codes uint8 [N][K].
+ */
+size_t tl_row_stride_4bit(int64_t K);
+tl_status tl_quantize_4bit(const float* W, int64_t N, int64_t K, int64_t group, uint8_t* codes, uint16_t* scales_fp16_bits, uint8_t* zeros);
+tl_status tl_pack_4bit(const uint8_t* codes, int64_t N, int64_t K, uint32_t* out);
+tl_status tl_unpack_4bit(const uint32_t* packed, int64_t N, int64_t K, uint8_t* codes);
+
+/*
+ * y[m][n] = sum_g scales[g][n] * ( sum_{k in group g} x[m][k] * (c[n][k] - z[g][n]) ),  fp32 accumulation, rounded once to y's type.
+ *   x        device, fp16 [M][K], 16-byte aligned
+ *   Wpacked  device, packed form, 16-byte aligned
+ *   scales   device, fp16 [ceil(K / group)][N], 16-byte aligned;  zeros: device, uint8 of the same shape, 16-byte aligned (any byte is taken as it is), or NULL
+ *   y        device, fp16 or fp32 [M][N], 16-byte aligned
+ *   group    a multiple of 32; the last group may be short
+ * Any M, N, K >= 1; made for few rows (weights are streamed once for every 64).  A NaN or an infinity in row m of x shows in row m of y and in no other, one in a scale in its
+ * column.  Deterministic: no atomics, fixed order.
+ */
+typedef struct tl_gemm_4bit_job {
+    const void* x;
+    const void* Wpacked;
+    const void* scales;
+    const void* zeros;
+    void* y;
+    int64_t M, N, K, group;
+    tl_real y_real;
+} tl_gemm_4bit_job;
+
+tl_status tl_gemm_4bit(const tl_gemm_4bit_job* job, void* stream);
+
+/*
  * Bandwidth calibration: a plain streaming copy dst[i] = src[i] of `bytes` bytes
  * (multiple of 16, both device pointers 16-byte aligned).  Not part of the
  * method; it gives the HBM counters and timers a kernel of known traffic.

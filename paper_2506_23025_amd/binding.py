@@ -19,6 +19,7 @@ TL_ERR_NULL, TL_ERR_SHAPE, TL_ERR_VALUE, TL_ERR_ALIGN, TL_ERR_UNSUPPORTED, TL_ER
 TL_FMT_2BIT, TL_FMT_1P6BIT, TL_FMT_1P6BIT_FX = 0, 1, 2
 TL_KV_INT8, TL_KV_FP8 = 0, 1
 TL_ROPE_PLAIN, TL_ROPE_LINEAR, TL_ROPE_BY_PARTS = 0, 1, 2
+TL_REAL_FP16, TL_REAL_FP32 = 0, 1
 TL_PATH_AUTO, TL_PATH_GENERIC, TL_PATH_GEMV, TL_PATH_MFMA = 0, 1, 2, 3
 
 EXPORTS = (
@@ -33,6 +34,15 @@ EXPORTS = (
     "tl_attn_cached_workspace",
     "tl_attn_cached",
     "tl_attn_prompt",
+    "tl_norm",
+    "tl_gate",
+    "tl_ternary_gemm_rows8",
+    "tl_ternary_gemm_rows8_grouped",
+    "tl_row_stride_4bit",
+    "tl_quantize_4bit",
+    "tl_pack_4bit",
+    "tl_unpack_4bit",
+    "tl_gemm_4bit",
     "tl_probe_copy",
     "tl_probe_read",
     "tl_probe_mfma",
@@ -101,6 +111,39 @@ class tl_prompt_job(ctypes.Structure):
         ("batch", tl_batch), ("q_heads", ctypes.c_int64), ("kv_heads", ctypes.c_int64), ("head_dim", ctypes.c_int64), ("scale", ctypes.c_float)]
 
 
+class tl_rows(ctypes.Structure):
+    """Mirror of struct tl_rows in include/tl.h."""
+    _fields_ = [("ptr", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class tl_rows8(ctypes.Structure):
+    """Mirror of struct tl_rows8 in include/tl.h."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class tl_norm_job(ctypes.Structure):
+    """Mirror of struct tl_norm_job in include/tl.h."""
+    _fields_ = [(n, tl_rows) for n in ("x", "residual", "sum", "y")] + [
+        ("out", tl_rows8), ("weight", ctypes.c_void_p), ("rows", ctypes.c_int64), ("dim", ctypes.c_int64), ("eps", ctypes.c_float), ("real", ctypes.c_int)]
+
+
+class tl_gate_job(ctypes.Structure):
+    """Mirror of struct tl_gate_job in include/tl.h."""
+    _fields_ = [(n, tl_rows) for n in ("gate", "up", "y")] + [("out", tl_rows8), ("rows", ctypes.c_int64), ("dim", ctypes.c_int64)]
+
+
+class tl_gemm_rows8_job(ctypes.Structure):
+    """Mirror of struct tl_gemm_rows8_job in include/tl.h."""
+    _fields_ = [("x", tl_rows8), ("Wpacked", ctypes.c_void_p), ("y", ctypes.c_void_p), ("M", ctypes.c_int64), ("N", ctypes.c_int64), ("K", ctypes.c_int64),
+                ("gamma_fp16_bits", ctypes.c_uint16)]
+
+
+class tl_gemm_4bit_job(ctypes.Structure):
+    """Mirror of struct tl_gemm_4bit_job in include/tl.h."""
+    _fields_ = [(n, ctypes.c_void_p) for n in ("x", "Wpacked", "scales", "zeros", "y")] + [(n, ctypes.c_int64) for n in ("M", "N", "K", "group")] + [
+        ("y_real", ctypes.c_int)]
+
+
 class TlError(RuntimeError):
     def __init__(self, status, where):
         self.status = int(status)
@@ -163,6 +206,18 @@ def _load():
     L.tl_attn_cached_workspace.restype = sz
     for name, job in (("tl_kv_append", tl_append_job), ("tl_attn_cached", tl_cached_job), ("tl_attn_prompt", tl_prompt_job)):
         getattr(L, name).argtypes = [ctypes.POINTER(job), vp]
+        getattr(L, name).restype = ci
+    for name, job in (("tl_norm", tl_norm_job), ("tl_gate", tl_gate_job), ("tl_ternary_gemm_rows8", tl_gemm_rows8_job), ("tl_gemm_4bit", tl_gemm_4bit_job)):
+        getattr(L, name).argtypes = [ctypes.POINTER(job), vp]
+        getattr(L, name).restype = ci
+    L.tl_ternary_gemm_rows8_grouped.argtypes = [ctypes.POINTER(tl_gemm_rows8_job), i64, vp]
+    L.tl_ternary_gemm_rows8_grouped.restype = ci
+    L.tl_row_stride_4bit.argtypes = [i64]
+    L.tl_row_stride_4bit.restype = sz
+    L.tl_quantize_4bit.argtypes = [vp, i64, i64, i64, vp, vp, vp]
+    L.tl_quantize_4bit.restype = ci
+    for name in ("tl_pack_4bit", "tl_unpack_4bit"):
+        getattr(L, name).argtypes = [vp, i64, i64, vp]
         getattr(L, name).restype = ci
     L.tl_probe_copy.argtypes = [vp, vp, sz, vp]
     L.tl_probe_copy.restype = ci
@@ -530,6 +585,146 @@ def make_prompt_job(q, k, v, out, batch, scale):
 
 def tl_attn_prompt(job, stream=None):
     _check(_lib.tl_attn_prompt(job, _stream(stream)), "tl_attn_prompt")
+
+
+# ---- rows in 8 bits -----------------------------------------------------------------------
+
+def _rows(t, what, like=None, dtype=("float16",)):
+    """[rows][dim], the stride as it is."""
+    if t is None:
+        return tl_rows(None, 0)
+    p = _wants(t, what, dtype, 2, False)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError(f"{what}: the places of a row have to stand side by side")
+    if like is not None and t.shape != like:
+        raise ValueError(f"{what} has shape {tuple(t.shape)}, not {tuple(like)}")
+    return tl_rows(p if t.numel() else _NOWHERE, t.stride(0) if t.shape[0] > 1 else 0)
+
+
+def make_rows8(codes, scales, dim):
+    """codes: int8 [rows][at least ceil(dim / 16) * 16], the stride as it is; scales: float32 [rows]; rows of `dim` places."""
+    p, s = _wants(codes, "codes", ("int8",), 2, False), _wants(scales, "scales", ("float32",), 1)
+    if dim < 1 or codes.shape[1] < (dim + 15) // 16 * 16 or codes.stride(1) != 1:
+        raise ValueError(f"codes: rows of {(dim + 15) // 16 * 16} bytes side by side are wanted, not {tuple(codes.shape)}")
+    if scales.shape[0] != codes.shape[0]:
+        raise ValueError(f"{scales.shape[0]} scales for {codes.shape[0]} rows")
+    r = tl_rows8(p if codes.numel() else _NOWHERE, s if scales.numel() else _NOWHERE, codes.stride(0) if codes.shape[0] > 1 else 0)
+    r.kept, r.rows, r.dim = (codes, scales), codes.shape[0], dim
+    return r
+
+
+def _out8(out, shape):
+    if out is None:
+        return tl_rows8(None, None, 0)
+    if (out.rows, out.dim) != tuple(shape):
+        raise ValueError(f"out has {out.rows} rows of {out.dim}, not {tuple(shape)}")
+    return out
+
+
+def make_norm_job(x, residual=None, sum=None, weight=None, y=None, out=None, eps=1e-5):
+    """x, y: float16 [rows][dim]; residual, sum: the same in float16 or float32; weight: float16 [dim]; out: make_rows8's; all but x may be None."""
+    real = TL_REAL_FP16 if residual is None or str(residual.dtype) == "torch.float16" else TL_REAL_FP32
+    kinds = ("float16",) if real == TL_REAL_FP16 else ("float32",)
+    if sum is not None and residual is None:
+        raise ValueError("sum without residual")
+    j = tl_norm_job(_rows(x, "x"), _rows(residual, "residual", x.shape, kinds), _rows(sum, "sum", x.shape, kinds), _rows(y, "y", x.shape), _out8(out, x.shape), None,
+                    x.shape[0], x.shape[1], eps, real)
+    if weight is not None:
+        j.weight = _wants(weight, "weight", ("float16",), 1)
+        if weight.shape[0] != x.shape[1]:
+            raise ValueError(f"weight has {weight.shape[0]} places, x {x.shape[1]}")
+    j.kept = (x, residual, sum, weight, y, out)
+    return j
+
+
+def tl_norm(job, stream=None):
+    _check(_lib.tl_norm(job, _stream(stream)), "tl_norm")
+
+
+def make_gate_job(gate, up, y=None, out=None):
+    """gate, up, y: float16 [rows][dim]; gate None: up as it is; out: make_rows8's."""
+    j = tl_gate_job(_rows(gate, "gate", up.shape), _rows(up, "up"), _rows(y, "y", up.shape), _out8(out, up.shape), up.shape[0], up.shape[1])
+    j.kept = (gate, up, y, out)
+    return j
+
+
+def tl_gate(job, stream=None):
+    _check(_lib.tl_gate(job, _stream(stream)), "tl_gate")
+
+
+def make_rows8_jobs(jobs):
+    """[(x, Wpacked, gamma_fp16_bits, y), ...] -> ctypes array of tl_gemm_rows8_job; x: make_rows8's, Wpacked: 32-bit words [N][ceil(K / 16)], y: float16 [M][N]."""
+    arr = (tl_gemm_rows8_job * len(jobs))()
+    for a, (x, Wp, gbits, y) in zip(arr, jobs):
+        a.y, a.Wpacked = _wants(y, "y", ("float16",), 2), _wants(Wp, "Wpacked", ("int32", "uint32"), 2)
+        if y.shape[0] != x.rows or tuple(Wp.shape) != (y.shape[1], (x.dim + 15) // 16):
+            raise ValueError(f"x has {x.rows} rows of {x.dim}, Wpacked is {tuple(Wp.shape)}, y {tuple(y.shape)}")
+        a.x, a.M, a.N, a.K, a.gamma_fp16_bits = x, x.rows, y.shape[1], x.dim, gbits
+    arr.kept = jobs
+    return arr
+
+
+def tl_ternary_gemm_rows8(x, Wpacked, gamma_fp16_bits, y, stream=None):
+    _check(_lib.tl_ternary_gemm_rows8(make_rows8_jobs([(x, Wpacked, gamma_fp16_bits, y)]), _stream(stream)), "tl_ternary_gemm_rows8")
+
+
+def tl_ternary_gemm_rows8_grouped(jobs, stream=None):
+    """jobs: list of (x, Wpacked, gamma_fp16_bits, y), or an array made by make_rows8_jobs."""
+    arr = jobs if isinstance(jobs, ctypes.Array) else make_rows8_jobs(jobs)
+    _check(_lib.tl_ternary_gemm_rows8_grouped(arr, len(arr), _stream(stream)), "tl_ternary_gemm_rows8_grouped")
+
+
+# ---- 4-bit weights ---------------------------------------------------------------------------
+
+def tl_row_stride_4bit(K):
+    return int(_lib.tl_row_stride_4bit(K))
+
+
+def tl_quantize_4bit(W, group, zeros=False):
+    """float32 [N][K] -> (codes uint8 [N][K], scales float16 [ceil(K / group)][N], zeros uint8 of that shape or None)."""
+    W = np.ascontiguousarray(W, dtype=np.float32)
+    N, K = W.shape
+    if group < 1:
+        raise TlError(TL_ERR_SHAPE, "tl_quantize_4bit")
+    codes, scales = np.empty((N, K), dtype=np.uint8), np.empty((-(-K // group), N), dtype=np.uint16)
+    z = np.empty(scales.shape, dtype=np.uint8) if zeros else None
+    _check(_lib.tl_quantize_4bit(W.ctypes.data, N, K, group, codes.ctypes.data, scales.ctypes.data, z.ctypes.data if zeros else None), "tl_quantize_4bit")
+    return codes, scales.view(np.float16), z
+
+
+def tl_pack_4bit(codes):
+    """uint8 [N][K] -> uint32 [N][16 ceil(K / 128)]."""
+    codes = np.ascontiguousarray(codes, dtype=np.uint8)
+    N, K = codes.shape
+    out = np.empty((N, tl_row_stride_4bit(K) // 4), dtype=np.uint32)
+    _check(_lib.tl_pack_4bit(codes.ctypes.data, N, K, out.ctypes.data), "tl_pack_4bit")
+    return out
+
+
+def tl_unpack_4bit(packed, N, K):
+    packed = np.ascontiguousarray(packed)
+    if packed.nbytes != N * tl_row_stride_4bit(K):
+        raise ValueError("packed size does not match N, K")
+    out = np.empty((N, K), dtype=np.uint8)
+    _check(_lib.tl_unpack_4bit(packed.ctypes.data, N, K, out.ctypes.data), "tl_unpack_4bit")
+    return out
+
+
+def make_4bit_job(x, Wpacked, scales, zeros, group, y):
+    """x: float16 [M][K]; Wpacked: 32-bit words [N][16 ceil(K / 128)]; scales: float16 [ceil(K / group)][N]; zeros: uint8 of that shape or None; y: float16 or float32 [M][N]."""
+    j = tl_gemm_4bit_job(_wants(x, "x", ("float16",), 2), _wants(Wpacked, "Wpacked", ("int32", "uint32"), 2), _wants(scales, "scales", ("float16",), 2),
+                         None if zeros is None else _wants(zeros, "zeros", ("uint8",), 2), _wants(y, "y", ("float16", "float32"), 2),
+                         x.shape[0], y.shape[1], x.shape[1], group, TL_REAL_FP16 if str(y.dtype) == "torch.float16" else TL_REAL_FP32)
+    if y.shape[0] != x.shape[0] or tuple(Wpacked.shape) != (y.shape[1], tl_row_stride_4bit(x.shape[1]) // 4):
+        raise ValueError(f"x is {tuple(x.shape)}, Wpacked {tuple(Wpacked.shape)}, y {tuple(y.shape)}")
+    if group < 1 or any(t is not None and tuple(t.shape) != (-(-x.shape[1] // group), y.shape[1]) for t in (scales, zeros)):
+        raise ValueError(f"scales and zeros: {(-(-x.shape[1] // max(group, 1)), y.shape[1])} is wanted")
+    j.kept = (x, Wpacked, scales, zeros, y)
+    return j
+
+
+def tl_gemm_4bit(job, stream=None):
+    _check(_lib.tl_gemm_4bit(job, _stream(stream)), "tl_gemm_4bit")
 
 
 def tl_probe_copy(dst, src, nbytes, stream=None):

@@ -10,7 +10,7 @@ LIB = os.path.join(HERE, "libtl.so")
 OBJDIR = os.path.join(HERE, "_build")
 
 SOURCES = ["tl_host.cpp", "tl_basic.hip", "tl_gemv.hip", "tl_gemv3.hip", "tl_tile_2bit.hip", "tl_tile_1p6.hip", "tl_tile_gs.hip", "tl_api.hip",
-           "tl_kv.hip", "tl_cached.hip", "tl_prompt.hip", "tl_attn_api.hip"]
+           "tl_kv.hip", "tl_cached.hip", "tl_prompt.hip", "tl_attn_api.hip", "tl_rows.hip", "tl_rows8.hip", "tl_four.hip", "tl_rows_api.hip"]
 
 # packed-fp32 VALU forms are switched off for every device translation unit.
 HIPCC_FLAGS = [

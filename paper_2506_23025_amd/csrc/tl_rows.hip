@@ -1,0 +1,287 @@
+// The residual's addition with the norm, the gate, and rows as they are, into fp16 and 8 bits.
+#include "tl_rows.hpp"
+
+namespace tl {
+namespace {
+
+// The value of the lane that DPP control CTRL names; 0 where there is none.
+template <int CTRL, int ROWS>
+__device__ inline uint32_t moved(uint32_t x) { return uint32_t(__builtin_amdgcn_update_dpp(0, int(x), CTRL, ROWS, 15, true)); }
+template <int CTRL, int ROWS>
+__device__ inline double moved(double x)
+{
+    const u32x2 u = __builtin_bit_cast(u32x2, x);
+    return __builtin_bit_cast(double, u32x2{moved<CTRL, ROWS>(u[0]), moved<CTRL, ROWS>(u[1])});
+}
+
+// Over the wave, the result in all lanes: from the lane 1, 2, 4 and 8 before in the row of 16, a row's last lane to the next row, lane 31 to rows 2 and 3.
+template <class T, class F>
+__device__ inline T over_wave(T x, F f)
+{
+    x = f(x, moved<0x111, 15>(x));
+    x = f(x, moved<0x112, 15>(x));
+    x = f(x, moved<0x114, 15>(x));
+    x = f(x, moved<0x118, 15>(x));
+    x = f(x, moved<0x142, 10>(x));
+    return f(x, moved<0x143, 12>(x));
+}
+__device__ inline double wave_sum(double x)
+{
+    const u32x2 u = __builtin_bit_cast(u32x2, over_wave(x, [](double a, double b) { return a + b; }));
+    return __builtin_bit_cast(double, u32x2{uint32_t(__builtin_amdgcn_readlane(int(u[0]), 63)), uint32_t(__builtin_amdgcn_readlane(int(u[1]), 63))});
+}
+__device__ inline uint32_t wave_max(uint32_t x)
+{
+    return uint32_t(__builtin_amdgcn_readlane(int(over_wave(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; })), 63));
+}
+
+// g / (1 + e^-g) * u in fp64, off by some 2^-51 of itself, so that its fp32 rounding is that of the exact value but for one in 2^27: e^-g = 2^n e^r with |r| <= log(2) / 2 and the
+// series up to r^12, the quotient from the hardware's reciprocal by a step of Newton's and one on the quotient itself.  fp64 costs what fp32 does here, and the loads take longer.
+__device__ inline float gated(float g, float u)
+{
+    const double gu = double(g) * double(u);              // exact: 22 bits
+    double t = -double(g);
+    t = t > 700.0 ? 700.0 : t < -700.0 ? -700.0 : t;
+    const double n = __builtin_rint(t * 1.44269504088896340736);
+    double r = __builtin_fma(n, -0x1.62e42fefa39efp-1, t);
+    r = __builtin_fma(n, -0x1.abc9e3b39803fp-56, r);
+    double p = 1.0 / 479001600.0;
+    p = __builtin_fma(p, r, 1.0 / 39916800.0);
+    p = __builtin_fma(p, r, 1.0 / 3628800.0);
+    p = __builtin_fma(p, r, 1.0 / 362880.0);
+    p = __builtin_fma(p, r, 1.0 / 40320.0);
+    p = __builtin_fma(p, r, 1.0 / 5040.0);
+    p = __builtin_fma(p, r, 1.0 / 720.0);
+    p = __builtin_fma(p, r, 1.0 / 120.0);
+    p = __builtin_fma(p, r, 1.0 / 24.0);
+    p = __builtin_fma(p, r, 1.0 / 6.0);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    const double d = 1.0 + __builtin_amdgcn_ldexp(p, int(n));
+    double q = __builtin_amdgcn_rcp(d);
+    q = __builtin_fma(__builtin_fma(-d, q, 1.0), q, q);
+    double v = gu * q;
+    v = __builtin_fma(__builtin_fma(-v, d, gu), q, v);
+    // an infinity: its product is the answer, but for a gate of -infinity, which has none
+    return __builtin_isfinite(gu) ? float(v) : g == -__builtin_inff() ? __builtin_nanf("") : float(gu);
+}
+
+// Eight values from place d of a row on; 0 behind its end.
+__device__ inline void take(const _Float16* row, int d, int dim, float* v)
+{
+    if (d + 8 <= dim) {
+        const f16x8 x = *reinterpret_cast<const f16x8*>(row + d);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = float(x[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = d + i < dim ? float(row[d + i]) : 0.0f;
+    }
+}
+__device__ inline void take(const float* row, int d, int dim, float* v)
+{
+    if (d + 8 <= dim) {
+        const f32x4 x = *reinterpret_cast<const f32x4*>(row + d), y = *reinterpret_cast<const f32x4*>(row + d + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = x[i], v[4 + i] = y[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = d + i < dim ? row[d + i] : 0.0f;
+    }
+}
+__device__ inline void put(_Float16* row, int d, int dim, const float* v)
+{
+    if (d + 8 <= dim) {
+        f16x8 x;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = _Float16(rounded(v[i]));
+        *reinterpret_cast<f16x8*>(row + d) = x;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < dim) row[d + i] = _Float16(rounded(v[i]));
+    }
+}
+__device__ inline void put(float* row, int d, int dim, const float* v)
+{
+    if (d + 8 <= dim) {
+        *reinterpret_cast<f32x4*>(row + d) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(row + d + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (d + i < dim) row[d + i] = v[i];
+    }
+}
+
+// W waves hold a row in registers, C pieces of 8 values a lane; workgroups of four rows where a wave has one to itself.
+template <RowsKind KIND, int W, int C>
+__global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) rows_kernel(RowsArgs a)
+{
+    constexpr bool NORM = KIND >= kNormRows;
+    __shared__ double sums[W];
+    __shared__ uint32_t tops[W];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t row = W == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
+    if (W == 1 && row >= a.rows) return;
+    const int first = (W == 1 ? lane : int(threadIdx.x)) * 8;
+    constexpr int STEP = 64 * 8 * W;
+    const int dim = a.dim;
+    const _Float16* const xa = static_cast<const _Float16*>(a.a.p) + row * a.a.stride;
+    float v[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) take(xa, first + c * STEP, dim, v[c]);
+    if constexpr (KIND == kGatedRows) {
+        const _Float16* const xg = static_cast<const _Float16*>(a.b.p) + row * a.b.stride;
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+            float g[8];
+            take(xg, first + c * STEP, dim, g);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = gated(g[i], v[c][i]);
+        }
+    }
+    if constexpr (NORM) {
+        if constexpr (KIND == kNormSum16) {
+            const _Float16* const xr = static_cast<const _Float16*>(a.b.p) + row * a.b.stride;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float r[8];
+                take(xr, first + c * STEP, dim, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = float(_Float16(rounded(r[i] + v[c][i])));
+                if (a.sum.p) put(static_cast<_Float16*>(a.sum.p) + row * a.sum.stride, first + c * STEP, dim, v[c]);
+            }
+        }
+        if constexpr (KIND == kNormSum32) {
+            const float* const xr = static_cast<const float*>(a.b.p) + row * a.b.stride;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float r[8];
+                take(xr, first + c * STEP, dim, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = r[i] + v[c][i];
+                if (a.sum.p) put(static_cast<float*>(a.sum.p) + row * a.sum.stride, first + c * STEP, dim, v[c]);
+            }
+        }
+        double ss = 0.0;
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) ss = __builtin_fma(double(v[c][i]), double(v[c][i]), ss);
+        ss = wave_sum(ss);
+        if constexpr (W > 1) {
+            if (lane == 0) sums[wave] = ss;
+            __syncthreads();
+            ss = 0.0;
+#pragma unroll
+            for (int w = 0; w < W; ++w) ss += sums[w];
+        }
+        const float r = float(1.0 / sqrt(ss / double(dim) + a.eps));
+#pragma unroll
+        for (int c = 0; c < C; ++c) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] *= r;
+            if (a.weight) {
+                float w[8];
+                take(a.weight, first + c * STEP, dim, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] *= w[i];
+            }
+        }
+    }
+    if (a.y.p) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) put(static_cast<_Float16*>(a.y.p) + row * a.y.stride, first + c * STEP, dim, v[c]);
+    }
+    if (!a.out.codes) return;
+    // The largest magnitude as its bits: they order as the numbers do, infinities and NaN above all.
+    uint32_t top = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t u = (first + c * STEP + i < dim ? __builtin_bit_cast(uint32_t, v[c][i]) : 0u) & 0x7fffffffu;
+            top = u > top ? u : top;
+        }
+    top = wave_max(top);
+    if constexpr (W > 1) {
+        if (lane == 0) tops[wave] = top;
+        __syncthreads();
+        top = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = tops[w] > top ? tops[w] : top;
+    }
+    const float most = __builtin_bit_cast(float, top);
+    const bool finite = top < 0x7f800000u, some = finite && most >= 0x1p-100f;
+    const float inverse = some ? 127.0f / most : 0.0f;
+    if (first == 0) a.out.scales[row] = some ? most / 127.0f : finite ? 0.0f : __builtin_nanf("");
+    int8_t* const codes = a.out.codes + row * a.out.stride;
+    const bool odd = lane & 1;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        // Two lanes hold a block of 16.  Each has two bytes of all four words of it (places s and 4 + s of its half); the even lane writes the first two words, the odd lane the others.
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = uint32_t(int(some ? __builtin_rintf(v[c][i] * inverse) : 0.0f)) & 255u;
+        const uint32_t lo = q[0] | q[4] << 8 | q[1] << 16 | q[5] << 24, hi = q[2] | q[6] << 8 | q[3] << 16 | q[7] << 24;
+        const uint32_t got = moved<0xB1, 15>(odd ? lo : hi), own = odd ? hi : lo;
+        const uint32_t l = odd ? got : own, h = odd ? own : got;
+        const int d = first + c * STEP;
+        if ((d & ~15) < dim) *reinterpret_cast<u32x2*>(codes + d) = u32x2{(l & 0xffffu) | h << 16, l >> 16 | (h & 0xffff0000u)};
+    }
+}
+
+template <RowsKind KIND, int W, int C>
+hipError_t launch(const RowsArgs& a, hipStream_t s)
+{
+    const unsigned groups = W == 1 ? unsigned((a.rows + 3) / 4) : unsigned(a.rows);
+    hipLaunchKernelGGL((rows_kernel<KIND, W, C>), dim3(groups), dim3(W == 1 ? 256 : 64 * W), 0, s, a);
+    return hipGetLastError();
+}
+
+template <RowsKind KIND>
+hipError_t launch_kind(const RowsArgs& a, hipStream_t s)
+{
+    const int pieces = (a.dim + 7) / 8;
+    if (pieces <= 64) return launch<KIND, 1, 1>(a, s);
+    if (pieces <= 256) return launch<KIND, 4, 1>(a, s);
+    if (pieces <= 512) return launch<KIND, 4, 2>(a, s);
+    if (pieces <= 1024) return launch<KIND, 4, 4>(a, s);
+    if (pieces <= 2048) return launch<KIND, 16, 2>(a, s);
+    if (pieces <= 4096) return launch<KIND, 16, 4>(a, s);
+    return launch<KIND, 16, 8>(a, s);
+}
+
+}  // namespace
+
+hipError_t launch_rows(RowsKind kind, const RowsArgs& all, hipStream_t s)
+{
+    // A grid counts its threads in 32 bits: 2^21 rows of 1024 at a time.
+    constexpr int kMost = 1 << 21;
+    RowsArgs a = all;
+    if (all.rows > kMost) {
+        const auto moved = [](Rows r, int64_t rows, int bytes) { return r.p ? Rows{static_cast<char*>(r.p) + rows * r.stride * bytes, r.stride} : r; };
+        const int wide = kind == kNormSum32 ? 4 : 2;
+        for (int64_t at = 0; at < all.rows; at += kMost) {
+            a.a = moved(all.a, at, 2);
+            a.b = moved(all.b, at, wide);
+            a.sum = moved(all.sum, at, wide);
+            a.y = moved(all.y, at, 2);
+            if (a.out.codes) a.out = {all.out.codes + at * all.out.stride, all.out.scales + at, all.out.stride};
+            a.rows = all.rows - at < kMost ? int(all.rows - at) : kMost;
+            if (const hipError_t e = launch_rows(kind, a, s); e != hipSuccess) return e;
+        }
+        return hipSuccess;
+    }
+    switch (kind) {
+    case kPlainRows: return launch_kind<kPlainRows>(a, s);
+    case kGatedRows: return launch_kind<kGatedRows>(a, s);
+    case kNormRows: return launch_kind<kNormRows>(a, s);
+    case kNormSum16: return launch_kind<kNormSum16>(a, s);
+    default: return launch_kind<kNormSum32>(a, s);
+    }
+}
+
+}  // namespace tl

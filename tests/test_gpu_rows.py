@@ -1,0 +1,535 @@
+"""The operators on 8-bit rows and 4-bit weights on the GPU, against the plain forms in rows.py."""
+import numpy as np
+import pytest
+
+import paper_2506_23025_amd as tl
+import rows as ref
+
+pytestmark = pytest.mark.gpu
+
+
+def gamma_bits(g):
+    return int(np.float16(g).view(np.uint16))
+
+
+def on(x):
+    import torch
+    return torch.from_numpy(np.ascontiguousarray(x)).cuda()
+
+
+def strided(x, extra=0):
+    """numpy [rows][dim] on the device, rows a multiple of 16 bytes apart and `extra` multiples more, NaN (or 77) between them."""
+    import torch
+    each = 16 // x.itemsize
+    wide = torch.full((x.shape[0], ref.up(x.shape[1], each) + each * extra), float("nan") if x.dtype.kind == "f" else 77, dtype=on(x[:0]).dtype, device="cuda")
+    wide[:, :x.shape[1]] = on(x)
+    return wide[:, :x.shape[1]]
+
+
+class Out:
+    """An output with guards before, behind and between its rows."""
+
+    def __init__(self, rows, dim, dtype, extra=0, fill=77):
+        import torch
+        each = 16 // torch.empty(0, dtype=dtype).element_size()
+        self.fill, self.dim = fill, dim
+        self.all = torch.full((rows + 2, ref.up(dim, each) + each * extra), fill, dtype=dtype, device="cuda")
+        self.t = self.all[1:rows + 1, :dim]
+
+    def taken(self):
+        import torch
+        torch.cuda.synchronize()
+        a = self.all.cpu().numpy()
+        assert (a[0] == self.fill).all() and (a[-1] == self.fill).all() and (a[:, self.dim:] == self.fill).all(), "written outside of the output"
+        return a[1:-1, :self.dim]
+
+
+class Out8:
+    def __init__(self, rows, dim, extra=0):
+        import torch
+        self.codes, self.dim = Out(rows, ref.up(dim, 16), torch.int8, extra), dim
+        self.scales = torch.full((rows + 2,), 77.0, device="cuda")
+        self.rows8 = tl.make_rows8(self.codes.t, self.scales[1:-1], dim)
+
+    def taken(self):
+        codes, s = self.codes.taken(), self.scales.cpu().numpy()
+        assert s[0] == s[-1] == 77
+        places = ref.out_of_order(codes, codes.shape[1])
+        assert (places[:, self.dim:] == 0).all(), "places behind the row"
+        return places[:, :self.dim], s[1:-1]
+
+
+def same(a, b):
+    assert a.dtype == b.dtype and a.shape == b.shape
+    assert np.array_equal(a, b, equal_nan=a.dtype.kind == "f"), f"{int((~((a == b) | ((a != a) & (b != b)))).sum())} of {a.size} differ"
+
+
+def values(rng, rows, dim, kind=np.float16, scale=1.0):
+    x = rng.standard_normal((rows, dim)) * scale
+    x[:, rng.integers(0, dim, 1 + dim // 100)] *= 8
+    return x.astype(kind)
+
+
+# ---- the norm ---------------------------------------------------------------------------------
+#
+# Every step is rounded as IEEE has it and the mean is summed in 64 bits, so results are those of the plain form, bit for bit.
+
+def check_norm(rows, dim, kind, weight=True, residual=True, y=True, codes=True, extra=0, eps=1e-5, x=None, r=None, seed=0):
+    import torch
+    rng = np.random.default_rng(seed + dim)
+    x = values(rng, rows, dim) if x is None else x
+    r = (values(rng, rows, dim, kind, 3.0) if r is None else r) if residual else None
+    w = (1 + 0.2 * rng.standard_normal(dim)).astype(np.float16) if weight else None
+    total = Out(rows, dim, torch.float32 if kind == np.float32 else torch.float16, extra) if residual else None
+    out, out8 = Out(rows, dim, torch.float16, extra) if y else None, Out8(rows, dim, extra) if codes else None
+    tl.tl_norm(tl.make_norm_job(strided(x, extra), None if r is None else strided(r, extra), total.t if total else None, None if w is None else on(w),
+                                out.t if out else None, out8.rows8 if out8 else None, eps))
+    s, v = ref.norm(x, r, w, eps, kind)
+    if total:
+        same(total.taken(), s)
+    with np.errstate(all="ignore"):
+        if out:
+            same(out.taken(), v.astype(np.float16))
+        if out8:
+            c, scale = out8.taken()
+            want, want_scale = ref.coded(v)
+            same(scale, want_scale)
+            same(c, want)
+
+
+@pytest.mark.parametrize("dim", [1, 7, 8, 15, 16, 17, 64, 100, 511, 512, 513, 1000, 2048, 2049, 4096, 5000, 8192, 11008, 14336, 16385, 40000, 65536])
+def test_norm_of_any_length(dim):
+    check_norm(3, dim, np.float16, seed=1)
+    check_norm(2, dim, np.float32, seed=2, extra=1)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 5, 64, 333, 3000])
+@pytest.mark.parametrize("dim", [48, 1000, 4096])
+def test_norm_of_any_number_of_rows(rows, dim):
+    check_norm(rows, dim, np.float16, seed=3)
+    check_norm(rows, dim, np.float32, seed=4)
+
+
+@pytest.mark.parametrize("kind", [np.float16, np.float32])
+@pytest.mark.parametrize("weight", [False, True])
+@pytest.mark.parametrize("y,codes", [(True, False), (False, True), (False, False)])
+def test_norm_with_what_is_wanted(kind, weight, y, codes):
+    check_norm(9, 776, kind, weight=weight, y=y, codes=codes, extra=2, seed=5)
+    if y or codes:
+        check_norm(9, 776, np.float16, weight=weight, residual=False, y=y, codes=codes, seed=6)
+
+
+def test_norm_of_zeros_infinities_and_nan():
+    rng = np.random.default_rng(7)
+    x = values(rng, 8, 600)
+    r = values(rng, 8, 600, np.float32)
+    x[1], r[1] = 0, 0
+    x[2, 5] = np.inf
+    x[3, 599] = np.nan
+    r[4, 0] = -np.inf
+    x[5], r[5] = 0, 1e-30
+    x[6], r[6] = 65504, 3e38
+    for eps in (1e-5, 0.0):
+        check_norm(8, 600, np.float32, x=x, r=r, eps=eps)
+        with np.errstate(over="ignore"):
+            check_norm(8, 600, np.float16, x=x, r=r.astype(np.float16), eps=eps)
+
+
+def test_norm_in_place():
+    import torch
+    rng = np.random.default_rng(8)
+    x, r = values(rng, 70, 1000), values(rng, 70, 1000)
+    s, v = ref.norm(x, r)
+    for to in ("residual", "x"):
+        xd, rd, out8 = on(x), on(r), Out8(70, 1000)
+        tl.tl_norm(tl.make_norm_job(xd, rd, rd if to == "residual" else xd, None, None if to == "x" else xd, out8.rows8))
+        same((rd if to == "residual" else xd).cpu().numpy(), s)
+        if to == "residual":
+            same(xd.cpu().numpy(), v.astype(np.float16))
+        same(out8.taken()[0], ref.coded(v)[0])
+    torch.cuda.synchronize()
+
+
+def test_one_row_for_all():
+    """A residual (or an input) that is the same for all rows, stride 0."""
+    import torch
+    rng = np.random.default_rng(9)
+    x, r = values(rng, 40, 304), values(rng, 1, 304)
+    total = Out(40, 304, torch.float16)
+    job = tl.make_norm_job(on(x), on(r).expand(40, 304), total.t)
+    assert job.residual.stride == 0
+    tl.tl_norm(job)
+    same(total.taken(), ref.norm(x, np.repeat(r, 40, 0))[0])
+
+
+# ---- the gate ---------------------------------------------------------------------------------
+#
+# The gate is within 2^-51 of the exact value before its rounding to 32 bits, numpy's within a few units of 2^-53: roundings fall on the same side but for one value in 2^26.
+
+def check_gate(rows, dim, plain=False, y=True, codes=True, extra=0, g=None, u=None, seed=0):
+    import torch
+    rng = np.random.default_rng(seed + dim)
+    g, u = (values(rng, rows, dim, scale=2.0) if g is None else g), (values(rng, rows, dim) if u is None else u)
+    out, out8 = Out(rows, dim, torch.float16, extra) if y else None, Out8(rows, dim, extra) if codes else None
+    tl.tl_gate(tl.make_gate_job(None if plain else strided(g, extra), strided(u, extra), out.t if out else None, out8.rows8 if out8 else None))
+    v = ref.gate(None if plain else g, u)
+    with np.errstate(all="ignore"):
+        if out:
+            same(out.taken(), v.astype(np.float16))
+        if out8:
+            c, scale = out8.taken()
+            want, want_scale = ref.coded(v)
+            same(scale, want_scale)
+            same(c, want)
+
+
+@pytest.mark.parametrize("dim", [1, 9, 16, 100, 512, 1000, 2816, 4096, 5632, 11008, 14336, 30001, 65536])
+@pytest.mark.parametrize("plain", [False, True])
+def test_gate_of_any_length(dim, plain):
+    check_gate(3, dim, plain, seed=1, extra=1)
+
+
+@pytest.mark.parametrize("rows", [1, 6, 129, 2500])
+@pytest.mark.parametrize("y,codes", [(True, True), (True, False), (False, True)])
+def test_gate_of_any_number_of_rows(rows, y, codes):
+    check_gate(rows, 1544, False, y, codes, seed=2)
+    check_gate(rows, 200, True, y, codes, seed=3)
+
+
+def test_gate_over_all_of_fp16():
+    """Every finite gate, of up values that leave its product within fp32 and fp16."""
+    g = np.arange(65536, dtype=np.uint16).view(np.float16)
+    g = g[np.isfinite(g)]
+    g = np.concatenate([g, np.zeros(-len(g) % 512, np.float16)]).reshape(-1, 512)
+    u = np.random.default_rng(4).standard_normal(g.shape).astype(np.float16)
+    check_gate(g.shape[0], 512, g=g, u=u)
+
+
+def test_gate_of_infinities_and_nan():
+    rng = np.random.default_rng(5)
+    g, u = values(rng, 7, 96), values(rng, 7, 96)
+    u[0, 3] = np.inf
+    g[1, 3], u[1, 3] = np.inf, 0.5
+    g[2, 95] = np.nan
+    u[3, 0] = np.nan
+    g[4, 50], u[4, 50] = -np.inf, 2
+    g[5], u[5] = 0, 0
+    check_gate(7, 96, g=g, u=u)
+    check_gate(7, 96, True, u=u)
+
+
+def test_gate_of_halves_of_one_row_in_place():
+    rng = np.random.default_rng(6)
+    both = values(rng, 50, 2 * 808)
+    for to in (0, 1):
+        d = on(both)
+        halves = d[:, :808], d[:, 808:]
+        tl.tl_gate(tl.make_gate_job(*halves, halves[to]))
+        got = d.cpu().numpy()
+        same(got[:, 808 * to:808 * to + 808], ref.gate(both[:, :808], both[:, 808:]).astype(np.float16))
+        same(got[:, 808 - 808 * to:1616 - 808 * to], both[:, 808 - 808 * to:1616 - 808 * to])
+
+
+# ---- ternary products over 8-bit rows ------------------------------------------------------------
+#
+# The sum is exact, the two products and the rounding are IEEE's: bit for bit the plain form's.
+
+def rows8_of(codes, scales, extra=0, fill=77):
+    """On the device; every byte behind place dim - 1 set to `fill`, which must not matter."""
+    rows, dim = codes.shape
+    c = ref.in_order(np.pad(codes, ((0, 0), (0, -dim % 16)), constant_values=fill))
+    return tl.make_rows8(strided(c, extra), on(scales), dim)
+
+
+def product(seed, M, N, K, extra=0, zero=0.4):
+    rng = np.random.default_rng(seed)
+    codes = np.clip(np.rint(rng.standard_normal((M, K)) * 40), -127, 127).astype(np.int8)
+    scales = (0.01 + rng.random(M) / 30).astype(np.float32)
+    W = rng.choice(np.array([-1, 0, 1], np.int8), (N, K), p=[(1 - zero) / 2, zero, (1 - zero) / 2])
+    gamma = 0.01 + 0.04 * rng.random()
+    return codes, scales, W, gamma
+
+
+def check_products(jobs, extra=0):
+    import torch
+    outs, calls = [], []
+    for codes, scales, W, gamma in jobs:
+        M, N = codes.shape[0], W.shape[0]
+        y = torch.full((M * N + 128,), 77.0, dtype=torch.float16, device="cuda")
+        at = y[64:64 + M * N].view(M, N)
+        outs.append((y, at))
+        calls.append((rows8_of(codes, scales, extra), on(tl.tl_pack_2bit(W).view(np.int32)), gamma_bits(gamma), at))
+    if len(calls) == 1:
+        tl.tl_ternary_gemm_rows8(*calls[0])
+    else:
+        tl.tl_ternary_gemm_rows8_grouped(calls)
+    torch.cuda.synchronize()
+    for (codes, scales, W, gamma), (y, at) in zip(jobs, outs):
+        assert (y[:64] == 77).all() and (y[64 + at.numel():] == 77).all(), "written outside of the output"
+        same(at.cpu().numpy(), ref.ternary(codes, scales, W, np.float16(gamma)))
+
+
+@pytest.mark.parametrize("K", [1, 15, 16, 17, 63, 64, 65, 100, 128, 192, 256, 500, 512, 513, 1024, 1040, 2048, 4096, 4100, 5000, 11008])
+@pytest.mark.parametrize("M", [1, 16, 40])
+def test_rows8_product_of_any_length(M, K):
+    check_products([product(K, M, 48, K)])
+    check_products([product(K + 1, M, 33, K)], extra=1)
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 8, 15, 16, 17, 31, 32, 33, 48, 64, 65, 96, 127, 128, 129, 200, 256, 300, 513])
+@pytest.mark.parametrize("N,K", [(16, 64), (100, 320), (1000, 1024), (272, 776)])
+def test_rows8_product_of_any_number_of_rows(M, N, K):
+    check_products([product(M, M, N, K)])
+
+
+@pytest.mark.parametrize("N", [1, 2, 15, 17, 31, 64, 127, 129, 255, 257, 500, 1023, 2048, 4097])
+def test_rows8_product_of_any_number_of_columns(N):
+    for M in (1, 20, 150):
+        check_products([product(N, M, N, 448)])
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 2048, 2048), (1, 14336, 4096), (16, 4096, 11008), (33, 4096, 4096), (100, 1000, 14336), (700, 1500, 2048), (2000, 640, 640)])
+def test_rows8_product_of_layers(M, N, K):
+    check_products([product(M + N + K, M, N, K)])
+
+
+def test_rows8_products_of_one_call():
+    check_products([product(1, 5, 96, 512), product(2, 5, 32, 512), product(3, 5, 33, 512)])
+    check_products([product(10 + i, 1 + 7 * i, 16 + 20 * i, 100 + 61 * i) for i in range(9)])
+    check_products([product(20 + i, 3, 48, 256) for i in range(70)])
+    check_products([product(30, 1, 4096, 2048), product(31, 300, 640, 1024), product(32, 16, 1000, 4096), product(33, 1, 1, 1)])
+
+
+def test_rows8_product_at_the_ends_of_its_range():
+    """The largest sums, codes of -128, scales and results out of fp16."""
+    for M in (2, 40):
+        W = np.ones((32, 4096), np.int8)
+        W[1::2] = -1
+        codes = np.full((M, 4096), 127, np.int8)
+        codes[1] = -128
+        scales = np.full(M, 1e-3, np.float32)
+        scales[0] = 1e3
+        check_products([(codes, scales, W, 0.02)])
+    codes, scales, W, gamma = product(5, 20, 64, 300)
+    scales[3], scales[7], scales[9], scales[12] = np.nan, np.inf, 0, 1e-38
+    codes[3] = 0
+    check_products([(codes, scales, W, gamma)])
+    check_products([(codes, scales, W, np.inf)])
+
+
+# ---- products with 4-bit weights ---------------------------------------------------------------------
+
+def check_four(seed, M, N, K, group, zeros=False, wide=False, x=None, codes=None):
+    import torch
+    rng = np.random.default_rng(seed)
+    x = values(rng, M, K) if x is None else x
+    codes = rng.integers(0, 16, (N, K)).astype(np.uint8) if codes is None else codes
+    G = -(-K // group)
+    scales = ((0.5 + rng.random((G, N))) / 16).astype(np.float16)
+    z = rng.integers(0, 16, (G, N)).astype(np.uint8) if zeros else None
+    kind = torch.float32 if wide else torch.float16
+    guard = 16
+    y = torch.full((M * N + 2 * guard,), 77.0, dtype=kind, device="cuda")
+    at = y[guard:guard + M * N].view(M, N)
+    tl.tl_gemm_4bit(tl.make_4bit_job(on(x), on(tl.tl_pack_4bit(codes).view(np.int32)), on(scales), None if z is None else on(z), group, at))
+    torch.cuda.synchronize()
+    assert (y[:guard] == 77).all() and (y[guard + M * N:] == 77).all(), "written outside of the output"
+    want, off = ref.gemm4(x, ref.weights4(codes, scales, z, group))
+    got = at.cpu().numpy().astype(np.float64)
+    room = off + np.abs(want) * (2.0 ** -24 if wide else 2.0 ** -11) + (0 if wide else 2.0 ** -25)
+    fine = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert (np.abs(got - want)[fine] <= room[fine]).all(), f"{np.abs(got - want)[fine].max()} off, {(np.abs(got - want) / room)[fine].max()} of what may be"
+    return got
+
+
+@pytest.mark.parametrize("K", [1, 8, 31, 32, 33, 64, 100, 127, 128, 129, 255, 256, 257, 300, 512, 640, 1000, 1024, 2048, 4096, 4100, 11008])
+@pytest.mark.parametrize("M", [1, 7])
+def test_four_of_any_length(M, K):
+    check_four(K, M, 48, K, 128)
+    check_four(K + 1, M, 35, K, 32, zeros=True, wide=True)
+
+
+@pytest.mark.parametrize("M", [1, 2, 5, 15, 16, 17, 24, 31, 32, 33, 48, 63, 64, 65, 100, 130, 200])
+@pytest.mark.parametrize("group", [32, 64, 128, 256])
+def test_four_of_any_number_of_rows(M, group):
+    check_four(M + group, M, 80, 776, group, zeros=M % 2 == 0, wide=M % 3 == 0)
+
+
+@pytest.mark.parametrize("group", [32, 64, 96, 128, 160, 256, 384, 512, 1024, 4096, 1 << 20])
+def test_four_with_groups_of_any_size(group):
+    for zeros in (False, True):
+        check_four(group + zeros, 3, 64, 2304, group, zeros)
+        check_four(group + zeros, 18, 37, 1000, group, zeros)
+
+
+@pytest.mark.parametrize("N", [1, 2, 3, 15, 16, 17, 31, 33, 100, 255, 257, 1000, 4097])
+def test_four_of_any_number_of_columns(N):
+    check_four(N, 2, N, 512, 64, zeros=True)
+    check_four(N, 40, N, 264, 128)
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (4, 32000, 2048), (16, 14336, 4096), (33, 4096, 14336)])
+def test_four_of_layers(M, N, K):
+    check_four(M + N, M, N, K, 128, wide=M == 4)
+
+
+def test_four_of_infinities_and_nan():
+    for M in (6, 40):
+        rng = np.random.default_rng(M)
+        x = values(rng, M, 300)
+        clean = check_four(9, M, 40, 300, 64, x=x, wide=True)
+        x[1, 299] = np.nan
+        x[4, 0] = np.inf
+        got = check_four_raw(9, M, 40, 300, 64, x)
+        rest = [m for m in range(M) if m not in (1, 4)]
+        assert np.isnan(got[1]).all() and not np.isfinite(got[4]).any() and np.array_equal(got[rest], clean[rest])
+
+
+def check_four_raw(seed, M, N, K, group, x):
+    """The same call as check_four's without its comparison."""
+    import torch
+    rng = np.random.default_rng(seed)
+    codes = rng.integers(0, 16, (N, K)).astype(np.uint8)
+    scales = ((0.5 + rng.random((-(-K // group), N))) / 16).astype(np.float16)
+    y = torch.empty((M, N), device="cuda")
+    tl.tl_gemm_4bit(tl.make_4bit_job(on(x), on(tl.tl_pack_4bit(codes).view(np.int32)), on(scales), None, group, y))
+    return y.cpu().numpy().astype(np.float64)
+
+
+# ---- together, on streams and in graphs -------------------------------------------------------------
+
+class Block:
+    """A block's way past attention on 8-bit rows, and the head: norm, queries' product, rows as they are, output product, norm, gate and up product, gate, down product, norm, 4-bit head."""
+
+    def __init__(self, M, width, hidden, vocab, seed):
+        import torch
+        rng = np.random.default_rng(seed)
+        self.M, self.width, self.hidden = M, width, hidden
+        self.h = {n: rng.choice(np.array([-1, 0, 1], np.int8), s) for n, s in (("q", (width, width)), ("o", (width, width)), ("up", (2 * hidden, width)), ("down", (width, hidden)))}
+        self.w = {n: on(tl.tl_pack_2bit(w).view(np.int32)) for n, w in self.h.items()}
+        self.gamma = np.float16(0.03)
+        self.weight = (1 + 0.2 * rng.standard_normal(width)).astype(np.float16)
+        self.codes4, self.scales4, _ = tl.tl_quantize_4bit(rng.standard_normal((vocab, width)).astype(np.float32) / 8, 64)
+        new = lambda n, t=torch.float16: torch.zeros((M, n), dtype=t, device="cuda")  # noqa: E731
+        self.x, self.res, self.start = new(width), new(width, torch.float32), rng
+        self.a, self.b, self.up, self.y, self.logits = new(width), new(width), new(2 * hidden), new(width), new(vocab, torch.float32)
+        self.r1 = tl.make_rows8(new(ref.up(width, 16), torch.int8), torch.zeros(M, device="cuda"), width)
+        self.r2 = tl.make_rows8(new(ref.up(hidden, 16), torch.int8), torch.zeros(M, device="cuda"), hidden)
+        g, w = gamma_bits(self.gamma), on(self.weight)
+        norm = lambda x, out=None, y=None: tl.make_norm_job(x, self.res, self.res, w, y, out)  # noqa: E731
+        self.steps = [(tl.tl_norm, norm(self.x, self.r1)), (tl.tl_ternary_gemm_rows8_grouped, tl.make_rows8_jobs([(self.r1, self.w["q"], g, self.a)])),
+                      (tl.tl_gate, tl.make_gate_job(None, self.a, None, self.r1)), (tl.tl_ternary_gemm_rows8_grouped, tl.make_rows8_jobs([(self.r1, self.w["o"], g, self.b)])),
+                      (tl.tl_norm, norm(self.b, self.r1)), (tl.tl_ternary_gemm_rows8_grouped, tl.make_rows8_jobs([(self.r1, self.w["up"], g, self.up)])),
+                      (tl.tl_gate, tl.make_gate_job(self.up[:, :hidden], self.up[:, hidden:], None, self.r2)),
+                      (tl.tl_ternary_gemm_rows8_grouped, tl.make_rows8_jobs([(self.r2, self.w["down"], g, self.b)])),
+                      (tl.tl_norm, norm(self.b, None, self.y)),
+                      (tl.tl_gemm_4bit, tl.make_4bit_job(self.y, on(tl.tl_pack_4bit(self.codes4).view(np.int32)), on(self.scales4), None, 64, self.logits))]
+
+    def set(self, x, res):
+        self.x.copy_(on(x))
+        self.res.copy_(on(res))
+
+    def run(self, stream=None):
+        for call, job in self.steps:
+            call(job, stream)
+
+    def want(self, x, res):
+        def rows(v):
+            return ref.coded(v)
+        res, v = ref.norm(x, res, self.weight, kind=np.float32)
+        a = ref.ternary(*rows(v), self.h["q"], self.gamma)
+        b = ref.ternary(*rows(a.astype(np.float32)), self.h["o"], self.gamma)
+        res, v = ref.norm(b, res, self.weight, kind=np.float32)
+        u = ref.ternary(*rows(v), self.h["up"], self.gamma)
+        b = ref.ternary(*rows(ref.gate(u[:, :self.hidden], u[:, self.hidden:])), self.h["down"], self.gamma)
+        res, v = ref.norm(b, res, self.weight, kind=np.float32)
+        return res, v.astype(np.float16), ref.gemm4(v.astype(np.float16), ref.weights4(self.codes4, self.scales4, None, 64))
+
+    def check(self, x, res):
+        import torch
+        torch.cuda.synchronize()
+        res, y, (logits, off) = self.want(x, res)
+        same(self.res.cpu().numpy(), res)
+        same(self.y.cpu().numpy(), y)
+        assert (np.abs(self.logits.cpu().numpy() - logits) <= off + 2.0 ** -24 * np.abs(logits)).all()
+
+
+@pytest.mark.parametrize("M", [1, 5, 70])
+def test_a_block_on_8_bit_rows(M):
+    rng = np.random.default_rng(M)
+    block = Block(M, 320, 808, 500, 1)
+    for _ in range(2):
+        x, res = values(rng, M, 320), values(rng, M, 320, np.float32, 2.0)
+        block.set(x, res)
+        block.run()
+        block.check(x, res)
+
+
+def test_a_captured_block_on_another_stream():
+    import torch
+    rng = np.random.default_rng(3)
+    block, other = Block(3, 256, 512, 300, 2), Block(2, 192, 256, 100, 3)
+    side = torch.cuda.Stream()
+    x, res = values(rng, 3, 256), values(rng, 3, 256, np.float32)
+    block.set(x, res)
+    other.set(values(rng, 2, 192), values(rng, 2, 192, np.float32))
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        block.run()
+    side.synchronize()
+    block.check(x, res)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        block.run()
+    for _ in range(3):
+        x, res = values(rng, 3, 256), values(rng, 3, 256, np.float32)
+        block.set(x, res)
+        graph.replay()
+        torch.cuda.synchronize()
+        block.check(x, res)
+        other.run()                                        # eager work between the replays
+        torch.cuda.synchronize()
+    block.set(x, res)
+    torch.cuda.synchronize()
+    block.run(side)                                        # a stream by hand
+    block.check(x, res)
+
+
+def test_results_do_not_change_from_call_to_call():
+    import torch
+    block = Block(33, 512, 1024, 1000, 4)
+    rng = np.random.default_rng(5)
+    x, res = values(rng, 33, 512), values(rng, 33, 512, np.float32)
+    found = []
+    for _ in range(3):
+        block.set(x, res)
+        block.run()
+        torch.cuda.synchronize()
+        found.append([t.cpu().numpy().copy() for t in (block.res, block.y, block.logits)])
+    for other in found[1:]:
+        for a, b in zip(found[0], other):
+            same(a, b)
+
+
+def test_calls_of_no_rows():
+    import torch
+    e = lambda n, t=torch.float16: torch.empty((0, n), dtype=t, device="cuda")  # noqa: E731
+    r = tl.make_rows8(e(64, torch.int8), torch.empty(0, device="cuda"), 64)
+    tl.tl_norm(tl.make_norm_job(e(64), e(64), e(64), None, e(64), r))
+    tl.tl_gate(tl.make_gate_job(e(64), e(64), e(64), r))
+
+
+def test_binding_refuses_what_does_not_fit():
+    import torch
+    z = lambda *s, t=torch.float16: torch.zeros(s, dtype=t, device="cuda")  # noqa: E731
+    r = tl.make_rows8(z(4, 64, t=torch.int8), z(4, t=torch.float32), 60)
+    for bad in (lambda: tl.make_rows8(z(4, 48, t=torch.int8), z(4, t=torch.float32), 60), lambda: tl.make_rows8(z(4, 64, t=torch.int8), z(5, t=torch.float32), 60),
+                lambda: tl.make_rows8(z(4, 64), z(4, t=torch.float32), 60), lambda: tl.make_norm_job(z(4, 60), z(4, 61)), lambda: tl.make_norm_job(z(4, 64), out=r),
+                lambda: tl.make_norm_job(z(4, 60), z(4, 60), z(4, 60, t=torch.float32)), lambda: tl.make_norm_job(z(4, 60), sum=z(4, 60)),
+                lambda: tl.make_norm_job(z(4, 60), weight=z(61), out=r), lambda: tl.make_norm_job(z(60, 4).t(), out=r), lambda: tl.make_gate_job(z(3, 60), z(4, 60), None, r),
+                lambda: tl.make_gate_job(None, z(4, 60), z(4, 60, t=torch.float32)), lambda: tl.make_rows8_jobs([(r, z(8, 5, t=torch.int32), 0, z(4, 8))]),
+                lambda: tl.make_rows8_jobs([(r, z(8, 4, t=torch.int32), 0, z(5, 8))]), lambda: tl.make_4bit_job(z(2, 64), z(8, 16, t=torch.int32), z(2, 8), None, 64, z(2, 8)),
+                lambda: tl.make_4bit_job(z(2, 64), z(8, 8, t=torch.int32), z(1, 8), None, 64, z(2, 8)), lambda: tl.make_4bit_job(z(2, 64), z(8, 16, t=torch.int32), z(1, 8), z(1, 8), 64, z(2, 8))):
+        with pytest.raises(ValueError):
+            bad()
