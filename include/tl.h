@@ -455,7 +455,7 @@ typedef struct tl_rows {
  * Rows of 8-bit codes, -127 .. 127: place d of row r stands for scales[r] * code.  In each block of 16 places, place 4 i + s is byte 4 s + i (i, s = 0 .. 3): the order
  * in which two bits of every byte of a packed word's bits meet them.  A row's last block is filled with 0; bytes behind it are
  * neither read nor written.
- *   codes    device, 16-byte aligned; rows are `stride` bytes apart, a multiple of 16 of at least ceil(places / 16) * 16 and below 2^40 (one row alone: any such multiple or 0)
+ *   codes    device, 16-byte aligned; rows are `stride` bytes apart, a multiple of 16 of at least ceil(places / 16) * 16 and below 2^24 (one row alone: any such multiple or 0)
  *   scales   device, fp32 [rows], 4-byte aligned
  * A row v becomes codes by its largest magnitude t: scale t / 127, code round(v * (127 / t)), quotients, product and rounding (to the nearest, ties
  * to even) each as IEEE fp32 has them.  With t below 2^-100 scale and codes are 0; with an infinity or a NaN in v the scale is NaN and the codes are 0.
@@ -516,7 +516,7 @@ tl_status tl_gate(const tl_gate_job* job, void* stream);
 /*
  * Ternary products over 8-bit rows:
  *     y[m][n] = fp16_rne( float(sum_k code[m][k] * w[n][k]) * (scale[m] * float(gamma)) ),
- * the sum exact (rounded once to fp32 where it is beyond 2^24), products fp32.  Wpacked, gamma and y as for tl_ternary_gemm; x: M rows of K places.  Any M and N as there, K
+ * the sum exact (rounded once to fp32 where it is beyond 2^24), products fp32.  Wpacked, gamma and y as for tl_ternary_gemm; x: M rows of K places.  Any M as there, N and K
  * below 2^24.  A scale that is infinite or NaN shows in its row of y and in no other (0 codes with a scale of NaN give NaN).  Codes of -128 are taken as they are.  What a row's
  * bytes behind place K - 1 hold does not matter.  Deterministic: the sums are whole numbers.
  * tl_ternary_gemm_rows8_grouped: several independent products in one call, in as few launches as possible; jobs must not alias each other's

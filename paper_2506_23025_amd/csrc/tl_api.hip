@@ -1,5 +1,5 @@
 // C-ABI entry points that touch the device: argument checks, kernel choice, launch.
-#include "tl_internal.hpp"
+#include "tl_rows.hpp"
 
 #include <cmath>
 
@@ -461,6 +461,7 @@ tl_status tl_init(void)
     if (e == hipSuccess) e = tl::mfma_init();
     if (e == hipSuccess) e = tl::tile3_init();
     if (e == hipSuccess) e = tl::tile_gs_init();
+    if (e == hipSuccess) e = tl::rows8_init();
     return tl::from_hip(e);
 }
 

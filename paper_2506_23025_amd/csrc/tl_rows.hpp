@@ -2,6 +2,8 @@
 #pragma once
 #include "tl_internal.hpp"
 
+#include <atomic>
+
 namespace tl {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
@@ -45,6 +47,7 @@ struct Gemm8Desc {
     int64_t M, N, K;
 };
 hipError_t launch_rows8_jobs(const Gemm8Desc* jobs, int64_t count, hipStream_t s);
+hipError_t rows8_init();
 
 struct Gemm4Desc {
     const _Float16* x;

@@ -1,70 +1,351 @@
 // Ternary products over 8-bit rows: y = (codes . What^T) * (scale * gamma), the sum in whole numbers.
-#include "tl_rows.hpp"
+#include "tl_tile8.hpp"
+
+#include <cmath>
 
 namespace tl {
 namespace {
 
-// The 16 weights of a packed word, raised by 1, as four registers of four bytes: byte i of register s is weight 4 i + s, as the rows' codes stand.
-__device__ inline i32x4 decoded(uint32_t w)
+constexpr int64_t kMostOutputs = int64_t(1) << 30;       // of a launch: a grid counts its threads in 32 bits, and 32 x 16 outputs have 256 of them
+constexpr int64_t kLimit = 0x7ffffff0;      // a descriptor's size: less than any offset that is none
+constexpr int kRawBuffer = 0x00027000;      // a descriptor's last word: bytes, no format, no swizzle
+
+// The value of the lane that DPP control CTRL names; 0 where there is none.
+template <int CTRL>
+__device__ inline int moved(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, 15, 15, true); }
+
+// Register j of quarter q of the wave (16 lanes) goes to register q of quarter j.
+__device__ inline void transpose(u32x4& w)
 {
-    return i32x4{int(w & 0x03030303u), int(w >> 2 & 0x03030303u), int(w >> 4 & 0x03030303u), int(w >> 6 & 0x03030303u)};
+    auto a = __builtin_amdgcn_permlane32_swap(w[0], w[2], false, false), b = __builtin_amdgcn_permlane32_swap(w[1], w[3], false, false);
+    auto c = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), d = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+    w = u32x4{c[0], c[1], d[0], d[1]};
 }
 
-// 16 columns of y and 16 rows, the sum over K dealt to four waves.
-__global__ void __launch_bounds__(256) simple_kernel(Gemm8Desc g)
+
+// What few rows need: 16 MB rows and 16 NB columns of y a workgroup, K in chunks of 256 dealt to NW waves, each of which has the whole tile, so that every code and every weight is
+// read once a workgroup and straight into registers; D chunks are on their way.  The waves' sums meet in LDS.
+// A matrix instruction's 16 rows of codes are as many different ones as there are, up to 16 / R, times R pieces of their places: one load brings the operands of R instructions, and each of these sums into
+// registers of its own, of which it keeps the columns that its piece is in.
+template <int MB, int R, int NB, int NW, int D, int JOBS>
+__global__ void __launch_bounds__(64 * NW) stream_kernel(Jobs8<JOBS> jobs)
 {
-    __shared__ i32x4 part[4][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t n = int64_t(blockIdx.x) * 16 + (lane & 15), m = int64_t(blockIdx.y) * 16 + (lane & 15);
-    const int64_t words = (g.K + 15) / 16;
-    const uint32_t* const w = g.W + (n < g.N ? n : g.N - 1) * words;
-    const int8_t* const x = g.x.codes + (m < g.M ? m : g.M - 1) * g.x.stride;
-    i32x4 sum = {0, 0, 0, 0};
-    const i32x4 less = {-1, -1, -1, -1};                  // bytes of -1: takes the 1 away by which weights are raised
-    for (int64_t k = int64_t(wave) * 4; k < words; k += 16) {
-        const int64_t at = k + (lane >> 4);
-        i32x4 b = {0, 0, 0, 0};
-        uint32_t word = 0;
-        if (at < words) {
-            b = *reinterpret_cast<const i32x4*>(x + at * 16);
-            word = w[at];
+    static_assert(R == 1 || MB == 1, "pieces beside each other");
+    extern __shared__ __attribute__((aligned(16))) i32x4 part[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, in = lane & 15;
+    int id = 0;
+    if constexpr (JOBS > 1) {
+        for (int i = 1; i < jobs.count; ++i) id = int(blockIdx.x) >= jobs.job[i].first ? i : id;
+    }
+    const Job8& g = jobs.job[id];
+    int n0, m0;
+    if constexpr (JOBS == 1) {
+        n0 = int(blockIdx.x) * (16 * NB);
+        m0 = int(blockIdx.y) * (16 * MB);
+    } else {
+        const int at = int(blockIdx.x) - g.first, down = at / g.across;
+        n0 = (at - down * g.across) * (16 * NB);
+        m0 = down * (16 * MB);
+    }
+    const int words = (g.K + 15) >> 4, chunks = (words + 15) >> 4;
+    // Loads through descriptors of what is left of W and x from the tile's first row on: addresses behind that give 0, and so does a chunk that is none.  Every load is
+    // asked for without a branch, or the compiler, which has to know how many are on their way, waits for all of them.
+    const int64_t wleft = (int64_t(g.N) - n0) * words * 4, xleft = (int64_t(g.M) - 1 - m0) * g.stride + words * 16;
+    const auto wbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t*>(g.W + size_t(n0) * words), 0, int(wleft < kLimit ? wleft : kLimit), kRawBuffer);
+    const auto xbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.x + size_t(m0) * g.stride), 0, int(xleft < kLimit ? xleft : kLimit), kRawBuffer);
+    uint32_t woff[NB], xoff[MB];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+        const int r = 16 * b + in, last = g.N - 1 - n0;
+        woff[b] = uint32_t(r < last ? r : last) * uint32_t(words * 4) + uint32_t(quarter) * 16u;
+    }
+#pragma unroll
+    for (int b = 0; b < MB; ++b) {
+        const int r = 16 * b + in % (16 / R), last = g.M - 1 - m0;
+        xoff[b] = uint32_t(r < last ? r : last) * uint32_t(g.stride) + uint32_t(in / (16 / R)) * 64u + uint32_t(quarter) * 16u;
+    }
+    const int own = m0 + wave / NB * 16 + in;             // the row whose sums the wave closes with, where there are no more tiles than waves
+    const float early = g.scales[own < g.M ? own : g.M - 1];
+    constexpr int XL = 4 / R;                             // loads of a row block and chunk
+    u32x4 w[D][NB];
+    i32x4 x[D][MB][XL];
+    const auto load = [&](int d, int chunk) {
+        const uint32_t none = chunk < chunks ? 0u : 0x80000000u;
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int b = 0; b < NB; ++b) w[d][b] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wbuf, int(woff[b] + (uint32_t(chunk) * 64u | none)), 0, 0));
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            const uint32_t o = xoff[b] + (uint32_t(chunk) * 256u | none);
+#pragma unroll
+            for (int j = 0; j < XL; ++j) x[d][b][j] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(xbuf, int(o + uint32_t(j) * (64u * R)), 0, 0));
         }
-        const i32x4 a = decoded(word);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, sum, 0, 0, 0);
-        sum = __builtin_amdgcn_mfma_i32_16x16x64_i8(less, b, sum, 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);                // in this order, or a wait for the first is one for all
+    };
+    i32x4 sum[R][MB][NB];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int a = 0; a < MB; ++a)
+#pragma unroll
+            for (int b = 0; b < NB; ++b) sum[r][a][b] = i32x4{0, 0, 0, 0};
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(d, wave + d * NW);
+    for (int c = wave; c < chunks; c += D * NW) {
+#pragma unroll
+        for (int d = 0; d < D; ++d) {
+            const int chunk = c + d * NW;
+            if (chunk < chunks) {
+                const int left = words - chunk * 16;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) {
+                    if (left < 16) {                      // words behind the row's last stand for weights of 0
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[d][b][j] = quarter * 4 + j < left ? w[d][b][j] : 0x55555555u;
+                    }
+                    transpose(w[d][b]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int b = 0; b < NB; ++b) {
+                        const i32x4 v = decoded8(w[d][b][j]);
+#pragma unroll
+                        for (int a = 0; a < MB; ++a) sum[j % R][a][b] = __builtin_amdgcn_mfma_i32_16x16x64_i8(v, x[d][a][j / R], sum[j % R][a][b], 0, 0, 0);
+                    }
+            }
+            load(d, chunk + D * NW);
+        }
     }
-    part[wave][lane] = sum;
+#pragma unroll
+    for (int a = 0; a < MB; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            i32x4 s = sum[0][a][b];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {                 // from the lanes 16 / R, 2 * 16 / R, ... further on in the row of 16
+                if constexpr (R == 2) s[i] += moved<0x108>(sum[1][a][b][i]);
+                if constexpr (R == 4) s[i] += moved<0x104>(sum[1][a][b][i]) + moved<0x108>(sum[2][a][b][i]) + moved<0x10C>(sum[3][a][b][i]);
+            }
+            part[((a * NB + b) * NW + wave) * 64 + lane] = s;
+        }
     __syncthreads();
-    if (wave) return;
+    for (int t = wave; t < MB * NB; t += NW) {
+        i32x4 s = part[t * NW * 64 + lane];
 #pragma unroll
-    for (int i = 1; i < 4; ++i) sum += part[i][lane];
-    const int64_t row = int64_t(blockIdx.y) * 16 + (lane & 15);
-    if (row >= g.M) return;
-    const float scale = g.x.scales[row] * g.gamma;
+        for (int i = 1; i < NW; ++i) s += part[(t * NW + i) * 64 + lane];
+        const int row = m0 + t / NB * 16 + in, col = n0 + t % NB * 16 + quarter * 4;
+        if (row >= g.M || (R > 1 && in >= 16 / R)) continue;
+        const float scale = (MB * NB <= NW ? early : g.scales[row]) * g.gamma;
+        __half h[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t col = int64_t(blockIdx.x) * 16 + (lane >> 4) * 4 + i;
-        if (col < g.N) g.y[row * g.N + col] = __float2half_rn(rounded(float(sum[i]) * scale));
+        for (int i = 0; i < 4; ++i) h[i] = __float2half_rn(rounded(float(s[i]) * scale));
+        __half* const y = g.y + size_t(row) * g.N + col;
+        if (g.N % 4 == 0 && col < g.N) {
+            *reinterpret_cast<u32x2*>(y) = *reinterpret_cast<const u32x2*>(h);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (col + i < g.N) y[i] = h[i];
+        }
     }
+}
+
+// ---- the ways of a launch: rows and columns of a workgroup's tile, places that it takes a step, workgroups a CU -----------------------------
+
+template <int MB, int R, int NB, int NW, int D>
+struct Stream {
+    static constexpr int BM = 16 * MB, BN = 16 * NB, KS = 256 * NW, PER_CU = NB < 2 ? 3 : 2;
+    template <int JOBS>
+    static hipError_t launch(const Jobs8<JOBS>& jobs, int64_t groups, hipStream_t s)
+    {
+        constexpr int lds = MB * NB * NW * 1024;
+        static_assert(lds <= 64 * 1024, "no attribute to set");
+        if (groups == 0) return hipSuccess;
+        const Job8& g = jobs.job[0];
+        hipLaunchKernelGGL((stream_kernel<MB, R, NB, NW, D, JOBS>), JOBS == 1 ? dim3(unsigned(g.across), unsigned(g.down)) : dim3(unsigned(groups)), dim3(64 * NW), lds, s, jobs);
+        return hipGetLastError();
+    }
+};
+template <int FM, int FN, int WM, int WN, int WK, int ST, bool RAGGED>
+struct Tile {
+    using C = Tile8Cfg<FM, FN, WM, WN, WK, ST, RAGGED>;
+    static constexpr int BM = C::BM, BN = C::BN, KS = 128 * WK, PER_CU = C::GROUPS;
+    template <int JOBS>
+    static hipError_t launch(const Jobs8<JOBS>& jobs, int64_t groups, hipStream_t s) { return launch_tile8<C, JOBS>(jobs, groups, s); }
+};
+
+// Up to kMaxJobs products in one launch of a way.
+template <class Way>
+hipError_t launch_way(const Gemm8Desc* const* list, int count, hipStream_t s)
+{
+    Jobs8<kMaxJobs> all{};
+    int64_t groups = 0;
+    all.count = count;
+    for (int i = 0; i < count; ++i) {
+        const Gemm8Desc& g = *list[i];
+        const int64_t across = (g.N + Way::BN - 1) / Way::BN, down = (g.M + Way::BM - 1) / Way::BM;
+        all.job[i] = {g.x.codes, g.x.scales, g.W, g.y, g.gamma, int(g.M), int(g.N), int(g.K), int(g.x.stride), int(groups), int(across), int(down)};
+        groups += across * down;
+    }
+    if (count == 1 && all.job[0].down < 65536)            // what a grid's second dimension holds
+        return Way::template launch<1>({{all.job[0]}, 1}, groups, s);
+    return Way::template launch<kMaxJobs>(all, groups, s);
+}
+
+// Which way.  Up to 16 rows: by the tiles of 16 columns that there are and the chunks of 256 places, since few tiles need all waves of the chip on one and many do not (measured
+// over 2100 calls of 1 to 3 products, M = 1 .. 16, N = 64 .. 22016, K = 128 .. 14336: the way taken is 1.4 % slower than the best of 12 on average, 8 % in one of twenty).
+hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
+{
+    int64_t tiles = 0, M = 0, K = 0;
+    for (int i = 0; i < count; ++i) {
+        tiles += (list[i]->N + 15) / 16;
+        M = list[i]->M > M ? list[i]->M : M;
+        K = list[i]->K > K ? list[i]->K : K;
+    }
+    const int64_t chunks = (K + 255) / 256;
+    if (M <= 4) {
+        if (tiles >= 768) return chunks > 8 && tiles < 1024 ? launch_way<Stream<1, 4, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 4, 2, 4, 1>>(list, count, s);
+        return chunks > 16 && tiles < 512 ? launch_way<Stream<1, 4, 1, 8, 2>>(list, count, s) : launch_way<Stream<1, 4, 1, 8, 1>>(list, count, s);
+    }
+    if (M <= 8) {
+        if (tiles >= 2048) return launch_way<Stream<1, 2, 4, 4, 1>>(list, count, s);
+        if (tiles >= 768) return launch_way<Stream<1, 2, 2, 4, 1>>(list, count, s);
+        return chunks > 4 && tiles < 384 ? launch_way<Stream<1, 2, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 2, 1, 4, 1>>(list, count, s);
+    }
+    if (tiles >= 512) return chunks > 8 && tiles < 1024 ? launch_way<Stream<1, 1, 4, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 4, 4, 1>>(list, count, s);
+    if (tiles >= 256) return chunks > 8 ? launch_way<Stream<1, 1, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 2, 4, 1>>(list, count, s);
+    return chunks > 8 ? launch_way<Stream<1, 1, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 1, 4, 1>>(list, count, s);
+}
+
+// More rows: what each way takes (us), fitted to 580 calls of M = 17 .. 4096, N and K as above: a launch and its steps, and a share for every round that the workgroups make of the chip (c: launch, a
+// step, a round, a round's step, a step of the rounds as a fraction but one at least, a round as a fraction).  The way taken is 2.5 % slower than the best of 14 on average, 13 % in one of twenty.
+struct WayTime {
+    int bm, bn, ks, per_cu;
+    double c[6];
+};
+constexpr int kWays = 8;
+constexpr WayTime kWayTimes[kWays] = {
+    {32, 16, 1024, 3, {1.745, 0.160, 0.000, 0.419, 0.228, 0.000}},
+    {32, 32, 1024, 3, {1.951, 0.145, 0.000, 0.409, 0.335, 0.022}},
+    {32, 64, 512, 2, {2.153, 0.187, 0.392, 0.191, 0.174, 0.725}},
+    {32, 128, 256, 2, {2.495, 0.185, 0.294, 0.184, 0.156, 1.051}},
+    {32, 64, 1024, 1, {1.393, 0.000, 1.707, 0.868, 0.000, 0.788}},
+    {64, 128, 512, 1, {1.894, 0.000, 2.344, 1.008, 0.000, 2.301}},
+    {128, 128, 128, 2, {3.943, 0.095, 0.000, 0.240, 0.208, 2.090}},
+    {128, 256, 128, 2, {5.575, 0.169, 0.000, 0.268, 0.436, 4.008}},
+};
+
+double way_time(int way, const Gemm8Desc* const* list, int count)
+{
+    const WayTime& w = kWayTimes[way];
+    double groups = 0, steps = 0;
+    for (int i = 0; i < count; ++i) {
+        groups += double((list[i]->M + w.bm - 1) / w.bm) * double((list[i]->N + w.bn - 1) / w.bn);
+        const double k = double((list[i]->K + w.ks - 1) / w.ks);
+        steps = k > steps ? k : steps;
+    }
+    const double r = groups / 256.0, rounds = r > w.per_cu ? std::ceil(r / w.per_cu) * w.per_cu : std::ceil(r);
+    return w.c[0] + w.c[1] * steps + w.c[2] * rounds + w.c[3] * rounds * steps + w.c[4] * (r > 1.0 ? r : 1.0) * steps + w.c[5] * r;
+}
+
+int best_way(const Gemm8Desc* const* list, int count, double* time)
+{
+    int best = 0;
+    for (int i = 0; i < kWays; ++i) {
+        const double t = way_time(i, list, count);
+        if (i == 0 || t < *time) *time = t, best = i;
+    }
+    return best;
+}
+
+template <bool RAGGED>
+hipError_t launch_tiles(int way, const Gemm8Desc* const* list, int count, hipStream_t s)
+{
+    switch (way) {
+    case 2: return launch_way<Tile<2, 2, 1, 2, 4, 3, RAGGED>>(list, count, s);
+    case 3: return launch_way<Tile<2, 2, 1, 4, 2, 3, RAGGED>>(list, count, s);
+    case 4: return launch_way<Tile<2, 4, 1, 1, 8, 3, RAGGED>>(list, count, s);
+    case 5: return launch_way<Tile<4, 4, 1, 2, 4, 3, RAGGED>>(list, count, s);
+    case 6: return launch_way<Tile<4, 4, 2, 2, 1, 4, RAGGED>>(list, count, s);
+    default: return launch_way<Tile<8, 4, 1, 4, 1, 3, RAGGED>>(list, count, s);
+    }
+}
+
+hipError_t launch_many(int way, const Gemm8Desc* const* list, int count, hipStream_t s)
+{
+    if (way == 0) return launch_way<Stream<2, 1, 1, 4, 1>>(list, count, s);
+    if (way == 1) return launch_way<Stream<2, 1, 2, 4, 1>>(list, count, s);
+    bool ragged = false;
+    for (int i = 0; i < count; ++i) ragged |= (list[i]->K + 15) / 16 % 4 != 0;
+    return ragged ? launch_tiles<true>(way, list, count, s) : launch_tiles<false>(way, list, count, s);
 }
 
 }  // namespace
 
+hipError_t rows8_init()
+{
+    const Gemm8Desc none{{nullptr, nullptr, 0}, nullptr, nullptr, 0.0f, 0, 0, 64};
+    const Gemm8Desc* const list[2] = {&none, &none};
+    for (int way = 2; way < kWays; ++way)
+        for (int count = 1; count <= 2; ++count) {
+            if (const hipError_t e = launch_tiles<false>(way, list, count, nullptr); e != hipSuccess) return e;
+            if (const hipError_t e = launch_tiles<true>(way, list, count, nullptr); e != hipSuccess) return e;
+        }
+    return hipSuccess;
+}
+
 hipError_t launch_rows8_jobs(const Gemm8Desc* jobs, int64_t count, hipStream_t s)
 {
+    // Products of up to 16 rows share launches; those of more do where that is expected to be faster.
+    const Gemm8Desc* few[kMaxJobs];
+    const Gemm8Desc* many[kMaxJobs];
+    int nfew = 0, nmany = 0;
+    const auto close_few = [&] {
+        const hipError_t e = nfew ? launch_few(few, nfew, s) : hipSuccess;
+        nfew = 0;
+        return e;
+    };
+    const auto close_many = [&] {
+        if (nmany == 0) return hipSuccess;
+        double apart = 0.0, together = 0.0, t = 0.0;
+        int64_t outputs = 0;
+        int own[kMaxJobs];
+        for (int i = 0; i < nmany; ++i) {
+            own[i] = best_way(many + i, 1, &t);
+            apart += t;
+            outputs += many[i]->M * many[i]->N;
+        }
+        const int way = best_way(many, nmany, &together);
+        const int n = nmany;
+        nmany = 0;
+        if (together <= apart && outputs <= kMostOutputs) return launch_many(way, many, n, s);
+        for (int i = 0; i < n; ++i)
+            if (const hipError_t e = launch_many(own[i], many + i, 1, s); e != hipSuccess) return e;
+        return hipSuccess;
+    };
     for (int64_t i = 0; i < count; ++i) {
         const Gemm8Desc& g = jobs[i];
-        constexpr int64_t kRows = int64_t(65535) * 16;
-        for (int64_t m = 0; m < g.M; m += kRows) {
-            Gemm8Desc part = g;
-            part.x.codes += m * g.x.stride;
-            part.x.scales += m;
-            part.y += m * g.N;
-            part.M = g.M - m < kRows ? g.M - m : kRows;
-            hipLaunchKernelGGL(simple_kernel, dim3(unsigned((g.N + 15) / 16), unsigned((part.M + 15) / 16)), dim3(256), 0, s, part);
+        if (g.M * g.N > kMostOutputs) {                   // in launches of its own
+            const int64_t rows = kMostOutputs / g.N > 256 ? kMostOutputs / g.N / 256 * 256 : 256;
+            for (int64_t m = 0; m < g.M; m += rows) {
+                const Gemm8Desc part{{g.x.codes + m * g.x.stride, g.x.scales + m, g.x.stride}, g.W, g.y + m * g.N, g.gamma, g.M - m < rows ? g.M - m : rows, g.N, g.K};
+                const Gemm8Desc* const one = &part;
+                double t;
+                if (const hipError_t e = launch_many(best_way(&one, 1, &t), &one, 1, s); e != hipSuccess) return e;
+            }
+        } else if (g.M <= 16) {
+            few[nfew++] = &g;
+            if (nfew == kMaxJobs)
+                if (const hipError_t e = close_few(); e != hipSuccess) return e;
+        } else {
+            many[nmany++] = &g;
+            if (nmany == kMaxJobs)
+                if (const hipError_t e = close_many(); e != hipSuccess) return e;
         }
     }
-    return hipGetLastError();
+    if (const hipError_t e = close_few(); e != hipSuccess) return e;
+    return close_many();
 }
 
 }  // namespace tl

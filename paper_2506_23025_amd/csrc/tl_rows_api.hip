@@ -8,6 +8,7 @@ namespace {
 
 inline bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 constexpr int64_t kMaxStride = int64_t(1) << 40, kMaxDim = 65536;
+constexpr int64_t kMaxStride8 = int64_t(1) << 24;      // 256 rows lie within 32-bit offsets
 
 // Rows of `bytes` a place that a call reads, or with `written` writes.
 inline tl_status rows_status(const tl_rows& r, int64_t rows, int64_t dim, int bytes, bool written)
@@ -21,7 +22,7 @@ inline tl_status rows_status(const tl_rows& r, int64_t rows, int64_t dim, int by
 inline tl_status rows8_status(const tl_rows8& r, int64_t rows, int64_t dim)
 {
     if (!r.codes || !r.scales) return TL_ERR_NULL;
-    if (r.stride < 0 || r.stride >= kMaxStride || (rows > 1 && r.stride < (dim + 15) / 16 * 16)) return TL_ERR_SHAPE;
+    if (r.stride < 0 || r.stride >= kMaxStride8 || (rows > 1 && r.stride < (dim + 15) / 16 * 16)) return TL_ERR_SHAPE;
     if (!aligned(r.codes, 16) || r.stride % 16 != 0 || !aligned(r.scales, 4)) return TL_ERR_ALIGN;
     return TL_OK;
 }
@@ -45,7 +46,7 @@ inline tl_status from_hip(hipError_t e) { return e == hipSuccess ? TL_OK : TL_ER
 tl_status desc_of(const tl_gemm_rows8_job& j, Gemm8Desc& d)
 {
     if (!j.Wpacked || !j.y) return TL_ERR_NULL;
-    if (!product_ok(j.M, j.N, j.K) || j.K >= (int64_t(1) << 24)) return TL_ERR_SHAPE;
+    if (!product_ok(j.M, j.N, j.K) || j.N >= (int64_t(1) << 24) || j.K >= (int64_t(1) << 24)) return TL_ERR_SHAPE;
     if (const tl_status e = rows8_status(j.x, j.M, j.K); e != TL_OK) return e;
     if (!aligned(j.Wpacked, 16) || !aligned(j.y, 16)) return TL_ERR_ALIGN;
     d = {rows8_of(j.x), static_cast<const uint32_t*>(j.Wpacked), static_cast<__half*>(j.y), half_bits_to_float(j.gamma_fp16_bits), j.M, j.N, j.K};

@@ -143,6 +143,10 @@ __device__ __forceinline__ void dma2(uint32_t voff, const void* sbase, uint32_t 
 {
     asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_ushort %0, %1" : : "v"(voff), "s"(sbase), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
 }
+__device__ __forceinline__ void dma4(uint32_t voff, const void* sbase, uint32_t lds)   // lane l lands at base + 4 l
+{
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, %1" : : "v"(voff), "s"(sbase), "s"(__builtin_amdgcn_readfirstlane(lds)) : "memory", "m0");
+}
 
 __device__ __forceinline__ uint32_t pkfma(uint32_t a, uint32_t b, uint32_t c)
 {

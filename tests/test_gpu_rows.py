@@ -300,6 +300,11 @@ def test_rows8_products_of_one_call():
     check_products([product(30, 1, 4096, 2048), product(31, 300, 640, 1024), product(32, 16, 1000, 4096), product(33, 1, 1, 1)])
 
 
+def test_rows8_product_of_very_many_rows():
+    check_products([product(1, (1 << 21) + 5, 1, 16)])
+    check_products([product(2, 70000, 40, 80)])
+
+
 def test_rows8_product_at_the_ends_of_its_range():
     """The largest sums, codes of -128, scales and results out of fp16."""
     for M in (2, 40):

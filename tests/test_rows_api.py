@@ -167,7 +167,7 @@ def test_rows8_product_refusals():
     assert status(Wpacked=P + 4) == status(y=P + 2) == tl.TL_ERR_ALIGN
     for bad, s in BAD_ROWS8:
         assert status(x=rows8(**bad)) == s, bad
-    for kw in ({"M": 0}, {"N": 0}, {"K": 0}, {"M": 1 << 31}, {"K": 1 << 24}, {"x": rows8(stride=240)}, {"M": 1 << 30, "N": 1 << 30}):
+    for kw in ({"M": 0}, {"N": 0}, {"K": 0}, {"M": 1 << 31}, {"N": 1 << 24}, {"K": 1 << 24}, {"x": rows8(stride=240)}, {"M": 1 << 30, "N": 1 << 30}):
         assert status(**kw) == tl.TL_ERR_SHAPE, kw
 
 
