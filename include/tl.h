@@ -562,7 +562,7 @@ tl_status tl_unpack_4bit(const uint32_t* packed, int64_t N, int64_t K, uint8_t* 
  *   scales   device, fp16 [ceil(K / group)][N], 16-byte aligned;  zeros: device, uint8 of the same shape, 16-byte aligned (any byte is taken as it is), or NULL
  *   y        device, fp16 or fp32 [M][N], 16-byte aligned
  *   group    a multiple of 32; the last group may be short
- * Any M, N, K >= 1; made for few rows (weights are streamed once for every 64).  A NaN or an infinity in row m of x shows in row m of y and in no other, one in a scale in its
+ * Any M >= 1, N below 2^24, K below 2^20; made for few rows (weights are streamed once for every 64).  A NaN or an infinity in row m of x shows in row m of y and in no other, one in a scale in its
  * column.  Deterministic: no atomics, fixed order.
  */
 typedef struct tl_gemm_4bit_job {

@@ -462,6 +462,7 @@ tl_status tl_init(void)
     if (e == hipSuccess) e = tl::tile3_init();
     if (e == hipSuccess) e = tl::tile_gs_init();
     if (e == hipSuccess) e = tl::rows8_init();
+    if (e == hipSuccess) e = tl::four_init();
     return tl::from_hip(e);
 }
 

@@ -4,18 +4,26 @@
 namespace tl {
 namespace {
 
+constexpr int64_t kLimit = 0x7ffffff0;      // a descriptor's size: less than any offset that is none
+constexpr int kRawBuffer = 0x00027000;      // a descriptor's last word: bytes, no format, no swizzle
+
 // The eight weights of a packed word in order, less what `less` (the negated 1024 + z twice, and 64 + z twice) holds.  A code in the lowest four bits of fp16's 1024 is 1024 + code,
 // one four bits further up in 64's mantissa 64 + code, and both differences are exact: no shift for half of the codes.
-__device__ inline f16x8 decoded(uint32_t w, f16x2 less1024, f16x2 less64)
-{
-    const auto pair = [](uint32_t u, uint32_t mask, uint32_t base, f16x2 less) { return __builtin_bit_cast(f16x2, (u & mask) | base) + less; };
-    const uint32_t v = w >> 8;
-    const f16x2 a = pair(w, 0x000F000Fu, 0x64006400u, less1024), b = pair(w, 0x00F000F0u, 0x54005400u, less64);
-    const f16x2 c = pair(v, 0x000F000Fu, 0x64006400u, less1024), d = pair(v, 0x00F000F0u, 0x54005400u, less64);
-    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
+// The masks and bases are kept from the compiler, which would write each into two instructions instead of one for both.
+struct Decode {
+    uint32_t mask0 = 0x000F000Fu, mask4 = 0x00F000F0u, base1024 = 0x64006400u, base64 = 0x54005400u;
+    __device__ Decode() { asm("" : "+s"(mask0), "+s"(mask4), "+v"(base1024), "+v"(base64)); }
+    __device__ inline f16x8 operator()(uint32_t w, f16x2 less1024, f16x2 less64) const
+    {
+        const auto pair = [](uint32_t u, uint32_t mask, uint32_t base, f16x2 less) { return __builtin_bit_cast(f16x2, (u & mask) | base) + less; };
+        const uint32_t v = w >> 8;
+        const f16x2 a = pair(w, mask0, base1024, less1024), b = pair(w, mask4, base64, less64);
+        const f16x2 c = pair(v, mask0, base1024, less1024), d = pair(v, mask4, base64, less64);
+        return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+    }
+};
 
-// 16 columns of y and 16 rows, the groups dealt to four waves.
+// Rows of less than eight places, which is what the other kernel fetches at a time: 16 columns of y and 16 rows, the groups dealt to four waves.
 __global__ void __launch_bounds__(256) simple_kernel(Gemm4Desc g)
 {
     __shared__ f32x4 part[4][64];
@@ -25,6 +33,7 @@ __global__ void __launch_bounds__(256) simple_kernel(Gemm4Desc g)
     const uint32_t* const w = g.W + n * ((g.K + 127) / 128 * 16);
     const _Float16* const x = g.x + m * g.K;
     const int64_t groups = (g.K + g.group - 1) / g.group;
+    const Decode decoded;
     f32x4 total = {0, 0, 0, 0};
     for (int64_t j = wave; j < groups; j += 4) {
         const int z = g.zeros ? g.zeros[j * g.N + n] : 8;
@@ -59,17 +68,272 @@ __global__ void __launch_bounds__(256) simple_kernel(Gemm4Desc g)
     }
 }
 
+typedef u32x4 __attribute__((aligned(2))) u32x4_any;
+
+// Eight fp16 less the first n of them, 0 behind: what a piece that was fetched n values early holds.
+__device__ inline u32x4 shifted(u32x4 v, int n)
+{
+    if (n & 4) v = u32x4{v[2], v[3], 0, 0};
+    if (n & 2) v = u32x4{v[1], v[2], v[3], 0};
+    if (n & 1) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    return n < 8 ? v : u32x4{0, 0, 0, 0};
+}
+
+// Up to MR rows and 16 FN WN columns of y a workgroup.  K goes by chunks of 128, dealt to WK sets of waves; a wave has FN column fragments, and their words, scales and zeros come straight into its
+// registers, D chunks ahead.  Rows of x go through registers into LDS, a panel of CP WK chunks at a time and the next one while a panel is used, since every wave needs all of them.
+// The words are the column operand of the matrix instruction: a lane has one column, so one zero point and one scale.  Sums of UNIT steps of 32 are scaled and added in fp32.
+template <int MR, int FN, int WN, int WK, int CP, int D, int UNIT, bool ZEROS>
+__global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
+{
+    constexpr int FM = (MR + 15) / 16, THREADS = 64 * WN * WK, PK = CP * WK, XL = (MR * PK * 16 + THREADS - 1) / THREADS, FOLDS = 4 / UNIT;
+    static_assert(MR < 16 || MR % 16 == 0, "rows");
+    static_assert(CP % D == 0 || D == 1, "register slots are known to the compiler");
+    extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), quarter = lane >> 4, in = lane & 15;
+    const int set = wave / WN, wn = wave % WN;
+    const int n0 = (int(blockIdx.x) * WN + wn) * (16 * FN), m0 = int(blockIdx.y) * MR;
+    const int K = int(g.K), N = int(g.N);
+    const int chunks = (K + 127) >> 7, panels = (chunks + PK - 1) / PK;
+    const int rows = int(g.M) - m0 < MR ? int(g.M) - m0 : MR;
+    const uint32_t blocks32 = uint32_t(K + 31) >> 5;
+
+    // ---- words, scales and zeros of a chunk ------------------------------------------------------------------
+    const int64_t row_bytes = int64_t(chunks) * 64, wleft = (int64_t(N) - n0) * row_bytes;
+    const auto wbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t*>(g.W) + n0 * (row_bytes / 4), 0, int(wleft < kLimit ? (wleft > 0 ? wleft : 0) : kLimit), kRawBuffer);
+    uint32_t woff[FN], col[FN];
+#pragma unroll
+    for (int f = 0; f < FN; ++f) {
+        const int n = 16 * f + in, last = N - 1 - n0;
+        col[f] = uint32_t(n < last ? n : (last > 0 ? last : 0));
+        woff[f] = col[f] * uint32_t(row_bytes) + uint32_t(quarter) * 16u;
+    }
+    const int nbase = n0 < N ? n0 : N - 1;                // a wave behind the last column looks at that one
+    struct Slot { u32x4 w[FN]; uint16_t s[FN][FOLDS]; uint8_t z[FN][FOLDS]; } slots[D];
+    const auto load = [&](Slot& b, int chunk) {
+        __builtin_amdgcn_sched_barrier(0);
+        const uint32_t o = chunk < chunks ? uint32_t(chunk) * 64u : 0x80000000u;
+#pragma unroll
+        for (int f = 0; f < FN; ++f) b.w[f] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wbuf, int(woff[f] + o), 0, 0));
+#pragma unroll
+        for (int h = 0; h < FOLDS; ++h) {
+            const uint32_t block = uint32_t(chunk * 4 + h * UNIT), group = uint32_t(uint64_t(block < blocks32 ? block : blocks32 - 1) * g.magic >> 31);
+            const int64_t at = int64_t(group) * N + nbase;
+            const char* const sbase = reinterpret_cast<const char*>(g.scales + at);
+            const char* const zbase = reinterpret_cast<const char*>(g.zeros + at);
+#pragma unroll
+            for (int f = 0; f < FN; ++f) {
+                b.s[f][h] = *reinterpret_cast<const uint16_t*>(sbase + col[f] * 2u);
+                if constexpr (ZEROS) b.z[f][h] = *reinterpret_cast<const uint8_t*>(zbase + col[f]);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    // ---- rows of a panel: piece i of a thread is eight places of a row ----------------------------------------------
+    u32x4 xr[XL];
+    const auto fetch = [&](int panel) {
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            const int at = i * THREADS + tid, r = at / (PK * 16), k = panel * (PK * 128) + (at % (PK * 16)) * 8;
+            const int64_t row = int64_t(m0) + (r < rows ? r : rows - 1);
+            xr[i] = *reinterpret_cast<const u32x4_any*>(g.x + row * K + (k < K - 8 ? k : K - 8));
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto place = [&](int panel) {
+#pragma unroll
+        for (int i = 0; i < XL; ++i) {
+            const int at = i * THREADS + tid, r = at / (PK * 16), p = at % (PK * 16), k = panel * (PK * 128) + p * 8;
+            u32x4 v = xr[i];
+            if (K % 8 != 0) v = shifted(v, k < K - 8 ? 0 : k - (K - 8) < 8 ? k - (K - 8) : 8);
+            else v = k < K ? v : u32x4{0, 0, 0, 0};
+            if (MR * PK * 16 % THREADS == 0 || r < MR)
+                *reinterpret_cast<u32x4*>(lds + (panel & 1) * (MR * PK * 256) + r * (PK * 256) + (p >> 4) * 256 + ((p ^ r) & 15) * 16) = v;
+        }
+    };
+    uint32_t xread[4];                                    // of the four steps of a chunk; rows that there are not hold another's places
+    const int xrow = MR < 16 && in >= MR ? MR - 1 : in;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) xread[t] = uint32_t(xrow) * (PK * 256) + uint32_t((4 * t + quarter) ^ xrow) * 16u;
+
+    const Decode decoded;
+    f32x4 total[FM][FN];
+#pragma unroll
+    for (int a = 0; a < FM; ++a)
+#pragma unroll
+        for (int f = 0; f < FN; ++f) total[a][f] = f32x4{0, 0, 0, 0};
+    const auto use = [&](const Slot& b, int panel, int local) {
+        const unsigned char* const xs = lds + (panel & 1) * (MR * PK * 256);
+        // all reads, all decodes, all products: the decodes take as long as the reads do
+        f16x8 x[4][FM], w[4][FN];
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int a = 0; a < FM; ++a) x[t][a] = *reinterpret_cast<const f16x8*>(xs + xread[t] + a * (16 * PK * 256) + local * 256);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                const int h = t / UNIT;
+                const _Float16 z = ZEROS ? _Float16(short(b.z[f][h])) : _Float16(8);
+                const _Float16 less1024 = _Float16(-1024) - z, less64 = _Float16(-64) - z;
+                w[t][f] = decoded(b.w[f][t], f16x2{less1024, less1024}, f16x2{less64, less64});
+            }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 sum[FM][FN];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int f = 0; f < FN; ++f)
+#pragma unroll
+                for (int a = 0; a < FM; ++a) {
+                    sum[a][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[t][a], w[t][f], t % UNIT == 0 ? f32x4{0, 0, 0, 0} : sum[a][f], 0, 0, 0);
+                    if (t % UNIT == UNIT - 1) total[a][f] += sum[a][f] * float(__builtin_bit_cast(_Float16, b.s[f][t / UNIT]));
+                }
+    };
+
+    fetch(0);
+#pragma unroll
+    for (int d = 0; d < D; ++d) load(slots[d], d * WK + set);
+    place(0);
+    __syncthreads();
+    const auto panel = [&](int p) {
+#pragma unroll
+        for (int c = 0; c < CP; ++c) {
+            const int chunk = (p * CP + c) * WK + set;
+            if (chunk < chunks) use(slots[c % D], p, c * WK + set);
+            load(slots[c % D], chunk + D * WK);
+        }
+    };
+    for (int p = 0; p < panels - 1; ++p) {
+        fetch(p + 1);
+        panel(p);
+        place(p + 1);
+        __syncthreads();
+    }
+    panel(panels - 1);
+
+    // ---- the sets' sums, in their order ------------------------------------------------------------------------------
+    const auto put = [&](f32x4 v, int a, int f, int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = a * 16 + quarter * 4 + i;
+            const int64_t c = int64_t(n) + f * 16 + in;
+            if (r >= rows || c >= N) continue;
+            const int64_t at = (int64_t(m0) + r) * N + c;
+            if (g.wide) static_cast<float*>(g.y)[at] = v[i];
+            else static_cast<_Float16*>(g.y)[at] = _Float16(v[i]);
+        }
+    };
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int a = 0; a < FM; ++a)
+#pragma unroll
+            for (int f = 0; f < FN; ++f) put(total[a][f], a, f, n0);
+    } else {
+        constexpr int TILES = WN * FM * FN;
+        f32x4* const part = reinterpret_cast<f32x4*>(lds);
+        __syncthreads();
+#pragma unroll
+        for (int a = 0; a < FM; ++a)
+#pragma unroll
+            for (int f = 0; f < FN; ++f) part[(set * TILES + (wn * FM + a) * FN + f) * 64 + lane] = total[a][f];
+        __syncthreads();
+        for (int t = wave; t < TILES; t += WN * WK) {
+            f32x4 v = part[t * 64 + lane];
+#pragma unroll
+            for (int i = 1; i < WK; ++i) v += part[(i * TILES + t) * 64 + lane];
+            put(v, t / FN % FM, t % FN, (int(blockIdx.x) * WN + t / (FN * FM)) * (16 * FN));
+        }
+    }
+}
+
+template <int MR, int FN, int WN, int WK, int CP, int D>
+struct Four {
+    static constexpr int BN = 16 * FN * WN, PANEL = MR * CP * WK * 256, RED = WK > 1 ? WN * WK * ((MR + 15) / 16) * FN * 1024 : 0;
+    static constexpr int MOST = 2 * PANEL > RED ? 2 * PANEL : RED;
+    static_assert(MOST <= 160 * 1024, "LDS");
+    template <int UNIT, bool ZEROS>
+    static hipError_t launch(const Gemm4Desc& g, hipStream_t s)
+    {
+        if constexpr (MOST > 64 * 1024) {
+            static std::atomic<uint64_t> set{0};
+            const int device = device_slot();
+            if (device < 0 || !(set.load(std::memory_order_relaxed) >> device & 1)) {
+                if (const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(four_kernel<MR, FN, WN, WK, CP, D, UNIT, ZEROS>), hipFuncAttributeMaxDynamicSharedMemorySize, MOST); e != hipSuccess) return e;
+                if (device >= 0) set.fetch_or(uint64_t(1) << device, std::memory_order_relaxed);
+            }
+        }
+        if (g.M == 0) return hipSuccess;
+        const int panels = (g.K + 128 * CP * WK - 1) / (128 * CP * WK) > 1 ? 2 : 1;
+        const int lds = panels * PANEL > RED ? panels * PANEL : RED;
+        hipLaunchKernelGGL((four_kernel<MR, FN, WN, WK, CP, D, UNIT, ZEROS>), dim3(unsigned((g.N + BN - 1) / BN), unsigned((g.M + MR - 1) / MR)), dim3(64 * WN * WK), lds, s, g);
+        return hipGetLastError();
+    }
+    static hipError_t launch(const Gemm4Desc& g, hipStream_t s)
+    {
+        if (g.group % 128 == 0) return g.zeros ? launch<4, true>(g, s) : launch<4, false>(g, s);
+        if (g.group % 64 == 0) return g.zeros ? launch<2, true>(g, s) : launch<2, false>(g, s);
+        return g.zeros ? launch<1, true>(g, s) : launch<1, false>(g, s);
+    }
+};
+
+// Which tile: by the rows, so that none is staged in vain, and by the column tiles of 16 that there are: few of them get all waves on their own part of K, many
+// share the rows of x among more columns.  Measured over 730 calls of M = 1 .. 64, N = 64 .. 65536, K = 64 .. 14336, groups of 32 to 256: the tile taken is 2 % slower than
+// the best of those built on average, 8 % in one of twenty.
+template <class F>
+hipError_t with_tile(int64_t M, int64_t N, int64_t K, F&& f)
+{
+    const int64_t tiles = (N + 15) / 16;
+    const bool longer = K > 2048;
+    if (M <= 1) return tiles < 768 ? f(Four<1, 1, 1, 8, 4, 2>{}) : tiles < 1536 ? f(Four<1, 1, 2, 4, 8, 2>{}) : f(Four<1, 2, 2, 4, 8, 2>{});
+    if (M <= 4 && tiles < 256) return f(Four<4, 1, 1, 8, 4, 2>{});
+    if (M <= 8) {
+        if (tiles < 512) return longer && M > 4 ? f(Four<8, 1, 1, 8, 4, 2>{}) : f(Four<8, 1, 2, 4, 4, 2>{});
+        return tiles < 1024 || M <= 4 ? f(Four<8, 2, 2, 4, 4, 2>{}) : f(Four<16, 1, 8, 1, 8, 4>{});
+    }
+    if (M <= 16) {
+        if (tiles >= 1024) return f(Four<16, 1, 8, 1, 8, 4>{});
+        if (!longer) return f(Four<16, 1, 2, 4, 1, 1>{});
+        return tiles < 256 ? f(Four<16, 1, 1, 8, 1, 1>{}) : tiles < 512 ? f(Four<16, 1, 2, 4, 2, 2>{}) : f(Four<16, 2, 2, 4, 2, 2>{});
+    }
+    if (M <= 32) {
+        if (tiles < 512) return longer && tiles < 256 ? f(Four<32, 1, 1, 8, 1, 1>{}) : f(Four<32, 1, 2, 4, 1, 1>{});
+        return tiles < 1024 ? f(Four<32, 1, 4, 2, 2, 2>{}) : f(Four<32, 1, 8, 1, 4, 4>{});
+    }
+    if (M <= 48) return tiles < 512 ? f(Four<48, 1, 2, 4, 1, 1>{}) : tiles < 1024 ? f(Four<48, 2, 2, 4, 1, 1>{}) : f(Four<48, 1, 8, 1, 2, 2>{});
+    return tiles < 512 ? f(Four<64, 1, 2, 4, 1, 1>{}) : tiles < 1024 ? f(Four<64, 2, 2, 4, 1, 1>{}) : f(Four<64, 1, 8, 1, 2, 2>{});
+}
+
 }  // namespace
+
+hipError_t four_init()
+{
+    // one call of no rows for every tile and form: it sets the kernel's limit for LDS
+    for (const int64_t M : {1, 2, 8, 16, 32, 48, 64})
+        for (const int64_t N : {16, 256 * 16, 512 * 16, 768 * 16, 1024 * 16, 1536 * 16})
+            for (const int64_t K : {1024, 4096})
+                for (const int64_t group : {32, 64, 128})
+                    for (int zeros = 0; zeros < 2; ++zeros) {
+                        Gemm4Desc g{nullptr, nullptr, nullptr, zeros ? reinterpret_cast<const uint8_t*>(&g) : nullptr, nullptr, 0, N, K, group, false, 0};
+                        if (const hipError_t e = with_tile(M, N, K, [&](auto tile) { return decltype(tile)::launch(g, nullptr); }); e != hipSuccess) return e;
+                    }
+    return hipSuccess;
+}
 
 hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s)
 {
-    constexpr int64_t kRows = int64_t(65535) * 16;
+    constexpr int64_t kRows = int64_t(65535) * 16;        // what a grid's second dimension holds
     for (int64_t m = 0; m < g.M; m += kRows) {
         Gemm4Desc part = g;
         part.x += m * g.K;
         part.y = static_cast<char*>(g.y) + m * g.N * (g.wide ? 4 : 2);
         part.M = g.M - m < kRows ? g.M - m : kRows;
-        hipLaunchKernelGGL(simple_kernel, dim3(unsigned((g.N + 15) / 16), unsigned((part.M + 15) / 16)), dim3(256), 0, s, part);
+        part.magic = g.group >= g.K ? 0u : uint32_t(((uint64_t(1) << 31) + g.group / 32 - 1) / uint64_t(g.group / 32));
+        if (g.K < 8) hipLaunchKernelGGL(simple_kernel, dim3(unsigned((g.N + 15) / 16), unsigned((part.M + 15) / 16)), dim3(256), 0, s, part);
+        else if (const hipError_t e = with_tile(part.M, g.N, g.K, [&](auto tile) { return decltype(tile)::launch(part, s); }); e != hipSuccess) return e;
     }
     return hipGetLastError();
 }

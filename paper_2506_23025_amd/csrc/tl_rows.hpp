@@ -57,7 +57,9 @@ struct Gemm4Desc {
     void* y;
     int64_t M, N, K, group;
     bool wide;                            // y is fp32
+    uint32_t magic;                       // 2^31 / (group / 32), rounded up, or 0 for one group: block * magic / 2^31 is the group of a block of 32 (blocks and groups are fewer than 2^15)
 };
-hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s);
+hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s);            // sets magic itself
+hipError_t four_init();
 
 }  // namespace tl

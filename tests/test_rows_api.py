@@ -180,6 +180,6 @@ def test_4_bit_product_refusals():
         assert status(**{name: None}) == tl.TL_ERR_NULL
     for name in ("x", "Wpacked", "scales", "zeros", "y"):
         assert status(**{name: P + 8}) == tl.TL_ERR_ALIGN
-    for kw in ({"M": 0}, {"N": 0}, {"K": 0}, {"group": 0}, {"group": 48}, {"group": -32}, {"N": 1 << 31}):
+    for kw in ({"M": 0}, {"N": 0}, {"K": 0}, {"group": 0}, {"group": 48}, {"group": -32}, {"N": 1 << 24}, {"K": 1 << 20}):
         assert status(**kw) == tl.TL_ERR_SHAPE, kw
     assert status(y_real=2) == tl.TL_ERR_UNSUPPORTED
