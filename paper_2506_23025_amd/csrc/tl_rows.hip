@@ -35,37 +35,37 @@ __device__ inline uint32_t wave_max(uint32_t x)
     return uint32_t(__builtin_amdgcn_readlane(int(over_wave(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; })), 63));
 }
 
-// g / (1 + e^-g) * u in fp64, off by some 2^-51 of itself, so that its fp32 rounding is that of the exact value but for one in 2^27: e^-g = 2^n e^r with |r| <= log(2) / 2 and the
-// series up to r^12, the quotient from the hardware's reciprocal by a step of Newton's and one on the quotient itself.  fp64 costs what fp32 does here, and the loads take longer.
-__device__ inline float gated(float g, float u)
-{
-    const double gu = double(g) * double(u);              // exact: 22 bits
-    double t = -double(g);
-    t = t > 700.0 ? 700.0 : t < -700.0 ? -700.0 : t;
-    const double n = __builtin_rint(t * 1.44269504088896340736);
-    double r = __builtin_fma(n, -0x1.62e42fefa39efp-1, t);
-    r = __builtin_fma(n, -0x1.abc9e3b39803fp-56, r);
-    double p = 1.0 / 479001600.0;
-    p = __builtin_fma(p, r, 1.0 / 39916800.0);
-    p = __builtin_fma(p, r, 1.0 / 3628800.0);
-    p = __builtin_fma(p, r, 1.0 / 362880.0);
-    p = __builtin_fma(p, r, 1.0 / 40320.0);
-    p = __builtin_fma(p, r, 1.0 / 5040.0);
-    p = __builtin_fma(p, r, 1.0 / 720.0);
-    p = __builtin_fma(p, r, 1.0 / 120.0);
-    p = __builtin_fma(p, r, 1.0 / 24.0);
-    p = __builtin_fma(p, r, 1.0 / 6.0);
-    p = __builtin_fma(p, r, 0.5);
-    p = __builtin_fma(p, r, 1.0);
-    p = __builtin_fma(p, r, 1.0);
-    const double d = 1.0 + __builtin_amdgcn_ldexp(p, int(n));
-    double q = __builtin_amdgcn_rcp(d);
-    q = __builtin_fma(__builtin_fma(-d, q, 1.0), q, q);
-    double v = gu * q;
-    v = __builtin_fma(__builtin_fma(-v, d, gu), q, v);
-    // an infinity: its product is the answer, but for a gate of -infinity, which has none
-    return __builtin_isfinite(gu) ? float(v) : g == -__builtin_inff() ? __builtin_nanf("") : float(gu);
-}
+// g / (1 + e^-g) * u in fp64, off by some 2^-50 of itself, so that its fp32 rounding is that of the exact value but for one in 2^26; an infinity or NaN where g or u is not finite.  e^-g = 2^n e^r with |r| <= log(2) / 2;
+// e^r by the polynomial of degree 10 that agrees with it at the eleven nodes of Chebyshev's on that interval (off by 2^-51); the quotient from the hardware's reciprocal q of d = 1 + e^-g, which is off by e = 1 - d q, as
+// w q (1 + e + e^2).  A product in fp64 costs what one in fp32 does here; conversions cost more, so n is found by a sum that leaves it in the lowest bits, and 2^n goes into the exponent by an
+// integer addition.
+struct Gate {
+    // in scalar registers: the compiler would move each into the sum's registers first
+    double c[10] = {0x1.28a2ca617b969p-22, 0x1.72fafebdaf273p-19, 0x1.a019a6611cad5p-16, 0x1.a01978b8b3d18p-13, 0x1.6c16c17f46982p-10,
+                    0x1.1111112ddae8bp-7, 0x1.55555555520a4p-5, 0x1.555555554b736p-3, 0x1.0000000000005p-1, 0x1.000000000001ep+0};
+    double rate = -0x1.71547652b82fep+0, log2 = -0x1.62e42fefa39efp-1, shift = 0x1.8p52;
+    __device__ Gate()
+    {
+#pragma unroll
+        for (int i = 1; i < 10; ++i) asm("" : "+s"(c[i]));
+        asm("" : "+s"(rate), "+s"(log2), "+v"(shift), "+v"(c[0]));
+    }
+    __device__ inline float operator()(float g, float u) const
+    {
+        const double x = double(__builtin_amdgcn_fmed3f(g, -700.0f, 700.0f));
+        const double z = __builtin_fma(x, rate, shift), n = z - shift;
+        const double r = __builtin_fma(n, log2, -x);      // log(2) rounded moves it by n 2^-55
+        double p = __builtin_fma(c[0], r, c[1]);
+#pragma unroll
+        for (int i = 2; i < 10; ++i) p = __builtin_fma(p, r, c[i]);
+        p = __builtin_fma(p, r, 1.0);
+        u32x2 t = __builtin_bit_cast(u32x2, p);
+        t[1] += __builtin_bit_cast(u32x2, z)[0] << 20;    // |n| <= 1010: within the exponent's range
+        const double d = 1.0 + __builtin_bit_cast(double, t), q = __builtin_amdgcn_rcp(d);
+        const double e = __builtin_fma(-d, q, 1.0), w = double(g * u) * q;      // g * u is exact: 22 bits
+        return float(__builtin_fma(w, __builtin_fma(e, e, e), w));
+    }
+};
 
 // Eight values from place d of a row on; 0 behind its end.
 __device__ inline void take(const _Float16* row, int d, int dim, float* v)
@@ -126,6 +126,7 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) rows_kernel(RowsArgs a)
     const int64_t row = W == 1 ? int64_t(blockIdx.x) * 4 + wave : blockIdx.x;
     if (W == 1 && row >= a.rows) return;
     const int first = (W == 1 ? lane : int(threadIdx.x)) * 8;
+    const int wave_first = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(wave) * 512;
     constexpr int STEP = 64 * 8 * W;
     const int dim = a.dim;
     const _Float16* const xa = static_cast<const _Float16*>(a.a.p) + row * a.a.stride;
@@ -134,8 +135,10 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) rows_kernel(RowsArgs a)
     for (int c = 0; c < C; ++c) take(xa, first + c * STEP, dim, v[c]);
     if constexpr (KIND == kGatedRows) {
         const _Float16* const xg = static_cast<const _Float16*>(a.b.p) + row * a.b.stride;
+        const Gate gated;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
+            if (wave_first + c * STEP >= dim) break;      // the pieces that a wave has none of
             float g[8];
             take(xg, first + c * STEP, dim, g);
 #pragma unroll
@@ -191,20 +194,34 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) rows_kernel(RowsArgs a)
             }
         }
     }
-    if (a.y.p) {
-#pragma unroll
-        for (int c = 0; c < C; ++c) put(static_cast<_Float16*>(a.y.p) + row * a.y.stride, first + c * STEP, dim, v[c]);
-    }
-    if (!a.out.codes) return;
-    // The largest magnitude as its bits: they order as the numbers do, infinities and NaN above all.
+    // The largest magnitude as its bits: they order as the numbers do, infinities and NaN above all.  Places behind the row are 0, or NaN in a row that is.
     uint32_t top = 0;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const uint32_t u = (first + c * STEP + i < dim ? __builtin_bit_cast(uint32_t, v[c][i]) : 0u) & 0x7fffffffu;
+            const uint32_t u = __builtin_bit_cast(uint32_t, v[c][i]) & 0x7fffffffu;
             top = u > top ? u : top;
         }
+    if constexpr (KIND == kGatedRows) {
+        // what is not finite in y: the product, but for a gate of -infinity, which has none
+        if (a.y.p && __any(top >= 0x7f800000u)) {
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                float g[8], u[8];
+                take(static_cast<const _Float16*>(a.b.p) + row * a.b.stride, first + c * STEP, dim, g);
+                take(xa, first + c * STEP, dim, u);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (!__builtin_isfinite(g[i] * u[i])) v[c][i] = g[i] == -__builtin_inff() ? __builtin_nanf("") : g[i] * u[i];
+            }
+        }
+    }
+    if (a.y.p) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) put(static_cast<_Float16*>(a.y.p) + row * a.y.stride, first + c * STEP, dim, v[c]);
+    }
+    if (!a.out.codes) return;
     top = wave_max(top);
     if constexpr (W > 1) {
         if (lane == 0) tops[wave] = top;
@@ -219,13 +236,18 @@ __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) rows_kernel(RowsArgs a)
     if (first == 0) a.out.scales[row] = some ? most / 127.0f : finite ? 0.0f : __builtin_nanf("");
     int8_t* const codes = a.out.codes + row * a.out.stride;
     const bool odd = lane & 1;
+    const uint32_t keep = some ? ~0u : 0u;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-        // Two lanes hold a block of 16.  Each has two bytes of all four words of it (places s and 4 + s of its half); the even lane writes the first two words, the odd lane the others.
+        // A product below 2^22 is rounded to a whole number by a sum that leaves it in the lowest bits.
         uint32_t q[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) q[i] = uint32_t(int(some ? __builtin_rintf(v[c][i] * inverse) : 0.0f)) & 255u;
-        const uint32_t lo = q[0] | q[4] << 8 | q[1] << 16 | q[5] << 24, hi = q[2] | q[6] << 8 | q[3] << 16 | q[7] << 24;
+        for (int i = 0; i < 8; ++i) q[i] = __builtin_bit_cast(uint32_t, rounded(v[c][i] * inverse) + 0x1.8p23f);
+        // Two lanes hold a block of 16.  Each has two bytes of all four words of it (places s and 4 + s of its half); the even lane writes the first two words, the odd lane the others.
+        const auto bytes = [&](int i, int j, int k, int l) {
+            return __builtin_amdgcn_perm(__builtin_amdgcn_perm(q[l], q[k], 0x0C0C0400u), __builtin_amdgcn_perm(q[j], q[i], 0x0C0C0400u), 0x05040100u) & keep;
+        };
+        const uint32_t lo = bytes(0, 4, 1, 5), hi = bytes(2, 6, 3, 7);
         const uint32_t got = moved<0xB1, 15>(odd ? lo : hi), own = odd ? hi : lo;
         const uint32_t l = odd ? got : own, h = odd ? own : got;
         const int d = first + c * STEP;
@@ -244,12 +266,18 @@ hipError_t launch(const RowsArgs& a, hipStream_t s)
 template <RowsKind KIND>
 hipError_t launch_kind(const RowsArgs& a, hipStream_t s)
 {
+    // A piece a lane as long as 16 waves hold the row; longer rows, where there are many, 8 waves with more.  Measured (us): 192 rows of 4096 places with a residual in fp16, 4 / 8 / 16
+    // waves 4.6 / 4.0 / 4.5; 2048 of 2048, 1 / 4 / 8 waves 11.3 / 10.0 / 11.4; 600 of 8192, 8 / 16 waves 11.1 / 13.0; 4096 of 11008, 8 / 12 / 16 waves 65 / 70 / 71, 64 rows of it 6.7 / 6.0 / 6.1.
     const int pieces = (a.dim + 7) / 8;
+    const bool many = a.rows >= 256;
     if (pieces <= 64) return launch<KIND, 1, 1>(a, s);
+    if (pieces <= 128) return launch<KIND, 2, 1>(a, s);
     if (pieces <= 256) return launch<KIND, 4, 1>(a, s);
-    if (pieces <= 512) return launch<KIND, 4, 2>(a, s);
-    if (pieces <= 1024) return launch<KIND, 4, 4>(a, s);
-    if (pieces <= 2048) return launch<KIND, 16, 2>(a, s);
+    if (pieces <= 384) return launch<KIND, 6, 1>(a, s);
+    if (pieces <= 512) return launch<KIND, 8, 1>(a, s);
+    if (pieces <= 1024) return many ? launch<KIND, 8, 2>(a, s) : launch<KIND, 16, 1>(a, s);
+    if (pieces <= 1536 && many) return launch<KIND, 8, 3>(a, s);
+    if (pieces <= 2048) return many ? launch<KIND, 8, 4>(a, s) : launch<KIND, 16, 2>(a, s);
     if (pieces <= 4096) return launch<KIND, 16, 4>(a, s);
     return launch<KIND, 16, 8>(a, s);
 }
