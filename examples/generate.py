@@ -6,7 +6,9 @@ Its weights are random, so what it says means nothing; what it does is what a se
 * prompts of different lengths come packed, one behind the other: tl_kv_append rotates queries and keys and puts keys and values into a paged 8-bit cache,
   tl_attn_prompt attends over what is at hand in fp16;
 * a further turn of a conversation, several tokens of each sequence, attends over the cache (tl_attn_cached);
-* generation takes one token of each sequence at a time, as one captured graph: lengths are read on the device, so it serves every step.
+* generation takes one token of each sequence at a time, as one captured graph: lengths are read on the device, so it serves every step;
+* with --rows8 what goes into the products is in 8 bits, made by the norm with the residual's addition (tl_norm) and by the gate (tl_gate), the products are sums of whole
+  numbers (tl_ternary_gemm_rows8), and the head has 4 bits a weight (tl_gemm_4bit); no torch operation is left between them.
 
     python examples/generate.py --layers 8 --width 2048 --heads 16 --kv-heads 4 --new 64
 """
@@ -32,8 +34,25 @@ class Linear:
         self.words = torch.from_numpy(tl.tl_pack_2bit(what).view(np.int32)).cuda()
 
     def __call__(self, x):
-        y = torch.empty((x.shape[0], self.n), dtype=torch.float16, device="cuda")
-        tl.tl_ternary_gemm(x, self.words, self.gamma, y, x.shape[0], self.n, self.k)
+        eight = isinstance(x, tl.tl_rows8)
+        y = torch.empty((x.rows if eight else x.shape[0], self.n), dtype=torch.float16, device="cuda")
+        if eight:
+            tl.tl_ternary_gemm_rows8(x, self.words, self.gamma, y)
+        else:
+            tl.tl_ternary_gemm(x, self.words, self.gamma, y, x.shape[0], self.n, self.k)
+        return y
+
+
+class Head:
+    """Logits in 32 bits, from 4-bit weights with a scale for every 64 of them."""
+
+    def __init__(self, w):
+        codes, scales, _ = tl.tl_quantize_4bit(w, 64)
+        self.n, self.words, self.scales = w.shape[0], torch.from_numpy(tl.tl_pack_4bit(codes).view(np.int32)).cuda(), torch.from_numpy(scales).cuda()
+
+    def __call__(self, x):
+        y = torch.empty((x.shape[0], self.n), dtype=torch.float32, device="cuda")
+        tl.tl_gemm_4bit(tl.make_4bit_job(x, self.words, self.scales, None, 64, y))
         return y
 
 
@@ -42,16 +61,71 @@ def norm(x):
     return (x * torch.rsqrt(x.square().mean(-1, keepdim=True) + 1e-5)).half()
 
 
+class Flow16:
+    """What stands between the products, in torch and fp16: the residual, its norms, the gate."""
+
+    def __init__(self, x):
+        self.x = x
+
+    def norm(self):
+        return norm(self.x)
+
+    last = norm
+
+    def add(self, y):
+        self.x = self.x + y
+
+    def rows(self, y):
+        return y
+
+    def gate(self, both):
+        gate, up = both.split(both.shape[1] // 2, dim=1)
+        return (torch.nn.functional.silu(gate.float()) * up.float()).half()
+
+
+class Flow8:
+    """The same into rows of 8 bits, the residual in 32: what is added waits for the norm that follows."""
+
+    def __init__(self, x):
+        self.y, self.residual = x, torch.zeros(x.shape, dtype=torch.float32, device="cuda")
+
+    def eight(self, t, n):
+        return tl.make_rows8(torch.empty((t, (n + 15) // 16 * 16), dtype=torch.int8, device="cuda"), torch.empty(t, device="cuda"), n)
+
+    def norm(self):
+        out = self.eight(*self.y.shape)
+        tl.tl_norm(tl.make_norm_job(self.y, self.residual, self.residual, out=out))
+        return out
+
+    def last(self):
+        out = torch.empty_like(self.y)
+        tl.tl_norm(tl.make_norm_job(self.y, self.residual, self.residual, y=out))
+        return out
+
+    def add(self, y):
+        self.y = y
+
+    def rows(self, y, gate=None):
+        out = self.eight(*y.shape)
+        tl.tl_gate(tl.make_gate_job(gate, y, None, out))
+        return out
+
+    def gate(self, both):
+        gate, up = both.split(both.shape[1] // 2, dim=1)
+        return self.rows(up, gate)
+
+
 class Decoder:
-    def __init__(self, layers=4, width=1024, heads=8, kv_heads=2, dim=128, hidden=2816, vocab=1000, seqs=4, room=2048, page_tokens=64, kind=tl.TL_KV_INT8, seed=0):
+    def __init__(self, layers=4, width=1024, heads=8, kv_heads=2, dim=128, hidden=2816, vocab=1000, seqs=4, room=2048, page_tokens=64, kind=tl.TL_KV_INT8, seed=0, rows8=False):
         """seqs sequences of up to `room` tokens each."""
         rng = np.random.default_rng(seed)
         self.heads, self.kv_heads, self.dim, self.seqs, self.kind, self.page_tokens = heads, kv_heads, dim, seqs, kind, page_tokens
         self.embedding = torch.from_numpy(rng.standard_normal((vocab, width), dtype=np.float32)).cuda().half()
-        self.head = torch.from_numpy(rng.standard_normal((width, vocab), dtype=np.float32)).cuda() / math.sqrt(width)
+        head = rng.standard_normal((width, vocab), dtype=np.float32)
+        self.head = Head(head.T / math.sqrt(width)) if rows8 else torch.from_numpy(head).cuda() / math.sqrt(width)
+        self.flow = Flow8 if rows8 else Flow16
         self.layers = [{"qkv": Linear(rng, (heads + 2 * kv_heads) * dim, width), "o": Linear(rng, width, heads * dim),
                         "up": Linear(rng, 2 * hidden, width), "down": Linear(rng, width, hidden)} for _ in range(layers)]
-        self.hidden = hidden
         self.rope = tl.make_rope(torch.from_numpy(tl.tl_rope_table(room, dim)).cuda(), dim)
         # A cache for each layer; all share one page table.  Pages are dealt out at random, as those of a server that has run for a while.
         each = (room + page_tokens - 1) // page_tokens
@@ -72,10 +146,10 @@ class Decoder:
         is attended to is in the call.  longest: a bound of the tokens cached, 0 if there is none at hand."""
         T, H, G, D = ids.shape[0], self.heads, self.kv_heads, self.dim
         batch = tl.make_batch(start, self.cached, self.seqs, T)
-        x = self.embedding[ids]
+        flow = self.flow(self.embedding[ids])
         space = None if fresh else torch.empty(tl.tl_attn_cached_workspace(self.seqs, T, H, G, D), dtype=torch.uint8, device="cuda")
         for w, cache in zip(self.layers, self.cache):
-            qkv = w["qkv"](norm(x)).view(T, H + 2 * G, D)
+            qkv = w["qkv"](flow.norm()).view(T, H + 2 * G, D)
             q, k, v = qkv[:, :H], qkv[:, H:H + G], qkv[:, H + G:]
             # queries and keys are rotated where they stand
             tl.tl_kv_append(tl.make_append_job(q, k, v, q, k if fresh else None, batch, cache, self.rope))
@@ -84,17 +158,16 @@ class Decoder:
                 tl.tl_attn_prompt(tl.make_prompt_job(q, k, v, seen, tl.make_batch(start, None, self.seqs, T), D ** -0.5))
             else:
                 tl.tl_attn_cached(tl.make_cached_job(q, seen, batch, cache, D ** -0.5, longest, space))
-            x = x + w["o"](seen.view(T, H * D))
-            gate, up = w["up"](norm(x)).split(self.hidden, dim=1)
-            x = x + w["down"]((torch.nn.functional.silu(gate.float()) * up.float()).half())
+            flow.add(w["o"](flow.rows(seen.view(T, H * D))))
+            flow.add(w["down"](flow.gate(w["up"](flow.norm()))))
         if start is None:
             self.cached += 1
         else:
             self.cached += start[1:] - start[:-1]
-        return norm(x)
+        return flow.last()
 
     def logits(self, x):
-        return x.float() @ self.head
+        return self.head(x) if isinstance(self.head, Head) else x.float() @ self.head
 
     def feed(self, turns, fresh):
         """Takes some tokens of each sequence (lists); logits after the last of each."""
@@ -139,9 +212,10 @@ def main():
     for name, value in (("layers", 4), ("width", 1024), ("heads", 8), ("kv-heads", 2), ("dim", 128), ("hidden", 2816), ("seqs", 4), ("prompt", 500), ("turn", 20), ("new", 32)):
         p.add_argument("--" + name, type=int, default=value)
     p.add_argument("--cache", choices=("int8", "fp8"), default="int8")
+    p.add_argument("--rows8", action="store_true", help="activations of the products in 8 bits, the head in 4")
     a = p.parse_args()
     room = a.prompt + a.turn + a.new + 1
-    model = Decoder(a.layers, a.width, a.heads, a.kv_heads, a.dim, a.hidden, seqs=a.seqs, room=room, kind=tl.TL_KV_INT8 if a.cache == "int8" else tl.TL_KV_FP8)
+    model = Decoder(a.layers, a.width, a.heads, a.kv_heads, a.dim, a.hidden, seqs=a.seqs, room=room, kind=tl.TL_KV_INT8 if a.cache == "int8" else tl.TL_KV_FP8, rows8=a.rows8)
     rng = np.random.default_rng(1)
     vocab = model.embedding.shape[0]
 
