@@ -79,13 +79,15 @@ __device__ inline u32x4 shifted(u32x4 v, int n)
     return n < 8 ? v : u32x4{0, 0, 0, 0};
 }
 
-// Up to MR rows and 16 FN WN columns of y a workgroup.  K goes by chunks of 128, dealt to WK sets of waves; a wave has FN column fragments, and their words, scales and zeros come straight into its
-// registers, D chunks ahead.  Rows of x go through registers into LDS, a panel of CP WK chunks at a time and the next one while a panel is used, since every wave needs all of them.
+// Up to MR rows and 16 FN WN columns of y a workgroup.  K goes by chunks of 128, dealt to WK sets of waves; a wave has FN column fragments, and their words come straight into its
+// registers, D chunks ahead.  Rows of x go through registers into LDS, a panel of CP WK chunks at a time and the next one while a panel is used, since every wave needs all of them; a panel's scales
+// and zeros go the same way, as a wave that fetched its own would ask for 32 bytes four times over at every turn.
 // The words are the column operand of the matrix instruction: a lane has one column, so one zero point and one scale.  Sums of UNIT steps of 32 are scaled and added in fp32.
 template <int MR, int FN, int WN, int WK, int CP, int D, int UNIT, bool ZEROS>
 __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 {
     constexpr int FM = (MR + 15) / 16, THREADS = 64 * WN * WK, PK = CP * WK, XL = (MR * PK * 16 + THREADS - 1) / THREADS, FOLDS = 4 / UNIT;
+    constexpr int BN = 16 * FN * WN, ENTRIES = PK * FOLDS * BN, SL = (ENTRIES + THREADS - 1) / THREADS, PANEL = MR * PK * 256 + ENTRIES * 4;
     static_assert(MR < 16 || MR % 16 == 0, "rows");
     static_assert(CP % D == 0 || D == 1, "register slots are known to the compiler");
     extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -97,46 +99,43 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
     const int rows = int(g.M) - m0 < MR ? int(g.M) - m0 : MR;
     const uint32_t blocks32 = uint32_t(K + 31) >> 5;
 
-    // ---- words, scales and zeros of a chunk ------------------------------------------------------------------
+    // ---- words of a chunk ------------------------------------------------------------------------------------
     const int64_t row_bytes = int64_t(chunks) * 64, wleft = (int64_t(N) - n0) * row_bytes;
     const auto wbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint32_t*>(g.W) + n0 * (row_bytes / 4), 0, int(wleft < kLimit ? (wleft > 0 ? wleft : 0) : kLimit), kRawBuffer);
-    uint32_t woff[FN], col[FN];
+    uint32_t woff[FN];
 #pragma unroll
     for (int f = 0; f < FN; ++f) {
         const int n = 16 * f + in, last = N - 1 - n0;
-        col[f] = uint32_t(n < last ? n : (last > 0 ? last : 0));
-        woff[f] = col[f] * uint32_t(row_bytes) + uint32_t(quarter) * 16u;
+        woff[f] = uint32_t(n < last ? n : (last > 0 ? last : 0)) * uint32_t(row_bytes) + uint32_t(quarter) * 16u;
     }
-    const int nbase = n0 < N ? n0 : N - 1;                // a wave behind the last column looks at that one
-    struct Slot { u32x4 w[FN]; uint16_t s[FN][FOLDS]; uint8_t z[FN][FOLDS]; } slots[D];
+    struct Slot { u32x4 w[FN]; } slots[D];
     const auto load = [&](Slot& b, int chunk) {
         __builtin_amdgcn_sched_barrier(0);
         const uint32_t o = chunk < chunks ? uint32_t(chunk) * 64u : 0x80000000u;
 #pragma unroll
         for (int f = 0; f < FN; ++f) b.w[f] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(wbuf, int(woff[f] + o), 0, 0));
-#pragma unroll
-        for (int h = 0; h < FOLDS; ++h) {
-            const uint32_t block = uint32_t(chunk * 4 + h * UNIT), group = uint32_t(uint64_t(block < blocks32 ? block : blocks32 - 1) * g.magic >> 31);
-            const int64_t at = int64_t(group) * N + nbase;
-            const char* const sbase = reinterpret_cast<const char*>(g.scales + at);
-            const char* const zbase = reinterpret_cast<const char*>(g.zeros + at);
-#pragma unroll
-            for (int f = 0; f < FN; ++f) {
-                b.s[f][h] = *reinterpret_cast<const uint16_t*>(sbase + col[f] * 2u);
-                if constexpr (ZEROS) b.z[f][h] = *reinterpret_cast<const uint8_t*>(zbase + col[f]);
-            }
-        }
         __builtin_amdgcn_sched_barrier(0);
     };
 
     // ---- rows of a panel: piece i of a thread is eight places of a row ----------------------------------------------
     u32x4 xr[XL];
+    uint16_t sr[SL];
+    uint8_t zr[SL];
     const auto fetch = [&](int panel) {
 #pragma unroll
         for (int i = 0; i < XL; ++i) {
             const int at = i * THREADS + tid, r = at / (PK * 16), k = panel * (PK * 128) + (at % (PK * 16)) * 8;
             const int64_t row = int64_t(m0) + (r < rows ? r : rows - 1);
             xr[i] = *reinterpret_cast<const u32x4_any*>(g.x + row * K + (k < K - 8 ? k : K - 8));
+        }
+        // a column's scale and zero for every UNIT blocks of 32 places
+#pragma unroll
+        for (int i = 0; i < SL; ++i) {
+            const int at = i * THREADS + tid, c = at % BN + int(blockIdx.x) * BN;
+            const uint32_t block = uint32_t(panel * (PK * 4) + at / BN * UNIT), group = uint32_t(uint64_t(block < blocks32 ? block : blocks32 - 1) * g.magic >> 31);
+            const int64_t from = int64_t(group) * N + (c < N ? c : N - 1);
+            sr[i] = reinterpret_cast<const uint16_t*>(g.scales)[from];
+            if constexpr (ZEROS) zr[i] = g.zeros[from];
         }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -148,7 +147,14 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
             if (K % 8 != 0) v = shifted(v, k < K - 8 ? 0 : k - (K - 8) < 8 ? k - (K - 8) : 8);
             else v = k < K ? v : u32x4{0, 0, 0, 0};
             if (MR * PK * 16 % THREADS == 0 || r < MR)
-                *reinterpret_cast<u32x4*>(lds + (panel & 1) * (MR * PK * 256) + r * (PK * 256) + (p >> 4) * 256 + ((p ^ r) & 15) * 16) = v;
+                *reinterpret_cast<u32x4*>(lds + (panel & 1) * PANEL + r * (PK * 256) + (p >> 4) * 256 + ((p ^ r) & 15) * 16) = v;
+        }
+#pragma unroll
+        for (int i = 0; i < SL; ++i) {
+            const int at = i * THREADS + tid;
+            uint32_t v = sr[i];
+            if constexpr (ZEROS) v |= uint32_t(__builtin_bit_cast(uint16_t, _Float16(short(zr[i])))) << 16;
+            if (ENTRIES % THREADS == 0 || at < ENTRIES) reinterpret_cast<uint32_t*>(lds + (panel & 1) * PANEL + MR * PK * 256)[at] = v;
         }
     };
     uint32_t xread[4];                                    // of the four steps of a chunk; rows that there are not hold another's places
@@ -163,7 +169,7 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 #pragma unroll
         for (int f = 0; f < FN; ++f) total[a][f] = f32x4{0, 0, 0, 0};
     const auto use = [&](const Slot& b, int panel, int local) {
-        const unsigned char* const xs = lds + (panel & 1) * (MR * PK * 256);
+        const unsigned char* const xs = lds + (panel & 1) * PANEL;
         // all reads, all decodes, all products: the decodes take as long as the reads do
         f16x8 x[4][FM], w[4][FN];
         __builtin_amdgcn_sched_barrier(0);
@@ -171,15 +177,19 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int a = 0; a < FM; ++a) x[t][a] = *reinterpret_cast<const f16x8*>(xs + xread[t] + a * (16 * PK * 256) + local * 256);
+        f16x2 sz[FN][FOLDS];                              // scale, zero
+#pragma unroll
+        for (int f = 0; f < FN; ++f)
+#pragma unroll
+            for (int h = 0; h < FOLDS; ++h)
+                sz[f][h] = *reinterpret_cast<const f16x2*>(xs + MR * PK * 256 + ((local * FOLDS + h) * BN + wn * (16 * FN) + f * 16 + in) * 4);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int f = 0; f < FN; ++f)
 #pragma unroll
             for (int t = 0; t < 4; ++t) {
-                const int h = t / UNIT;
-                const _Float16 z = ZEROS ? _Float16(short(b.z[f][h])) : _Float16(8);
-                const _Float16 less1024 = _Float16(-1024) - z, less64 = _Float16(-64) - z;
-                w[t][f] = decoded(b.w[f][t], f16x2{less1024, less1024}, f16x2{less64, less64});
+                const _Float16 z = ZEROS ? sz[f][t / UNIT][1] : _Float16(8);
+                w[t][f] = decoded(b.w[f][t], f16x2{_Float16(-1024), _Float16(-1024)} - f16x2{z, z}, f16x2{_Float16(-64), _Float16(-64)} - f16x2{z, z});
             }
         __builtin_amdgcn_sched_barrier(0);
         f32x4 sum[FM][FN];
@@ -190,7 +200,7 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 #pragma unroll
                 for (int a = 0; a < FM; ++a) {
                     sum[a][f] = __builtin_amdgcn_mfma_f32_16x16x32_f16(x[t][a], w[t][f], t % UNIT == 0 ? f32x4{0, 0, 0, 0} : sum[a][f], 0, 0, 0);
-                    if (t % UNIT == UNIT - 1) total[a][f] += sum[a][f] * float(__builtin_bit_cast(_Float16, b.s[f][t / UNIT]));
+                    if (t % UNIT == UNIT - 1) total[a][f] += sum[a][f] * float(sz[f][t / UNIT][0]);
                 }
     };
 
@@ -252,12 +262,12 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 
 template <int MR, int FN, int WN, int WK, int CP, int D>
 struct Four {
-    static constexpr int BN = 16 * FN * WN, PANEL = MR * CP * WK * 256, RED = WK > 1 ? WN * WK * ((MR + 15) / 16) * FN * 1024 : 0;
-    static constexpr int MOST = 2 * PANEL > RED ? 2 * PANEL : RED;
-    static_assert(MOST <= 160 * 1024, "LDS");
+    static constexpr int BN = 16 * FN * WN, RED = WK > 1 ? WN * WK * ((MR + 15) / 16) * FN * 1024 : 0;
     template <int UNIT, bool ZEROS>
     static hipError_t launch(const Gemm4Desc& g, hipStream_t s)
     {
+        constexpr int PANEL = MR * CP * WK * 256 + CP * WK * (4 / UNIT) * BN * 4, MOST = 2 * PANEL > RED ? 2 * PANEL : RED;
+        static_assert(MOST <= 160 * 1024, "LDS");
         if constexpr (MOST > 64 * 1024) {
             static std::atomic<uint64_t> set{0};
             const int device = device_slot();
@@ -281,17 +291,20 @@ struct Four {
 };
 
 // Which tile: by the rows, so that none is staged in vain, and by the column tiles of 16 that there are: few of them get all waves on their own part of K, many
-// share the rows of x among more columns.  Measured over 730 calls of M = 1 .. 64, N = 64 .. 65536, K = 64 .. 14336, groups of 32 to 256: the tile taken is 2 % slower than
+// share the rows of x among more columns.  Measured over 700 calls of M = 1 .. 64, N = 64 .. 65536, K = 64 .. 14336, groups of 32 to 256: the tile taken is 2 % slower than
 // the best of those built on average, 8 % in one of twenty.
 template <class F>
 hipError_t with_tile(int64_t M, int64_t N, int64_t K, F&& f)
 {
     const int64_t tiles = (N + 15) / 16;
     const bool longer = K > 2048;
-    if (M <= 1) return tiles < 768 ? f(Four<1, 1, 1, 8, 4, 2>{}) : tiles < 1536 ? f(Four<1, 1, 2, 4, 8, 2>{}) : f(Four<1, 2, 2, 4, 8, 2>{});
+    if (M <= 1) {
+        if (tiles < 256) return K > 4096 ? f(Four<1, 1, 1, 8, 4, 4>{}) : f(Four<1, 1, 1, 8, 4, 2>{});
+        return tiles < 768 ? f(Four<1, 1, 1, 4, 8, 4>{}) : tiles < 1536 ? f(Four<1, 1, 2, 4, 8, 2>{}) : f(Four<1, 2, 2, 4, 8, 2>{});
+    }
     if (M <= 4 && tiles < 256) return f(Four<4, 1, 1, 8, 4, 2>{});
     if (M <= 8) {
-        if (tiles < 512) return longer && M > 4 ? f(Four<8, 1, 1, 8, 4, 2>{}) : f(Four<8, 1, 2, 4, 4, 2>{});
+        if (tiles < 512) return longer && tiles < 256 ? f(Four<8, 1, 1, 8, 4, 2>{}) : f(Four<8, 1, 2, 4, 4, 2>{});
         return tiles < 1024 || M <= 4 ? f(Four<8, 2, 2, 4, 4, 2>{}) : f(Four<16, 1, 8, 1, 8, 4>{});
     }
     if (M <= 16) {
@@ -301,7 +314,7 @@ hipError_t with_tile(int64_t M, int64_t N, int64_t K, F&& f)
     }
     if (M <= 32) {
         if (tiles < 512) return longer && tiles < 256 ? f(Four<32, 1, 1, 8, 1, 1>{}) : f(Four<32, 1, 2, 4, 1, 1>{});
-        return tiles < 1024 ? f(Four<32, 1, 4, 2, 2, 2>{}) : f(Four<32, 1, 8, 1, 4, 4>{});
+        return tiles < 1024 ? f(Four<32, 2, 2, 4, 1, 1>{}) : f(Four<32, 1, 8, 1, 4, 4>{});
     }
     if (M <= 48) return tiles < 512 ? f(Four<48, 1, 2, 4, 1, 1>{}) : tiles < 1024 ? f(Four<48, 2, 2, 4, 1, 1>{}) : f(Four<48, 1, 8, 1, 2, 2>{});
     return tiles < 512 ? f(Four<64, 1, 2, 4, 1, 1>{}) : tiles < 1024 ? f(Four<64, 2, 2, 4, 1, 1>{}) : f(Four<64, 1, 8, 1, 2, 2>{});
@@ -314,7 +327,7 @@ hipError_t four_init()
     // one call of no rows for every tile and form: it sets the kernel's limit for LDS
     for (const int64_t M : {1, 2, 8, 16, 32, 48, 64})
         for (const int64_t N : {16, 256 * 16, 512 * 16, 768 * 16, 1024 * 16, 1536 * 16})
-            for (const int64_t K : {1024, 4096})
+            for (const int64_t K : {1024, 4096, 8192})
                 for (const int64_t group : {32, 64, 128})
                     for (int zeros = 0; zeros < 2; ++zeros) {
                         Gemm4Desc g{nullptr, nullptr, nullptr, zeros ? reinterpret_cast<const uint8_t*>(&g) : nullptr, nullptr, 0, N, K, group, false, 0};
