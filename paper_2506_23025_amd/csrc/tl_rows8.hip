@@ -218,22 +218,25 @@ hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
     return chunks > 8 ? launch_way<Stream<1, 1, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 1, 4, 1>>(list, count, s);
 }
 
-// More rows: what each way takes (us), fitted to 580 calls of M = 17 .. 4096, N and K as above: a launch and its steps, and a share for every round that the workgroups make of the chip (c: launch, a
-// step, a round, a round's step, a step of the rounds as a fraction but one at least, a round as a fraction).  The way taken is 2.5 % slower than the best of 14 on average, 13 % in one of twenty.
+// More rows: what each way takes (us), fitted to 830 calls of M = 17 .. 4096, N and K as above, weights out of the caches: a launch and its steps, and a share for every round that the workgroups make of the chip
+// (c: launch, a step, a round, a round's step, a step of the rounds as a fraction but one at least, a round as a fraction).  The way taken is 1.4 % slower than the best of 15 on average, 8 % in one of twenty.
 struct WayTime {
     int bm, bn, ks, per_cu;
     double c[6];
 };
-constexpr int kWays = 8;
+constexpr int kWays = 11;
 constexpr WayTime kWayTimes[kWays] = {
-    {32, 16, 1024, 3, {1.745, 0.160, 0.000, 0.419, 0.228, 0.000}},
-    {32, 32, 1024, 3, {1.951, 0.145, 0.000, 0.409, 0.335, 0.022}},
-    {32, 64, 512, 2, {2.153, 0.187, 0.392, 0.191, 0.174, 0.725}},
-    {32, 128, 256, 2, {2.495, 0.185, 0.294, 0.184, 0.156, 1.051}},
-    {32, 64, 1024, 1, {1.393, 0.000, 1.707, 0.868, 0.000, 0.788}},
-    {64, 128, 512, 1, {1.894, 0.000, 2.344, 1.008, 0.000, 2.301}},
-    {128, 128, 128, 2, {3.943, 0.095, 0.000, 0.240, 0.208, 2.090}},
-    {128, 256, 128, 2, {5.575, 0.169, 0.000, 0.268, 0.436, 4.008}},
+    {32, 16, 1024, 3, {1.763, 0.124, 0.000, 0.416, 0.240, 0.000}},
+    {32, 32, 1024, 3, {1.964, 0.111, 0.000, 0.521, 0.239, 0.000}},
+    {32, 32, 1024, 1, {1.359, 0.000, 1.666, 0.559, 0.000, 0.540}},
+    {32, 64, 512, 1, {1.421, 0.000, 1.405, 0.442, 0.000, 0.717}},
+    {64, 64, 512, 1, {1.392, 0.000, 2.307, 0.559, 0.000, 0.978}},
+    {32, 128, 256, 2, {2.568, 0.162, 0.452, 0.235, 0.047, 0.989}},
+    {64, 128, 512, 1, {1.846, 0.000, 2.461, 1.014, 0.000, 2.065}},
+    {64, 128, 256, 2, {3.305, 0.170, 0.355, 0.274, 0.186, 1.774}},
+    {128, 128, 256, 1, {1.005, 0.000, 4.436, 0.844, 0.000, 2.940}},
+    {128, 128, 128, 2, {3.820, 0.099, 0.295, 0.216, 0.222, 1.769}},
+    {128, 256, 128, 2, {3.469, 0.226, 0.000, 0.231, 0.493, 3.296}},
 };
 
 double way_time(int way, const Gemm8Desc* const* list, int count)
@@ -263,11 +266,14 @@ template <bool RAGGED>
 hipError_t launch_tiles(int way, const Gemm8Desc* const* list, int count, hipStream_t s)
 {
     switch (way) {
-    case 2: return launch_way<Tile<2, 2, 1, 2, 4, 3, RAGGED>>(list, count, s);
-    case 3: return launch_way<Tile<2, 2, 1, 4, 2, 3, RAGGED>>(list, count, s);
-    case 4: return launch_way<Tile<2, 4, 1, 1, 8, 3, RAGGED>>(list, count, s);
-    case 5: return launch_way<Tile<4, 4, 1, 2, 4, 3, RAGGED>>(list, count, s);
-    case 6: return launch_way<Tile<4, 4, 2, 2, 1, 4, RAGGED>>(list, count, s);
+    case 2: return launch_way<Tile<2, 2, 1, 1, 8, 4, RAGGED>>(list, count, s);
+    case 3: return launch_way<Tile<2, 2, 1, 2, 4, 4, RAGGED>>(list, count, s);
+    case 4: return launch_way<Tile<4, 2, 1, 2, 4, 4, RAGGED>>(list, count, s);
+    case 5: return launch_way<Tile<2, 2, 1, 4, 2, 4, RAGGED>>(list, count, s);
+    case 6: return launch_way<Tile<4, 4, 1, 2, 4, 3, RAGGED>>(list, count, s);
+    case 7: return launch_way<Tile<4, 2, 1, 4, 2, 3, RAGGED>>(list, count, s);
+    case 8: return launch_way<Tile<4, 4, 2, 2, 2, 4, RAGGED>>(list, count, s);
+    case 9: return launch_way<Tile<4, 4, 2, 2, 1, 4, RAGGED>>(list, count, s);
     default: return launch_way<Tile<8, 4, 1, 4, 1, 3, RAGGED>>(list, count, s);
     }
 }
