@@ -214,7 +214,7 @@ hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
         return chunks > 4 && tiles < 384 ? launch_way<Stream<1, 2, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 2, 1, 4, 1>>(list, count, s);
     }
     if (tiles >= 512) return chunks > 8 && tiles < 1024 ? launch_way<Stream<1, 1, 4, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 4, 4, 1>>(list, count, s);
-    if (tiles >= 256) return chunks > 8 ? launch_way<Stream<1, 1, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 2, 4, 1>>(list, count, s);
+    if (tiles > 256) return chunks > 8 ? launch_way<Stream<1, 1, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 2, 4, 1>>(list, count, s);
     return chunks > 8 ? launch_way<Stream<1, 1, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 1, 4, 1>>(list, count, s);
 }
 

@@ -162,6 +162,28 @@ def test_one_row_for_all():
     same(total.taken(), ref.norm(x, np.repeat(r, 40, 0))[0])
 
 
+def test_norm_of_very_many_rows():
+    """More than a launch takes."""
+    check_norm((1 << 21) + 3, 16, np.float16, weight=False, seed=10)
+
+
+def test_norm_of_rows_far_apart():
+    """Rows whose offsets pass 32 bits, in bytes and in elements."""
+    import torch
+    rng = np.random.default_rng(11)
+    x, r = values(rng, 3, 200), values(rng, 3, 200, np.float32)
+    far = (1 << 31) + 64
+    xd, rd = (torch.empty(2 * far + 200, dtype=t, device="cuda").as_strided((3, 200), (far, 1)) for t in (torch.float16, torch.float32))
+    xd.copy_(on(x))
+    rd.copy_(on(r))
+    y, codes, scales = torch.empty_strided((3, 200), (far, 1), dtype=torch.float16, device="cuda"), torch.zeros((3, 208), dtype=torch.int8, device="cuda"), torch.empty(3, device="cuda")
+    tl.tl_norm(tl.make_norm_job(xd, rd, rd, None, y, tl.make_rows8(codes, scales, 200)))
+    s, v = ref.norm(x, r, kind=np.float32)
+    same(rd.cpu().numpy(), s)
+    same(y.cpu().numpy(), v.astype(np.float16))
+    same(ref.out_of_order(codes.cpu().numpy(), 200), ref.coded(v)[0])
+
+
 # ---- the gate ---------------------------------------------------------------------------------
 #
 # The gate is within 2^-51 of the exact value before its rounding to 32 bits, numpy's within a few units of 2^-53: roundings fall on the same side but for one value in 2^26.
@@ -322,6 +344,54 @@ def test_rows8_product_at_the_ends_of_its_range():
     check_products([(codes, scales, W, np.inf)])
 
 
+@pytest.mark.parametrize("M", [2, 12, 40, 600])
+def test_rows8_product_of_more_than_4_gb_of_weights(M):
+    import torch
+    N, K = (1 << 18) + 5, 1 << 16
+    rng = np.random.default_rng(M)
+    codes = np.clip(np.rint(rng.standard_normal((M, K)) * 40), -127, 127).astype(np.int8)
+    scales = (0.01 + rng.random(M) / 30).astype(np.float32)
+    few = rng.choice(np.array([-1, 0, 1], np.int8), (40, K))
+    at = np.concatenate([[0, 1, N - 1, N - 2], rng.integers(0, N, 36)])
+    words = torch.zeros((N, K // 16), dtype=torch.int32, device="cuda")
+    words[torch.from_numpy(at).cuda()] = on(tl.tl_pack_2bit(few).view(np.int32))
+    y = torch.empty((M, N), dtype=torch.float16, device="cuda")
+    tl.tl_ternary_gemm_rows8(rows8_of(codes, scales), words, gamma_bits(0.03), y)
+    last = {int(n): i for i, n in enumerate(at)}                # a column drawn twice holds what was written last
+    cols = sorted(last)
+    got = y[:, torch.tensor(cols).cuda()].cpu().numpy()
+    fine = [c for c in cols if (at == c).sum() == 1]
+    same(got[:, [cols.index(c) for c in fine]], ref.ternary(codes, scales, few[[last[c] for c in fine]], np.float16(0.03)))
+
+
+def test_rows8_product_of_rows_far_apart():
+    """4 GB of codes, rows as far apart as they may be."""
+    import torch
+    stride, M, K = (1 << 24) - 16, 300, 200
+    codes, scales, W, gamma = product(3, M, 70, K)
+    x = torch.empty(stride * (M - 1) + 208, dtype=torch.int8, device="cuda").as_strided((M, 208), (stride, 1))
+    x.copy_(on(ref.in_order(codes)))
+    for rows in (3, 16, 30, 300):
+        y = torch.empty((rows, 70), dtype=torch.float16, device="cuda")
+        tl.tl_ternary_gemm_rows8(tl.make_rows8(x[-rows:], on(scales[-rows:]), K), on(tl.tl_pack_2bit(W).view(np.int32)), gamma_bits(gamma), y)
+        same(y.cpu().numpy(), ref.ternary(codes[-rows:], scales[-rows:], W, np.float16(gamma)))
+
+
+def test_rows8_products_on_two_streams():
+    """Two calls at once, each on a stream of its own."""
+    import torch
+    jobs = [product(40 + i, 60, 700, 2048) for i in range(2)]
+    args = [(rows8_of(c, s), on(tl.tl_pack_2bit(W).view(np.int32)), gamma_bits(g), torch.empty((60, 700), dtype=torch.float16, device="cuda")) for c, s, W, g in jobs]
+    streams = [torch.cuda.Stream() for _ in jobs]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for a, st in zip(args, streams):
+            tl.tl_ternary_gemm_rows8(*a, stream=st)
+    torch.cuda.synchronize()
+    for (c, s, W, g), a in zip(jobs, args):
+        same(a[3].cpu().numpy(), ref.ternary(c, s, W, np.float16(g)))
+
+
 # ---- products with 4-bit weights ---------------------------------------------------------------------
 
 def check_four(seed, M, N, K, group, zeros=False, wide=False, x=None, codes=None):
@@ -377,6 +447,24 @@ def test_four_of_any_number_of_columns(N):
 @pytest.mark.parametrize("M,N,K", [(1, 4096, 4096), (4, 32000, 2048), (16, 14336, 4096), (33, 4096, 14336)])
 def test_four_of_layers(M, N, K):
     check_four(M + N, M, N, K, 128, wide=M == 4)
+
+
+@pytest.mark.parametrize("M", [1, 3, 20, 70])
+def test_four_of_more_than_4_gb_of_weights(M):
+    import torch
+    N, K = (1 << 17) + 3, 1 << 16
+    rng = np.random.default_rng(M)
+    x = values(rng, M, K)
+    few = rng.integers(0, 16, (20, K)).astype(np.uint8)
+    at = np.unique(np.concatenate([[0, N - 1], rng.integers(0, N, 18)]))
+    few = few[:len(at)]
+    words = torch.zeros((N, K // 8), dtype=torch.int32, device="cuda")
+    words[torch.from_numpy(at).cuda()] = on(tl.tl_pack_4bit(few).view(np.int32))
+    scales = torch.full((K // 128, N), 1 / 16, dtype=torch.float16, device="cuda")
+    y = torch.empty((M, N), device="cuda")
+    tl.tl_gemm_4bit(tl.make_4bit_job(on(x), words, scales, None, 128, y))
+    want, off = ref.gemm4(x, (few.astype(np.float64) - 8) / 16)
+    assert (np.abs(y[:, torch.from_numpy(at).cuda()].cpu().numpy() - want) <= off + 2.0 ** -24 * np.abs(want)).all()
 
 
 def test_four_of_infinities_and_nan():
