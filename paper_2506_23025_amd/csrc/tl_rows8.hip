@@ -33,17 +33,13 @@ __global__ void __launch_bounds__(64 * NW) stream_kernel(Jobs8<JOBS> jobs)
     static_assert(R == 1 || MB == 1, "pieces beside each other");
     extern __shared__ __attribute__((aligned(16))) i32x4 part[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), quarter = lane >> 4, in = lane & 15;
-    int id = 0;
-    if constexpr (JOBS > 1) {
-        for (int i = 1; i < jobs.count; ++i) id = int(blockIdx.x) >= jobs.job[i].first ? i : id;
-    }
-    const Job8& g = jobs.job[id];
+    const Job8& g = jobs.job[job_of(jobs)];
     int n0, m0;
     if constexpr (JOBS == 1) {
         n0 = int(blockIdx.x) * (16 * NB);
         m0 = int(blockIdx.y) * (16 * MB);
     } else {
-        const int at = int(blockIdx.x) - g.first, down = at / g.across;
+        const int at = int(blockIdx.x) - g.first, down = g.down == 1 ? 0 : at / g.across;
         n0 = (at - down * g.across) * (16 * NB);
         m0 = down * (16 * MB);
     }
@@ -181,20 +177,22 @@ hipError_t launch_way(const Gemm8Desc* const* list, int count, hipStream_t s)
 {
     Jobs8<kMaxJobs> all{};
     int64_t groups = 0;
-    all.count = count;
+    for (int i = 0; i < kMaxJobs; ++i) all.first[i] = 0x7fffffff;
     for (int i = 0; i < count; ++i) {
         const Gemm8Desc& g = *list[i];
         const int64_t across = (g.N + Way::BN - 1) / Way::BN, down = (g.M + Way::BM - 1) / Way::BM;
         all.job[i] = {g.x.codes, g.x.scales, g.W, g.y, g.gamma, int(g.M), int(g.N), int(g.K), int(g.x.stride), int(groups), int(across), int(down)};
+        all.first[i] = int(groups);
         groups += across * down;
     }
     if (count == 1 && all.job[0].down < 65536)            // what a grid's second dimension holds
-        return Way::template launch<1>({{all.job[0]}, 1}, groups, s);
+        return Way::template launch<1>({{0}, {all.job[0]}}, groups, s);
     return Way::template launch<kMaxJobs>(all, groups, s);
 }
 
-// Which way.  Up to 16 rows: by the tiles of 16 columns that there are and the chunks of 256 places, since few tiles need all waves of the chip on one and many do not (measured
-// over 2100 calls of 1 to 3 products, M = 1 .. 16, N = 64 .. 22016, K = 128 .. 14336: the way taken is 1.4 % slower than the best of 12 on average, 8 % in one of twenty).
+// Which way.  Up to 16 rows: by the tiles of 16 columns that there are and the chunks of 256 places, since few tiles need all waves of the chip on one and many do not.  Measured over calls
+// of 1 to 3 products, N = 64 .. 22016, K = 128 .. 14336: the way taken is 1.4 % slower than the best of 12 on average with up to 4 rows (1150 calls), 2 % and 1.6 % slower than the best of 10 with 5 to 8 (500) and
+// 9 to 16 (960), 8 % in one of twenty.
 hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
 {
     int64_t tiles = 0, M = 0, K = 0;
@@ -208,14 +206,25 @@ hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
         if (tiles >= 768) return chunks > 8 && tiles < 1024 ? launch_way<Stream<1, 4, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 4, 2, 4, 1>>(list, count, s);
         return chunks > 16 && tiles < 512 ? launch_way<Stream<1, 4, 1, 8, 2>>(list, count, s) : launch_way<Stream<1, 4, 1, 8, 1>>(list, count, s);
     }
+    // As few columns a workgroup as leave one to a CU, or two, three, ...: 12288 x 4096 at M = 16 with 32 / 48 / 64 columns (384, 256, 192 workgroups) 8.7 / 6.4 / 7.0 us.
+    const auto groups = [&](int nb) {
+        int64_t n = 0;
+        for (int i = 0; i < count; ++i) n += (list[i]->N + 16 * nb - 1) / (16 * nb);
+        return n;
+    };
     if (M <= 8) {
-        if (tiles >= 2048) return launch_way<Stream<1, 2, 4, 4, 1>>(list, count, s);
-        if (tiles >= 768) return launch_way<Stream<1, 2, 2, 4, 1>>(list, count, s);
-        return chunks > 4 && tiles < 384 ? launch_way<Stream<1, 2, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 2, 1, 4, 1>>(list, count, s);
+        if (tiles < 896) return chunks > 4 && tiles < 384 ? launch_way<Stream<1, 2, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 2, 1, 4, 1>>(list, count, s);
+        const int64_t most = (groups(4) + 255) / 256 * 256;
+        if (tiles < 1536 || groups(2) <= most) return launch_way<Stream<1, 2, 2, 4, 1>>(list, count, s);
+        return groups(3) <= most ? launch_way<Stream<1, 2, 3, 4, 1>>(list, count, s) : launch_way<Stream<1, 2, 4, 4, 1>>(list, count, s);
     }
-    if (tiles >= 512) return chunks > 8 && tiles < 1024 ? launch_way<Stream<1, 1, 4, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 4, 4, 1>>(list, count, s);
-    if (tiles > 256) return chunks > 8 ? launch_way<Stream<1, 1, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 2, 4, 1>>(list, count, s);
-    return chunks > 8 ? launch_way<Stream<1, 1, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 1, 4, 1>>(list, count, s);
+    const int64_t most = (groups(6) + 255) / 256 * 256;
+    const bool two = chunks > 8;
+    if (groups(1) <= most) return two ? launch_way<Stream<1, 1, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 1, 4, 1>>(list, count, s);
+    if (groups(2) <= most) return two ? launch_way<Stream<1, 1, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 2, 4, 1>>(list, count, s);
+    if (groups(3) <= most) return two ? launch_way<Stream<1, 1, 3, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 3, 4, 1>>(list, count, s);
+    if (groups(4) <= most) return two ? launch_way<Stream<1, 1, 4, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 4, 4, 1>>(list, count, s);
+    return chunks > 16 ? launch_way<Stream<1, 1, 6, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 6, 4, 1>>(list, count, s);
 }
 
 // More rows: what each way takes (us), fitted to 830 calls of M = 17 .. 4096, N and K as above, weights out of the caches: a launch and its steps, and a share for every round that the workgroups make of the chip

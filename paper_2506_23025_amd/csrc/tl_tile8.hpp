@@ -24,9 +24,18 @@ struct Job8 {
 constexpr int kMaxJobs = 16;              // of a launch
 template <int JOBS>
 struct Jobs8 {
+    int first[JOBS];                      // the jobs' first workgroups, or more than any: side by side, so that one load brings them
     Job8 job[JOBS];
-    int count;
 };
+// The job of this workgroup.
+template <int JOBS>
+__device__ inline int job_of(const Jobs8<JOBS>& jobs)
+{
+    int id = 0;
+#pragma unroll
+    for (int i = 1; i < JOBS; ++i) id += int(blockIdx.x) >= jobs.first[i];
+    return id;
+}
 
 // The 16 weights of a packed word as four registers of four bytes: byte i of register s is weight 4 i + s, as the rows' codes stand.  A code picks its byte of a table.
 __device__ inline i32x4 decoded8(uint32_t w)
@@ -66,11 +75,7 @@ tile8_kernel(Jobs8<JOBS> jobs)
     const int set = wave / (C::WM * C::WN), wm = wave / C::WN % C::WM, wn = wave % C::WN;
     const uint32_t lds0 = uint32_t(uintptr_t((const __attribute__((address_space(3))) unsigned char*)lds));
 
-    int id = 0;
-    if constexpr (JOBS > 1) {
-        for (int i = 1; i < jobs.count; ++i) id = int(blockIdx.x) >= jobs.job[i].first ? i : id;
-    }
-    const Job8& g = jobs.job[id];
+    const Job8& g = jobs.job[job_of(jobs)];
 
     // Workgroup ids go round the 8 XCDs, each with an L2 of its own: an XCD takes a contiguous piece of an order that walks the grid in bands of 4 row blocks, column by column.
     int tm, tn;
