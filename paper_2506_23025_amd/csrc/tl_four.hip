@@ -83,6 +83,9 @@ __device__ inline u32x4 shifted(u32x4 v, int n)
 // registers, D chunks ahead.  Rows of x go through registers into LDS, a panel of CP WK chunks at a time and the next one while a panel is used, since every wave needs all of them; a panel's scales
 // and zeros go the same way, as a wave that fetched its own would ask for 32 bytes four times over at every turn.
 // The words are the column operand of the matrix instruction: a lane has one column, so one zero point and one scale.  Sums of UNIT steps of 32 are scaled and added in fp32.
+// What bounds it (MI355X, weights out of the caches): one row memory, 32000 x 4096 14.0 us = 5.7 TB/s without the launch's 2.5, 4096 x 4096 4.2; the decode before that (masks and bases as literals, 13
+// instead of 9 instructions a word: 15.4 and 4.7).  More rows what every workgroup fetches of x: 24 rows of 32000 x 4096 19.9 us, 64 rows of 4096 x 4096 13.5 (0.5 MB of x for every CU).  More chunks
+// ahead, and all columns' sums in one wave, made no difference or less.
 template <int MR, int FN, int WN, int WK, int CP, int D, int UNIT, bool ZEROS>
 __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 {
