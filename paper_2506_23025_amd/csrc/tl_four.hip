@@ -155,7 +155,7 @@ __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 #pragma unroll
         for (int i = 0; i < SL; ++i) {
             const int at = i * THREADS + tid;
-            uint32_t v = sr[i];
+            uint32_t v = uint32_t(panel * (PK * 4) + at / BN * UNIT) < blocks32 ? sr[i] : 0u;      // nothing behind K: an infinite scale would make its 0 a NaN
             if constexpr (ZEROS) v |= uint32_t(__builtin_bit_cast(uint16_t, _Float16(short(zr[i])))) << 16;
             if (ENTRIES % THREADS == 0 || at < ENTRIES) reinterpret_cast<uint32_t*>(lds + (panel & 1) * PANEL + MR * PK * 256)[at] = v;
         }

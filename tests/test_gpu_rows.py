@@ -479,6 +479,24 @@ def test_four_of_infinities_and_nan():
         assert np.isnan(got[1]).all() and not np.isfinite(got[4]).any() and np.array_equal(got[rest], clean[rest])
 
 
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("M,K", [(1, 290), (3, 290), (20, 290), (2, 33), (70, 1025)])
+def test_four_of_an_infinite_scale_in_the_last_group(M, K, group):
+    """The places that fill up a block of 128 have no part in a sum: 0 times the last group's scale is no number if that is infinite."""
+    import torch
+    N, rng = 40, np.random.default_rng(K)
+    x = np.ones((M, K), np.float16)
+    codes = rng.integers(9, 16, (N, K)).astype(np.uint8)
+    scales = np.full((-(-K // group), N), 1 / 16, np.float16)
+    scales[-1, 7] = np.inf
+    scales[-1, 9] = -np.inf
+    y = torch.empty((M, N), device="cuda")
+    tl.tl_gemm_4bit(tl.make_4bit_job(on(x), on(tl.tl_pack_4bit(codes).view(np.int32)), on(scales), None, group, y))
+    want = np.broadcast_to((codes.astype(np.float64) - 8).sum(1) / 16, (M, N)).copy()
+    want[:, 7], want[:, 9] = np.inf, -np.inf
+    np.testing.assert_array_equal(y.cpu().numpy(), want)
+
+
 def check_four_raw(seed, M, N, K, group, x):
     """The same call as check_four's without its comparison."""
     import torch
