@@ -1,6 +1,8 @@
 // Products with 4-bit weights and group scales.
 #include "tl_rows.hpp"
 
+#include <cmath>
+
 namespace tl {
 namespace {
 
@@ -84,8 +86,8 @@ __device__ inline u32x4 shifted(u32x4 v, int n)
 // and zeros go the same way, as a wave that fetched its own would ask for 32 bytes four times over at every turn.
 // The words are the column operand of the matrix instruction: a lane has one column, so one zero point and one scale.  Sums of UNIT steps of 32 are scaled and added in fp32.
 // What bounds it (MI355X, weights out of the caches): one row memory, 32000 x 4096 14.0 us = 5.7 TB/s without the launch's 2.5, 4096 x 4096 4.2; the decode before that (masks and bases as literals, 13
-// instead of 9 instructions a word: 15.4 and 4.7).  More rows what every workgroup fetches of x: 24 rows of 32000 x 4096 19.9 us, 64 rows of 4096 x 4096 13.5 (0.5 MB of x for every CU).  More chunks
-// ahead, and all columns' sums in one wave, made no difference or less.
+// instead of 9 instructions a word: 15.4 and 4.7).  More rows what every workgroup fetches of x: 24 rows of 32000 x 4096 20.3 us, 64 rows of 4096 x 4096 9.2.  More chunks ahead, and all columns' sums
+// in one wave, made no difference or less.
 template <int MR, int FN, int WN, int WK, int CP, int D, int UNIT, bool ZEROS>
 __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
 {
@@ -293,55 +295,108 @@ struct Four {
     }
 };
 
-// Which tile: by the rows, so that none is staged in vain, and by the column tiles of 16 that there are: few of them get all waves on their own part of K, many
-// share the rows of x among more columns.  Measured over 700 calls of M = 1 .. 64, N = 64 .. 65536, K = 64 .. 14336, groups of 32 to 256: the tile taken is 2 % slower than
-// the best of those built on average, 8 % in one of twenty.
+// The time of a way, in us: rows, columns and K of a step of one workgroup, workgroups that a CU takes side by side, and what was fitted to 2 to 300 rows
+// (launch, a step, a round, a round's step, a step of the rounds as a fraction but one at least, a round as a fraction).  The rows are dealt to several workgroups where there are few columns: at
+// 64 x 4096 x 4096 32 rows a workgroup take 9.3 us and 64 rows, which leave half of the CUs without one, 14.0; at 64 x 1024 x 11008 32 rows 16.0, 16 rows 10.9 and 64 rows 32.0.  Over 5192 calls of N = 64 .. 65536,
+// K = 256 .. 14336 and groups of 32 to 256 the way taken is 2.0 % slower than the best of 31 on average; over 1105 more calls 3.2 %, 12 % in one of twenty.
+struct WayTime {
+    int rows, columns, step, per_cu;
+    float c[6];
+};
+constexpr int kManyWays = 19;
+constexpr WayTime kWayTimes[kManyWays] = {
+    {1, 16, 1024, 1, {2.132f, 0.153f, 0.000f, 0.214f, 0.014f, 0.369f}},
+    {4, 16, 1024, 1, {2.655f, 0.054f, 0.000f, 0.365f, 0.056f, 0.409f}},
+    {8, 16, 1024, 2, {2.710f, 0.285f, 0.084f, 0.242f, 0.086f, 0.627f}},
+    {8, 32, 1024, 1, {2.066f, 0.000f, 0.351f, 0.807f, 0.033f, 0.857f}},
+    {8, 64, 512, 1, {1.940f, 0.000f, 0.292f, 0.724f, 0.000f, 1.129f}},
+    {16, 16, 1024, 1, {2.083f, 0.350f, 0.000f, 0.455f, 0.108f, 0.395f}},
+    {16, 32, 512, 3, {2.011f, 0.367f, 0.000f, 0.207f, 0.153f, 0.405f}},
+    {16, 64, 512, 1, {2.068f, 0.000f, 0.199f, 0.804f, 0.033f, 1.021f}},
+    {16, 128, 128, 1, {2.415f, 0.077f, 0.129f, 0.323f, 0.000f, 0.916f}},
+    {32, 16, 1024, 1, {1.662f, 0.000f, 0.650f, 1.455f, 0.000f, 0.327f}},
+    {32, 32, 512, 2, {2.093f, 0.360f, 0.094f, 0.377f, 0.233f, 0.368f}},
+    {32, 64, 512, 1, {1.319f, 0.033f, 0.929f, 1.242f, 0.004f, 0.760f}},
+    {32, 128, 256, 1, {1.174f, 0.000f, 1.208f, 0.924f, 0.002f, 1.586f}},
+    {48, 32, 512, 1, {1.306f, 0.000f, 1.026f, 1.132f, 0.121f, 0.397f}},
+    {48, 64, 512, 1, {1.278f, 0.025f, 1.493f, 1.627f, 0.000f, 0.666f}},
+    {48, 128, 128, 1, {1.986f, 0.145f, 0.382f, 0.312f, 0.253f, 1.460f}},
+    {64, 32, 512, 1, {1.573f, 0.003f, 0.878f, 1.615f, 0.000f, 0.408f}},
+    {64, 64, 512, 1, {1.522f, 0.060f, 1.493f, 1.968f, 0.000f, 0.789f}},
+    {64, 128, 128, 1, {1.512f, 0.090f, 1.148f, 0.771f, 0.000f, 1.590f}},
+};
+constexpr int kWays = kManyWays + 4;        // and those for one row alone
+
 template <class F>
-hipError_t with_tile(int64_t M, int64_t N, int64_t K, F&& f)
+hipError_t with_way(int way, F&& f)
 {
-    const int64_t tiles = (N + 15) / 16;
-    const bool longer = K > 2048;
+    switch (way) {
+    case 0: return f(Four<1, 1, 1, 8, 4, 2>{});
+    case 1: return f(Four<4, 1, 1, 8, 4, 4>{});
+    case 2: return f(Four<8, 1, 1, 8, 4, 2>{});
+    case 3: return f(Four<8, 1, 2, 8, 2, 2>{});
+    case 4: return f(Four<8, 1, 4, 4, 2, 2>{});
+    case 5: return f(Four<16, 1, 1, 8, 1, 1>{});
+    case 6: return f(Four<16, 1, 2, 4, 1, 1>{});
+    case 7: return f(Four<16, 1, 4, 4, 2, 2>{});
+    case 8: return f(Four<16, 1, 8, 1, 8, 4>{});
+    case 9: return f(Four<32, 1, 1, 8, 1, 1>{});
+    case 10: return f(Four<32, 1, 2, 4, 1, 1>{});
+    case 11: return f(Four<32, 2, 2, 4, 1, 1>{});
+    case 12: return f(Four<32, 1, 8, 2, 2, 2>{});
+    case 13: return f(Four<48, 1, 2, 4, 1, 1>{});
+    case 14: return f(Four<48, 2, 2, 4, 1, 1>{});
+    case 15: return f(Four<48, 1, 8, 1, 2, 2>{});
+    case 16: return f(Four<64, 1, 2, 4, 1, 1>{});
+    case 17: return f(Four<64, 2, 2, 4, 1, 1>{});
+    case 18: return f(Four<64, 1, 8, 1, 2, 2>{});
+    case 19: return f(Four<1, 1, 1, 8, 4, 4>{});
+    case 20: return f(Four<1, 1, 1, 4, 8, 4>{});
+    case 21: return f(Four<1, 1, 2, 4, 8, 2>{});
+    default: return f(Four<1, 2, 2, 4, 8, 2>{});
+    }
+}
+
+int way_of(int64_t M, int64_t N, int64_t K)
+{
     if (M <= 1) {
-        if (tiles < 256) return K > 4096 ? f(Four<1, 1, 1, 8, 4, 4>{}) : f(Four<1, 1, 1, 8, 4, 2>{});
-        return tiles < 768 ? f(Four<1, 1, 1, 4, 8, 4>{}) : tiles < 1536 ? f(Four<1, 1, 2, 4, 8, 2>{}) : f(Four<1, 2, 2, 4, 8, 2>{});
+        // by the column tiles of 16 that there are: few of them get all waves on their own part of K, many share the row's places among more columns (4096 x 4096 4.20 us with four sets of waves, 4.50
+        // with eight; 4096 x 11008 7.8 and 7.1)
+        const int64_t tiles = (N + 15) / 16;
+        if (tiles <= 256 && K > 4096) return kManyWays;
+        if (tiles < 256) return 0;
+        return tiles < 768 ? kManyWays + 1 : tiles < 1536 ? kManyWays + 2 : kManyWays + 3;
     }
-    if (M <= 4 && tiles < 256) return f(Four<4, 1, 1, 8, 4, 2>{});
-    if (M <= 8) {
-        if (tiles < 512) return longer && tiles < 256 ? f(Four<8, 1, 1, 8, 4, 2>{}) : f(Four<8, 1, 2, 4, 4, 2>{});
-        return tiles < 1024 || M <= 4 ? f(Four<8, 2, 2, 4, 4, 2>{}) : f(Four<16, 1, 8, 1, 8, 4>{});
+    int best = 0;
+    float least = 0;
+    for (int i = 0; i < kManyWays; ++i) {
+        const WayTime& w = kWayTimes[i];
+        if (w.rows < 64 && M > w.rows * 4) continue;
+        const float r = float((M + w.rows - 1) / w.rows) * float((uint32_t(N) + uint32_t(w.columns) - 1) / uint32_t(w.columns)) * (1.0f / 256), k = float((uint32_t(K) + uint32_t(w.step) - 1) / uint32_t(w.step));
+        const float turns = std::ceil(r > float(w.per_cu) ? r / float(w.per_cu) : r), rounds = r > float(w.per_cu) ? turns * float(w.per_cu) : turns;
+        const float t = w.c[0] + w.c[1] * k + w.c[2] * rounds + w.c[3] * rounds * k + w.c[4] * (r > 1.0f ? r : 1.0f) * k + w.c[5] * r;
+        if (least == 0 || t < least) least = t, best = i;
     }
-    if (M <= 16) {
-        if (tiles >= 1024) return f(Four<16, 1, 8, 1, 8, 4>{});
-        if (!longer) return f(Four<16, 1, 2, 4, 1, 1>{});
-        return tiles < 256 ? f(Four<16, 1, 1, 8, 1, 1>{}) : tiles < 512 ? f(Four<16, 1, 2, 4, 2, 2>{}) : f(Four<16, 2, 2, 4, 2, 2>{});
-    }
-    if (M <= 32) {
-        if (tiles < 512) return longer && tiles < 256 ? f(Four<32, 1, 1, 8, 1, 1>{}) : f(Four<32, 1, 2, 4, 1, 1>{});
-        return tiles < 1024 ? f(Four<32, 2, 2, 4, 1, 1>{}) : f(Four<32, 1, 8, 1, 4, 4>{});
-    }
-    if (M <= 48) return tiles < 512 ? f(Four<48, 1, 2, 4, 1, 1>{}) : tiles < 1024 ? f(Four<48, 2, 2, 4, 1, 1>{}) : f(Four<48, 1, 8, 1, 2, 2>{});
-    return tiles < 512 ? f(Four<64, 1, 2, 4, 1, 1>{}) : tiles < 1024 ? f(Four<64, 2, 2, 4, 1, 1>{}) : f(Four<64, 1, 8, 1, 2, 2>{});
+    return best;
 }
 
 }  // namespace
 
 hipError_t four_init()
 {
-    // one call of no rows for every tile and form: it sets the kernel's limit for LDS
-    for (const int64_t M : {1, 2, 8, 16, 32, 48, 64})
-        for (const int64_t N : {16, 256 * 16, 512 * 16, 768 * 16, 1024 * 16, 1536 * 16})
-            for (const int64_t K : {1024, 4096, 8192})
-                for (const int64_t group : {32, 64, 128})
-                    for (int zeros = 0; zeros < 2; ++zeros) {
-                        Gemm4Desc g{nullptr, nullptr, nullptr, zeros ? reinterpret_cast<const uint8_t*>(&g) : nullptr, nullptr, 0, N, K, group, false, 0};
-                        if (const hipError_t e = with_tile(M, N, K, [&](auto tile) { return decltype(tile)::launch(g, nullptr); }); e != hipSuccess) return e;
-                    }
+    // one call of no rows for every way and form: it sets the kernel's limit for LDS
+    for (int way = 0; way < kWays; ++way)
+        for (const int64_t group : {32, 64, 128})
+            for (int zeros = 0; zeros < 2; ++zeros) {
+                Gemm4Desc g{nullptr, nullptr, nullptr, zeros ? reinterpret_cast<const uint8_t*>(&g) : nullptr, nullptr, 0, 16, 128, group, false, 0};
+                if (const hipError_t e = with_way(way, [&](auto tile) { return decltype(tile)::launch(g, nullptr); }); e != hipSuccess) return e;
+            }
     return hipSuccess;
 }
 
 hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s)
 {
-    constexpr int64_t kRows = int64_t(65535) * 16;        // what a grid's second dimension holds
+    constexpr int64_t kRows = 65535;                      // what a grid's second dimension holds, of workgroups with one row each
     for (int64_t m = 0; m < g.M; m += kRows) {
         Gemm4Desc part = g;
         part.x += m * g.K;
@@ -349,7 +404,7 @@ hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s)
         part.M = g.M - m < kRows ? g.M - m : kRows;
         part.magic = g.group >= g.K ? 0u : uint32_t(((uint64_t(1) << 31) + g.group / 32 - 1) / uint64_t(g.group / 32));
         if (g.K < 8) hipLaunchKernelGGL(simple_kernel, dim3(unsigned((g.N + 15) / 16), unsigned((part.M + 15) / 16)), dim3(256), 0, s, part);
-        else if (const hipError_t e = with_tile(part.M, g.N, g.K, [&](auto tile) { return decltype(tile)::launch(part, s); }); e != hipSuccess) return e;
+        else if (const hipError_t e = with_way(way_of(part.M, g.N, g.K), [&](auto tile) { return decltype(tile)::launch(part, s); }); e != hipSuccess) return e;
     }
     return hipGetLastError();
 }

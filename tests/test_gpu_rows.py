@@ -449,6 +449,15 @@ def test_four_of_layers(M, N, K):
     check_four(M + N, M, N, K, 128, wide=M == 4)
 
 
+# a call for each of the ways to deal the rows and columns to workgroups, the rows to one workgroup and to several
+@pytest.mark.parametrize("M,N,K", [(2, 65, 520), (5, 65, 1100), (17, 65, 2600), (17, 2501, 1900), (2, 9000, 520), (5, 65, 520), (33, 1501, 520), (33, 4097, 1100), (49, 4097, 520), (65, 65, 520),
+                                   (65, 65, 1100), (100, 3201, 520), (100, 4097, 520), (130, 65, 520), (130, 3201, 1100), (130, 3201, 520), (211, 65, 520), (211, 2501, 1100), (211, 2501, 520),
+                                   (1, 65, 4100), (1, 9000, 520), (1, 13001, 520), (1, 25001, 520)])
+def test_four_of_few_and_many_columns(M, N, K):
+    check_four(M + N, M, N, K, 128, wide=True)
+    check_four(M + N + 1, M, N, K - 3, 32, zeros=True)
+
+
 @pytest.mark.parametrize("M", [1, 3, 20, 70])
 def test_four_of_more_than_4_gb_of_weights(M):
     import torch
