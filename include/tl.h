@@ -454,7 +454,7 @@ typedef struct tl_rows {
 /*
  * Rows of 8-bit codes, -127 .. 127: place d of row r stands for scales[r] * code.  In each block of 16 places, place 4 i + s is byte 4 s + i (i, s = 0 .. 3): the order
  * in which two bits of every byte of a packed word's bits meet them.  A row's last block is filled with 0; bytes behind it are
- * neither read nor written.
+ * not written, and what they hold does not matter.
  *   codes    device, 16-byte aligned; rows are `stride` bytes apart, a multiple of 16 of at least ceil(places / 16) * 16 and below 2^24 (one row alone: any such multiple or 0)
  *   scales   device, fp32 [rows], 4-byte aligned
  * A row v becomes codes by its largest magnitude t: scale t / 127, code round(v * (127 / t)), quotients, product and rounding (to the nearest, ties
@@ -562,7 +562,7 @@ tl_status tl_unpack_4bit(const uint32_t* packed, int64_t N, int64_t K, uint8_t* 
  *   scales   device, fp16 [ceil(K / group)][N], 16-byte aligned;  zeros: device, uint8 of the same shape, 16-byte aligned (any byte is taken as it is), or NULL
  *   y        device, fp16 or fp32 [M][N], 16-byte aligned
  *   group    a multiple of 32; the last group may be short
- * Any M >= 1, N below 2^24, K below 2^20; made for few rows (weights are streamed once for every 64).  A NaN or an infinity in row m of x shows in row m of y and in no other, one in a scale in its
+ * Any M >= 1, N below 2^24, K below 2^20; made for few rows (a pass over the weights serves up to 64).  A NaN or an infinity in row m of x shows in row m of y and in no other, one in a scale in its
  * column.  Deterministic: no atomics, fixed order.
  */
 typedef struct tl_gemm_4bit_job {
