@@ -454,6 +454,17 @@ __attribute__((visibility("default"))) int tl_internal_jobs_by_table(int count, 
 // Likewise: workgroups of `waves` waves that a launch of the 1.6-bit streaming kernel puts on a CU, and the LDS that one is given.
 __attribute__((visibility("default"))) int tl_internal_stream3_per_cu(int waves, int* lds) { return tl::gemv3_per_cu(waves, lds); }
 
+// Likewise: the launches of products over 8-bit rows (M, N, K each, up to 64 of them), rows8_launches.
+__attribute__((visibility("default"))) int tl_internal_rows8_launches(const int64_t* sizes, int count, int64_t* out, int most)
+{
+    tl::Gemm8Desc jobs[64];
+    if (count > 64) return -1;
+    const auto at = [] { return reinterpret_cast<void*>(uintptr_t(0x1000)); };       // nothing is read there
+    for (int j = 0; j < count; ++j)
+        jobs[j] = {{static_cast<int8_t*>(at()), static_cast<float*>(at()), 0}, nullptr, static_cast<__half*>(at()), 1.0f, sizes[3 * j], sizes[3 * j + 1], sizes[3 * j + 2]};
+    return tl::rows8_launches(jobs, count, out, most);
+}
+
 tl_status tl_init(void)
 {
     hipError_t e = tl::gemv_init();

@@ -48,6 +48,8 @@ struct Gemm8Desc {
 };
 hipError_t launch_rows8_jobs(const Gemm8Desc* jobs, int64_t count, hipStream_t s);
 hipError_t rows8_init();
+// For the tests: the launches that launch_rows8_jobs makes, and of the first `most` of them: up to 16 rows or more (1, 0), way, odd packed rows, products, rows, workgroups, threads of one.
+int rows8_launches(const Gemm8Desc* jobs, int count, int64_t* out, int most);
 
 struct Gemm4Desc {
     const _Float16* x;

@@ -6,7 +6,8 @@
 namespace tl {
 namespace {
 
-constexpr int64_t kMostOutputs = int64_t(1) << 30;       // of a launch: a grid counts its threads in 32 bits, and 32 x 16 outputs have 256 of them
+// Tiles of 32 x 16 outputs of a launch of more than 16 rows: a grid counts its threads in 32 bits, and a workgroup of any way has 512 of them at most and one tile, also where that has fewer columns.
+constexpr int64_t kMostTiles = int64_t(1) << 21;
 constexpr int64_t kLimit = 0x7ffffff0;      // a descriptor's size: less than any offset that is none
 constexpr int kRawBuffer = 0x00027000;      // a descriptor's last word: bytes, no format, no swizzle
 
@@ -153,7 +154,7 @@ __global__ void __launch_bounds__(64 * NW) stream_kernel(Jobs8<JOBS> jobs)
 
 template <int MB, int R, int NB, int NW, int D>
 struct Stream {
-    static constexpr int BM = 16 * MB, BN = 16 * NB, KS = 256 * NW, PER_CU = NB < 2 ? 3 : 2;
+    static constexpr int BM = 16 * MB, BN = 16 * NB, THREADS = 64 * NW;
     template <int JOBS>
     static hipError_t launch(const Jobs8<JOBS>& jobs, int64_t groups, hipStream_t s)
     {
@@ -168,7 +169,7 @@ struct Stream {
 template <int FM, int FN, int WM, int WN, int WK, int ST, bool RAGGED>
 struct Tile {
     using C = Tile8Cfg<FM, FN, WM, WN, WK, ST, RAGGED>;
-    static constexpr int BM = C::BM, BN = C::BN, KS = 128 * WK, PER_CU = C::GROUPS;
+    static constexpr int BM = C::BM, BN = C::BN, THREADS = 64 * C::WAVES;
     template <int JOBS>
     static hipError_t launch(const Jobs8<JOBS>& jobs, int64_t groups, hipStream_t s) { return launch_tile8<C, JOBS>(jobs, groups, s); }
 };
@@ -195,7 +196,7 @@ hipError_t launch_way(const Gemm8Desc* const* list, int count, hipStream_t s)
 // Which way.  Up to 16 rows: by the tiles of 16 columns that there are and the chunks of 256 places, since few tiles need all waves of the chip on one and many do not.  Measured over calls
 // of 1 to 3 products, N = 64 .. 22016, K = 128 .. 14336: the way taken is 1.4 % slower than the best of 12 on average with up to 4 rows (1150 calls), 2 % and 1.6 % slower than the best of 10 with 5 to 8 (500) and
 // 9 to 16 (960), 8 % in one of twenty.
-hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
+int few_way(const Gemm8Desc* const* list, int count)
 {
     int64_t tiles = 0, M = 0, K = 0;
     for (int i = 0; i < count; ++i) {
@@ -205,8 +206,8 @@ hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
     }
     const int64_t chunks = (K + 255) / 256;
     if (M <= 4) {
-        if (tiles >= 768) return chunks > 8 && tiles < 1024 ? launch_way<Stream<1, 4, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 4, 2, 4, 1>>(list, count, s);
-        return chunks > 16 && tiles < 512 ? launch_way<Stream<1, 4, 1, 8, 2>>(list, count, s) : launch_way<Stream<1, 4, 1, 8, 1>>(list, count, s);
+        if (tiles >= 768) return chunks > 8 && tiles < 1024 ? 3 : 2;
+        return chunks > 16 && tiles < 512 ? 1 : 0;
     }
     // As few columns a workgroup as leave one to a CU, or two, three, ...: 12288 x 4096 at M = 16 with 32 / 48 / 64 columns (384, 256, 192 workgroups) 8.7 / 6.4 / 7.0 us.
     const auto groups = [&](int nb) {
@@ -215,18 +216,41 @@ hipError_t launch_few(const Gemm8Desc* const* list, int count, hipStream_t s)
         return n;
     };
     if (M <= 8) {
-        if (tiles < 896) return chunks > 4 && tiles < 384 ? launch_way<Stream<1, 2, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 2, 1, 4, 1>>(list, count, s);
+        if (tiles < 896) return chunks > 4 && tiles < 384 ? 5 : 4;
         const int64_t most = (groups(4) + 255) / 256 * 256;
-        if (tiles < 1536 || groups(2) <= most) return launch_way<Stream<1, 2, 2, 4, 1>>(list, count, s);
-        return groups(3) <= most ? launch_way<Stream<1, 2, 3, 4, 1>>(list, count, s) : launch_way<Stream<1, 2, 4, 4, 1>>(list, count, s);
+        if (tiles < 1536 || groups(2) <= most) return 6;
+        return groups(3) <= most ? 7 : 8;
     }
     const int64_t most = (groups(6) + 255) / 256 * 256;
-    const bool two = chunks > 8;
-    if (groups(1) <= most) return two ? launch_way<Stream<1, 1, 1, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 1, 4, 1>>(list, count, s);
-    if (groups(2) <= most) return two ? launch_way<Stream<1, 1, 2, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 2, 4, 1>>(list, count, s);
-    if (groups(3) <= most) return two ? launch_way<Stream<1, 1, 3, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 3, 4, 1>>(list, count, s);
-    if (groups(4) <= most) return two ? launch_way<Stream<1, 1, 4, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 4, 4, 1>>(list, count, s);
-    return chunks > 16 ? launch_way<Stream<1, 1, 6, 4, 2>>(list, count, s) : launch_way<Stream<1, 1, 6, 4, 1>>(list, count, s);
+    const int two = chunks > 8;
+    for (int nb = 1; nb <= 4; ++nb)
+        if (groups(nb) <= most) return 7 + 2 * nb + two;
+    return chunks > 16 ? 18 : 17;
+}
+template <class F>
+hipError_t with_few(int way, F&& f)
+{
+    switch (way) {
+    case 0: return f(Stream<1, 4, 1, 8, 1>{});
+    case 1: return f(Stream<1, 4, 1, 8, 2>{});
+    case 2: return f(Stream<1, 4, 2, 4, 1>{});
+    case 3: return f(Stream<1, 4, 2, 4, 2>{});
+    case 4: return f(Stream<1, 2, 1, 4, 1>{});
+    case 5: return f(Stream<1, 2, 1, 4, 2>{});
+    case 6: return f(Stream<1, 2, 2, 4, 1>{});
+    case 7: return f(Stream<1, 2, 3, 4, 1>{});
+    case 8: return f(Stream<1, 2, 4, 4, 1>{});
+    case 9: return f(Stream<1, 1, 1, 4, 1>{});
+    case 10: return f(Stream<1, 1, 1, 4, 2>{});
+    case 11: return f(Stream<1, 1, 2, 4, 1>{});
+    case 12: return f(Stream<1, 1, 2, 4, 2>{});
+    case 13: return f(Stream<1, 1, 3, 4, 1>{});
+    case 14: return f(Stream<1, 1, 3, 4, 2>{});
+    case 15: return f(Stream<1, 1, 4, 4, 1>{});
+    case 16: return f(Stream<1, 1, 4, 4, 2>{});
+    case 17: return f(Stream<1, 1, 6, 4, 1>{});
+    default: return f(Stream<1, 1, 6, 4, 2>{});
+    }
 }
 
 // More rows: what each way takes (us), fitted to 830 calls of M = 17 .. 4096, N and K as above, weights out of the caches: a launch and its steps, and a share for every round that the workgroups make of the chip
@@ -273,83 +297,86 @@ int best_way(const Gemm8Desc* const* list, int count, double* time)
     return best;
 }
 
-template <bool RAGGED>
-hipError_t launch_tiles(int way, const Gemm8Desc* const* list, int count, hipStream_t s)
+template <bool RAGGED, class F>
+hipError_t with_tile(int way, F&& f)
 {
     switch (way) {
-    case 2: return launch_way<Tile<2, 2, 1, 1, 8, 4, RAGGED>>(list, count, s);
-    case 3: return launch_way<Tile<2, 2, 1, 2, 4, 4, RAGGED>>(list, count, s);
-    case 4: return launch_way<Tile<4, 2, 1, 2, 4, 4, RAGGED>>(list, count, s);
-    case 5: return launch_way<Tile<2, 2, 1, 4, 2, 4, RAGGED>>(list, count, s);
-    case 6: return launch_way<Tile<4, 4, 1, 2, 4, 3, RAGGED>>(list, count, s);
-    case 7: return launch_way<Tile<4, 2, 1, 4, 2, 3, RAGGED>>(list, count, s);
-    case 8: return launch_way<Tile<4, 4, 2, 2, 2, 4, RAGGED>>(list, count, s);
-    case 9: return launch_way<Tile<4, 4, 2, 2, 1, 4, RAGGED>>(list, count, s);
-    default: return launch_way<Tile<8, 4, 1, 4, 1, 3, RAGGED>>(list, count, s);
+    case 2: return f(Tile<2, 2, 1, 1, 8, 4, RAGGED>{});
+    case 3: return f(Tile<2, 2, 1, 2, 4, 4, RAGGED>{});
+    case 4: return f(Tile<4, 2, 1, 2, 4, 4, RAGGED>{});
+    case 5: return f(Tile<2, 2, 1, 4, 2, 4, RAGGED>{});
+    case 6: return f(Tile<4, 4, 1, 2, 4, 3, RAGGED>{});
+    case 7: return f(Tile<4, 2, 1, 4, 2, 3, RAGGED>{});
+    case 8: return f(Tile<4, 4, 2, 2, 2, 4, RAGGED>{});
+    case 9: return f(Tile<4, 4, 2, 2, 1, 4, RAGGED>{});
+    default: return f(Tile<8, 4, 1, 4, 1, 3, RAGGED>{});
     }
 }
-
-hipError_t launch_many(int way, const Gemm8Desc* const* list, int count, hipStream_t s)
+template <class F>
+hipError_t with_many(int way, bool ragged, F&& f)
 {
-    if (way == 0) return launch_way<Stream<2, 1, 1, 4, 1>>(list, count, s);
-    if (way == 1) return launch_way<Stream<2, 1, 2, 4, 1>>(list, count, s);
+    if (way == 0) return f(Stream<2, 1, 1, 4, 1>{});
+    if (way == 1) return f(Stream<2, 1, 2, 4, 1>{});
+    return ragged ? with_tile<true>(way, f) : with_tile<false>(way, f);
+}
+
+// The launch that products share.
+struct Launch8 {
+    bool few, ragged;                     // up to 16 rows; packed rows that are no multiple of 16 bytes
+    int way, count;
+    const Gemm8Desc* const* list;
+    template <class F>
+    hipError_t with(F&& f) const { return few ? with_few(way, f) : with_many(way, ragged, f); }
+};
+int64_t tiles_of(const Gemm8Desc& g) { return (g.M + 31) / 32 * ((g.N + 15) / 16); }
+Launch8 launch_few(const Gemm8Desc* const* list, int count) { return {true, false, few_way(list, count), count, list}; }
+Launch8 launch_many(int way, const Gemm8Desc* const* list, int count)
+{
     bool ragged = false;
     for (int i = 0; i < count; ++i) ragged |= (list[i]->K + 15) / 16 % 4 != 0;
-    return ragged ? launch_tiles<true>(way, list, count, s) : launch_tiles<false>(way, list, count, s);
+    return {false, ragged, way, count, list};
 }
 
-}  // namespace
-
-hipError_t rows8_init()
-{
-    const Gemm8Desc none{{nullptr, nullptr, 0}, nullptr, nullptr, 0.0f, 0, 0, 64};
-    const Gemm8Desc* const list[2] = {&none, &none};
-    for (int way = 2; way < kWays; ++way)
-        for (int count = 1; count <= 2; ++count) {
-            if (const hipError_t e = launch_tiles<false>(way, list, count, nullptr); e != hipSuccess) return e;
-            if (const hipError_t e = launch_tiles<true>(way, list, count, nullptr); e != hipSuccess) return e;
-        }
-    return hipSuccess;
-}
-
-hipError_t launch_rows8_jobs(const Gemm8Desc* jobs, int64_t count, hipStream_t s)
+// The launches of a call, one after the other.
+template <class F>
+hipError_t each_launch(const Gemm8Desc* jobs, int64_t count, F&& f)
 {
     // Products of up to 16 rows share launches; those of more do where that is expected to be faster.
     const Gemm8Desc* few[kMaxJobs];
     const Gemm8Desc* many[kMaxJobs];
     int nfew = 0, nmany = 0;
     const auto close_few = [&] {
-        const hipError_t e = nfew ? launch_few(few, nfew, s) : hipSuccess;
+        const hipError_t e = nfew ? f(launch_few(few, nfew)) : hipSuccess;
         nfew = 0;
         return e;
     };
     const auto close_many = [&] {
         if (nmany == 0) return hipSuccess;
         double apart = 0.0, together = 0.0, t = 0.0;
-        int64_t outputs = 0;
+        int64_t tiles = 0;
         int own[kMaxJobs];
         for (int i = 0; i < nmany; ++i) {
             own[i] = best_way(many + i, 1, &t);
             apart += t;
-            outputs += many[i]->M * many[i]->N;
+            tiles += tiles_of(*many[i]);
         }
         const int way = best_way(many, nmany, &together);
         const int n = nmany;
         nmany = 0;
-        if (together <= apart && outputs <= kMostOutputs) return launch_many(way, many, n, s);
+        if (together <= apart && tiles <= kMostTiles) return f(launch_many(way, many, n));
         for (int i = 0; i < n; ++i)
-            if (const hipError_t e = launch_many(own[i], many + i, 1, s); e != hipSuccess) return e;
+            if (const hipError_t e = f(launch_many(own[i], many + i, 1)); e != hipSuccess) return e;
         return hipSuccess;
     };
     for (int64_t i = 0; i < count; ++i) {
         const Gemm8Desc& g = jobs[i];
-        if (g.M * g.N > kMostOutputs) {                   // in launches of its own
-            const int64_t rows = kMostOutputs / g.N > 256 ? kMostOutputs / g.N / 256 * 256 : 256;
+        if (g.M > 16 && tiles_of(g) > kMostTiles) {       // in launches of its own; 256 rows of the widest matrix are 2^23 tiles, which have 2^31 threads, as no way gives wide matrices more than 256 a tile
+            const int64_t most = kMostTiles / ((g.N + 15) / 16) * 32, rows = most > 256 ? most / 256 * 256 : 256;
             for (int64_t m = 0; m < g.M; m += rows) {
                 const Gemm8Desc part{{g.x.codes + m * g.x.stride, g.x.scales + m, g.x.stride}, g.W, g.y + m * g.N, g.gamma, g.M - m < rows ? g.M - m : rows, g.N, g.K};
                 const Gemm8Desc* const one = &part;
                 double t;
-                if (const hipError_t e = launch_many(best_way(&one, 1, &t), &one, 1, s); e != hipSuccess) return e;
+                if (const hipError_t e = f(launch_many(best_way(&one, 1, &t), &one, 1)); e != hipSuccess) return e;
             }
         } else if (g.M <= 16) {
             few[nfew++] = &g;
@@ -363,6 +390,44 @@ hipError_t launch_rows8_jobs(const Gemm8Desc* jobs, int64_t count, hipStream_t s
     }
     if (const hipError_t e = close_few(); e != hipSuccess) return e;
     return close_many();
+}
+
+}  // namespace
+
+hipError_t rows8_init()
+{
+    const Gemm8Desc none{{nullptr, nullptr, 0}, nullptr, nullptr, 0.0f, 0, 0, 64};
+    const Gemm8Desc* const list[2] = {&none, &none};
+    for (int way = 2; way < kWays; ++way)
+        for (int count = 1; count <= 2; ++count)
+            for (int ragged = 0; ragged < 2; ++ragged)
+                if (const hipError_t e = with_many(way, ragged, [&](auto w) { return launch_way<decltype(w)>(list, count, nullptr); }); e != hipSuccess) return e;
+    return hipSuccess;
+}
+
+hipError_t launch_rows8_jobs(const Gemm8Desc* jobs, int64_t count, hipStream_t s)
+{
+    return each_launch(jobs, count, [s](const Launch8& l) { return l.with([&](auto w) { return launch_way<decltype(w)>(l.list, l.count, s); }); });
+}
+
+int rows8_launches(const Gemm8Desc* jobs, int count, int64_t* out, int most)
+{
+    int n = 0;
+    const hipError_t none = each_launch(jobs, count, [&](const Launch8& l) {
+        return l.with([&](auto w) {
+            using Way = decltype(w);
+            int64_t groups = 0, rows = 0;
+            for (int i = 0; i < l.count; ++i) {
+                groups += ((l.list[i]->M + Way::BM - 1) / Way::BM) * ((l.list[i]->N + Way::BN - 1) / Way::BN);
+                rows += l.list[i]->M;
+            }
+            const int64_t now[7] = {l.few, l.way, l.ragged, l.count, rows, groups, Way::THREADS};
+            for (int i = 0; n < most && i < 7; ++i) out[n * 7 + i] = now[i];
+            ++n;
+            return hipSuccess;
+        });
+    });
+    return none == hipSuccess ? n : -1;
 }
 
 }  // namespace tl
