@@ -4,6 +4,7 @@ import ctypes
 import pytest
 
 import paper_2506_23025_amd as tl
+import test_gpu_rows8_ways as on_gpu
 
 _launches = tl.raw().tl_internal_rows8_launches           # not in tl.h: for the tests alone
 _launches.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_void_p, ctypes.c_int]
@@ -26,3 +27,22 @@ def test_a_launch_counts_its_threads_in_32_bits(sizes):
     found = launches(*sizes, most=1 << 16)
     assert all(0 < launch["groups"] * launch["threads"] < 1 << 32 for launch in found)
     assert sum(launch["rows"] for launch in found) == sum(M for M, _, _ in sizes)
+
+
+def ways(few, calls):
+    """The (way, odd packed rows) of calls that make one launch each."""
+    found = set()
+    for sizes in calls:
+        (launch,) = launches(*sizes)
+        assert launch["few"] == few and launch["jobs"] == len(sizes), sizes
+        found.add((launch["way"], launch["ragged"]))
+    return found
+
+
+def test_calls_of_the_gpu_tests_reach_every_way():
+    every = {(way, ragged) for way in range(11) for ragged in (0, 1)}
+    for calls in ([(s,) for s in on_gpu.MANY], [(s,) for s in on_gpu.LONG], on_gpu.JOINT):
+        assert ways(0, calls) == every
+    every = {(way, 0) for way in range(19)}
+    assert ways(1, [(s,) for s in on_gpu.FEW]) == every
+    assert ways(1, [((M, N - N // 3, K), (max(1, M - 1), N // 3, K)) for M, N, K in on_gpu.FEW]) == every
