@@ -35,10 +35,13 @@ __device__ inline uint32_t wave_max(uint32_t x)
     return uint32_t(__builtin_amdgcn_readlane(int(over_wave(x, [](uint32_t a, uint32_t b) { return a > b ? a : b; })), 63));
 }
 
-// g / (1 + e^-g) * u in fp64, off by some 2^-50 of itself, so that its fp32 rounding is that of the exact value but for one in 2^26; an infinity or NaN where g or u is not finite.  e^-g = 2^n e^r with |r| <= log(2) / 2;
+// g / (1 + e^-g) * u in fp64; an infinity or NaN where g or u is not finite.  e^-g = 2^n e^r with |r| <= log(2) / 2;
 // e^r by the polynomial of degree 10 that agrees with it at the eleven nodes of Chebyshev's on that interval (off by 2^-51); the quotient from the hardware's reciprocal q of d = 1 + e^-g, which is off by e = 1 - d q, as
 // w q (1 + e + e^2).  A product in fp64 costs what one in fp32 does here; conversions cost more, so n is found by a sum that leaves it in the lowest bits, and 2^n goes into the exponent by an
 // integer addition.
+// How far it is off: 2^-51 of itself for g > -1, 2^-50.1 down to -10, 2^-49.5 to -22, 2^-48.9 to -40, 2^-47.8 at -104, below which fp32 has nothing: log(2) is one number, and what it lacks moves e^-g by n 2^-55.2.  Two numbers for it,
+// one more sum a value, would keep 2^-50.7 and change no result: over every g of fp16 and every mantissa of u (72 million pairs) both give the exact value's rounding to fp32 but for the same 100 pairs,
+// all with |g| <= 2^-16, where g / 2 + g^2 / 4 is a tie between two numbers and what decides is below 2^-53 of it.
 struct Gate {
     // in scalar registers: the compiler would move each into the sum's registers first
     double c[10] = {0x1.28a2ca617b969p-22, 0x1.72fafebdaf273p-19, 0x1.a019a6611cad5p-16, 0x1.a01978b8b3d18p-13, 0x1.6c16c17f46982p-10,
