@@ -1,8 +1,9 @@
-"""The gate over the ranges of fp16, as fp32 has it."""
+"""The gate over the ranges of fp16 as fp32 has it, and 4-bit products with zero points of any byte."""
 import numpy as np
 import pytest
 
 import paper_2506_23025_amd as tl
+import rows as ref
 from test_gpu_rows import on, same
 
 pytestmark = pytest.mark.gpu
@@ -46,3 +47,17 @@ def test_gate_in_32_bits(lo, hi):
         a, b = ((np.where(np.abs(t) >= least, np.abs(t) / np.float32(127), np.float32(0))).astype(np.float32) for t in (v, other))
     assert ((scales == a) | (near & (scales == b))).all(), f"{int((scales != a).sum())} differ, {int(near.sum())} near"
     same(codes, np.where(scales > 0, np.where(v < 0, -127, 127), 0).astype(np.int8))
+
+
+@pytest.mark.parametrize("M,N,K,group", [(1, 40, 5, 32), (1, 70, 520, 128), (3, 70, 500, 64), (20, 70, 500, 32), (70, 33, 300, 256), (130, 65, 260, 64)])
+def test_four_of_any_zero_point(M, N, K, group):
+    import torch
+    rng = np.random.default_rng(M + N + K)
+    x, codes = rng.standard_normal((M, K)).astype(np.float16), rng.integers(0, 16, (N, K)).astype(np.uint8)
+    G = -(-K // group)
+    scales, zeros = ((0.5 + rng.random((G, N))) / 16).astype(np.float16), rng.integers(0, 256, (G, N)).astype(np.uint8)
+    zeros[0, :4] = 255, 254, 16, 128
+    y = torch.empty((M, N), device="cuda")
+    tl.tl_gemm_4bit(tl.make_4bit_job(on(x), on(tl.tl_pack_4bit(codes).view(np.int32)), on(scales), on(zeros), group, y))
+    want, off = ref.gemm4(x, ref.weights4(codes, scales, zeros, group))     # code - zero is exact in fp16 for any byte: 1024 + 255 is below 2048
+    assert (np.abs(y.cpu().numpy() - want) <= off + 2.0 ** -24 * np.abs(want)).all()

@@ -56,6 +56,17 @@ def test_quantising_to_4_bits():
     assert scales[0, 0] == s and zeros[0, 0] == 8 and zeros[1, 0] == 8 and codes[0, :4].tolist() == [15, 5, 9, 0] or codes[0, 3] in (0, 1)
 
 
+def test_quantising_to_4_bits_with_zero_points():
+    codes, scales, zeros = tl.tl_quantize_4bit(np.array([[0.7, -0.3, 0.05, -0.8] + [0] * 60], dtype=np.float32), 32, True)
+    s = np.float16((np.float64(np.float32(0.7)) + np.float64(np.float32(0.8))) / 15)
+    assert scales[:, 0].tolist() == [s, 0] and zeros[:, 0].tolist() == [8, 8]
+    assert codes[0, :4].tolist() == [15, 5, 9, 0]          # 8 + round(w / s): w / s is 7.0, -3.0, 0.5001 (s is below 0.1) and -8.0
+    assert (codes[0, 4:] == 8).all()
+    codes, scales, zeros = tl.tl_quantize_4bit(np.array([[3.0, 6.0, 15.0] + [3.0] * 29, [-15.0, -2.0, -7.0] + [-2.0] * 29], dtype=np.float32), 32, True)
+    assert scales[0].tolist() == [1, 1] and zeros[0].tolist() == [0, 15]                # 0 is always among what a group can be
+    assert codes[0, :4].tolist() == [3, 6, 15, 3] and codes[1, :4].tolist() == [0, 13, 8, 13]
+
+
 @pytest.mark.parametrize("zeros", [False, True])
 @pytest.mark.parametrize("group", [32, 96, 4096])
 def test_quantised_weights_are_near(group, zeros):
