@@ -465,6 +465,9 @@ __attribute__((visibility("default"))) int tl_internal_rows8_launches(const int6
     return tl::rows8_launches(jobs, count, out, most);
 }
 
+// Likewise: the way of a product with 4-bit weights.
+__attribute__((visibility("default"))) int tl_internal_four_way(int64_t M, int64_t N, int64_t K) { return tl::four_way(M, N, K); }
+
 tl_status tl_init(void)
 {
     hipError_t e = tl::gemv_init();

@@ -394,6 +394,8 @@ hipError_t four_init()
     return hipSuccess;
 }
 
+int four_way(int64_t M, int64_t N, int64_t K) { return K < 8 ? -1 : way_of(M, N, K); }
+
 hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s)
 {
     constexpr int64_t kRows = 65535;                      // what a grid's second dimension holds, of workgroups with one row each

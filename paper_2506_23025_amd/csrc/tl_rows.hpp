@@ -63,5 +63,6 @@ struct Gemm4Desc {
 };
 hipError_t launch_gemm4(const Gemm4Desc& g, hipStream_t s);            // sets magic itself
 hipError_t four_init();
+int four_way(int64_t M, int64_t N, int64_t K);                         // for the tests: the way of a product, or -1 for the kernel for K < 8
 
 }  // namespace tl
