@@ -445,6 +445,7 @@ tl_status tl_attn_prompt(const tl_prompt_job* job, void* stream);
  *
  * Rows of numbers: element (row r, place d) at ptr + r * stride + d, fp16 unless said otherwise.  ptr is 16-byte aligned; the stride is in elements, a
  * multiple of 16 bytes, not negative and below 2^40; rows that a call writes are at least as far apart as they are long (one row alone: any stride).
+ * Products write dense rows, and tl_gemm_4bit reads such: several rows of a product go straight into these calls, and theirs into it, where the number of places is a multiple of 8.
  */
 typedef struct tl_rows {
     void* ptr;                /* device */

@@ -86,7 +86,7 @@ __device__ inline u32x4 shifted(u32x4 v, int n)
 // and zeros go the same way, as a wave that fetched its own would ask for 32 bytes four times over at every turn.
 // The words are the column operand of the matrix instruction: a lane has one column, so one zero point and one scale.  Sums of UNIT steps of 32 are scaled and added in fp32.
 // What bounds it (MI355X, weights out of the caches): one row memory, 32000 x 4096 14.0 us = 5.7 TB/s without the launch's 2.5, 4096 x 4096 4.2; the decode before that (masks and bases as literals, 13
-// instead of 9 instructions a word: 15.4 and 4.7).  More rows what every workgroup fetches of x: 24 rows of 32000 x 4096 20.3 us, 64 rows of 4096 x 4096 9.2.  More chunks ahead, and all columns' sums
+// instead of 9 instructions a word: 15.4 and 4.7).  More rows what every workgroup fetches of x: 24 rows of 32000 x 4096 21.7 us (16.6 to 17.5 where some of the 65 MB are in the caches), 64 rows of 4096 x 4096 9.0.  More chunks ahead, and all columns' sums
 // in one wave, made no difference or less.
 template <int MR, int FN, int WN, int WK, int CP, int D, int UNIT, bool ZEROS>
 __global__ void __launch_bounds__(64 * WN * WK) four_kernel(Gemm4Desc g)
@@ -299,6 +299,7 @@ struct Four {
 // (launch, a step, a round, a round's step, a step of the rounds as a fraction but one at least, a round as a fraction).  The rows are dealt to several workgroups where there are few columns: at
 // 64 x 4096 x 4096 32 rows a workgroup take 9.3 us and 64 rows, which leave half of the CUs without one, 14.0; at 64 x 1024 x 11008 32 rows 16.0, 16 rows 10.9 and 64 rows 32.0.  Over 5192 calls of N = 64 .. 65536,
 // K = 256 .. 14336 and groups of 32 to 256 the way taken is 2.0 % slower than the best of 31 on average; over 1105 more calls 3.2 %, 12 % in one of twenty.
+// Beyond 300 rows and below K = 256 the times are extrapolated; more than 192 rows have the ways of 64 alone to choose from, and every 64 rows read and decode the weights again.
 struct WayTime {
     int rows, columns, step, per_cu;
     float c[6];

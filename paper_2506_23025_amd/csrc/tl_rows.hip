@@ -120,9 +120,12 @@ __device__ inline void put(float* row, int d, int dim, const float* v)
 
 // W waves hold a row in registers, C pieces of 8 values a lane; workgroups of four rows where a wave has one to itself.  One pass over memory: a row is read once, its sum of squares (fp64: squares of
 // fp32 numbers are exact there, and with the root and the quotient in it too every rounding falls as the formula's does, whatever the order) and its largest magnitude go over the wave by DPP and over
-// the waves through LDS.  What bounds it (MI355X): a lone row the launch, 2.4 us; the norm memory, 8192 rows of 4096 places with a residual in fp16 to 8 bits 45.2 us = 5.2 TB/s read and written, what a
-// large copy reaches on the card; 32-bit residuals 5.4 TB/s.  The gate the vector unit, busy 77 % at 4096 rows of 11008, 61 to 64 us = 3.5 TB/s: 37 instructions a value, 21 of them in fp64.  Before
-// the polynomial of degree 10, constants in scalar registers, conversions and selects taken out it took 116 us.
+// the waves through LDS.  What bounds it (MI355X): a lone row the launch, 2.4 us; the norm memory, 8192 rows of 4096 places with a residual in fp16 to 8 bits 45 us = 5.2 TB/s read and written, what a
+// large copy reaches on the card; 32-bit residuals 5.4 TB/s.  The gate the vector unit, busy 77 % of the time at 4096 rows of 11008 (26.2 M instructions, fp64 conversions and reciprocals longer than others), 62 to 65 us = 3.5 TB/s:
+// 37 instructions a value, 21 of them in fp64.  Before the polynomial of degree 10, constants in scalar registers, conversions and selects taken out it took 116 us.
+// What it waits for besides: a piece is loaded behind a branch and converted in it, so each load is waited for before the next is asked for; x, residual and weight are three trips to memory one after the other
+// (192 rows of 4096 with a 32-bit residual 4.0 us, a lone row 2.4).  The last piece of a row that is no multiple of 8 is loaded a value at a time: 8192 rows of 4093 places 68 us in a loop that takes 48 for 4096, the gate of 4096 rows of
+// 11005 73 and 68.  The gate of rows of more than 32768 places (16 waves, 8 pieces) keeps 75 registers in memory: 256 rows of 65536 27.7 us, of 32768 15.8.
 template <RowsKind KIND, int W, int C>
 __global__ void __launch_bounds__(W == 1 ? 256 : 64 * W) rows_kernel(RowsArgs a)
 {
