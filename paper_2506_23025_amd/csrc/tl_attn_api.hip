@@ -46,7 +46,7 @@ inline tl_status heads_number_status(int64_t q_heads, int64_t kv_heads)
 inline tl_status cache_status(const tl_kv_cache& c)
 {
     if (!c.k || !c.v || !c.k_scale || !c.v_scale || !c.page_table) return TL_ERR_NULL;
-    if (c.type != TL_KV_INT8 && c.type != TL_KV_FP8) return TL_ERR_UNSUPPORTED;
+    if (code_of(c.type) != TL_KV_INT8 && code_of(c.type) != TL_KV_FP8) return TL_ERR_UNSUPPORTED;
     if (c.kv_heads < 1 || c.kv_heads > kMaxHeads || !dim_ok(c.head_dim)) return TL_ERR_SHAPE;
     const int64_t lim = int64_t(1) << 31;
     if (c.page_tokens < 16 || c.page_tokens > 1024 || (c.page_tokens & (c.page_tokens - 1))) return TL_ERR_SHAPE;
@@ -80,7 +80,7 @@ tl_status tl_rope_table(float* table, int64_t positions, int64_t rot_dim, double
     if (!positive(base)) return TL_ERR_VALUE;
     const tl_rope_scaling none{TL_ROPE_PLAIN, 1.0, 1.0, 0.0, 1.0, 1.0};
     const tl_rope_scaling& sc = scaling ? *scaling : none;
-    if (sc.kind != TL_ROPE_PLAIN && sc.kind != TL_ROPE_LINEAR && sc.kind != TL_ROPE_BY_PARTS) return TL_ERR_UNSUPPORTED;
+    if (const int kind = tl::code_of(sc.kind); kind != TL_ROPE_PLAIN && kind != TL_ROPE_LINEAR && kind != TL_ROPE_BY_PARTS) return TL_ERR_UNSUPPORTED;
     if (!positive(sc.magnitude) || (sc.kind != TL_ROPE_PLAIN && !positive(sc.factor))) return TL_ERR_VALUE;
     if (sc.kind == TL_ROPE_BY_PARTS && (!positive(sc.trained) || !(sc.low >= 0.0) || !(sc.low < sc.high) || !std::isfinite(sc.high))) return TL_ERR_VALUE;
     const int64_t half = rot_dim / 2;

@@ -18,6 +18,16 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 
+// A code of a caller's struct as the whole number that is there: one that its enum cannot hold is refused, and loading it as the enum would be undefined.
+template <class E>
+inline int code_of(const E& e)
+{
+    static_assert(sizeof(E) == sizeof(int), "C enums");
+    int v;
+    __builtin_memcpy(&v, &e, sizeof v);
+    return v;
+}
+
 // Launchers return hipGetLastError() of their launch.  All pointers are device pointers.
 hipError_t launch_unpack2(const uint32_t* packed, int64_t N, int64_t K, int8_t* out, hipStream_t s);
 // fx: the fixed-point byte code of Sec. 3.2 (decoded by App. F, Alg. 1) instead of plain base 3

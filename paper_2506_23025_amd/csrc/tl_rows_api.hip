@@ -81,7 +81,7 @@ tl_status tl_norm(const tl_norm_job* job, void* stream)
     const tl_norm_job& j = *job;
     tl_status e = sizes_status(j.rows, j.dim);
     if (e != TL_OK) return e;
-    if (j.real != TL_REAL_FP16 && j.real != TL_REAL_FP32) return TL_ERR_UNSUPPORTED;
+    if (code_of(j.real) != TL_REAL_FP16 && code_of(j.real) != TL_REAL_FP32) return TL_ERR_UNSUPPORTED;
     if (!(j.eps >= 0.0f) || !std::isfinite(j.eps)) return TL_ERR_VALUE;
     const int wide = j.real == TL_REAL_FP32 ? 4 : 2;
     const bool sum = j.residual.ptr && j.sum.ptr;
@@ -207,7 +207,7 @@ tl_status tl_gemm_4bit(const tl_gemm_4bit_job* job, void* stream)
     const tl_gemm_4bit_job& j = *job;
     if (!j.x || !j.Wpacked || !j.scales || !j.y) return TL_ERR_NULL;
     if (!product_ok(j.M, j.N, j.K) || j.N >= (int64_t(1) << 24) || j.K >= (int64_t(1) << 20) || !group_ok(j.group)) return TL_ERR_SHAPE;
-    if (j.y_real != TL_REAL_FP16 && j.y_real != TL_REAL_FP32) return TL_ERR_UNSUPPORTED;
+    if (code_of(j.y_real) != TL_REAL_FP16 && code_of(j.y_real) != TL_REAL_FP32) return TL_ERR_UNSUPPORTED;
     if (!aligned(j.x, 16) || !aligned(j.Wpacked, 16) || !aligned(j.scales, 16) || !aligned(j.zeros, 16) || !aligned(j.y, 16)) return TL_ERR_ALIGN;
     const Gemm4Desc d{static_cast<const _Float16*>(j.x), static_cast<const uint32_t*>(j.Wpacked), static_cast<const _Float16*>(j.scales),
                       static_cast<const uint8_t*>(j.zeros), j.y, j.M, j.N, j.K, j.group, j.y_real == TL_REAL_FP32, 0};

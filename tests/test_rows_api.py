@@ -194,3 +194,14 @@ def test_4_bit_product_refusals():
     for kw in ({"M": 0}, {"N": 0}, {"K": 0}, {"group": 0}, {"group": 48}, {"group": -32}, {"N": 1 << 24}, {"K": 1 << 20}):
         assert status(**kw) == tl.TL_ERR_SHAPE, kw
     assert status(y_real=2) == tl.TL_ERR_UNSUPPORTED
+
+
+def test_codes_that_are_no_type():
+    """Any int may stand where a type or a kind is wanted, negative ones too: refused, and in the build with sanitizers not an undefined load."""
+    scaling, table = tl.tl_rope_scaling(0, 1.0, 1.0, 0.0, 1.0, 1.0), np.zeros(8, np.float32)
+    four = tl.tl_gemm_4bit_job(P, P, P, P, P, 1, 16, 256, 64, 0)
+    for code in (-1, -2 ** 31, 7, 2 ** 31 - 1):
+        assert norm(real=code) == tl.TL_ERR_UNSUPPORTED
+        four.y_real = scaling.kind = code
+        assert tl.raw().tl_gemm_4bit(ctypes.byref(four), None) == tl.TL_ERR_UNSUPPORTED
+        assert tl.raw().tl_rope_table(table.ctypes.data, 1, 8, 1e4, ctypes.byref(scaling)) == tl.TL_ERR_UNSUPPORTED
