@@ -16,8 +16,8 @@ LONG = [(17, 16, 4032), (17, 16, 4007), (33, 2056, 3839), (33, 2112, 4010), (19,
         (389, 13464, 2112), (399, 13608, 2149), (100, 4096, 11008)]
 # Two products that share a launch.
 JOINT = [((19, 17, 3008), (19, 16, 512)), ((19, 17, 2736), (19, 16, 238)), ((21, 21, 2496), (17, 4140, 256)), ((33, 41, 2847), (17, 5071, 227)), ((21, 17, 5184), (17, 17, 384)),
-         ((21, 17, 5643), (17, 17, 576)), ((17, 95, 4032), (17, 8524, 256)), ((71, 39, 4849), (35, 5907, 208)), ((65, 21, 3072), (65, 6049, 256)), ((33, 33, 4168), (33, 8667, 444)),
-         ((81, 21, 2304), (81, 8299, 256)), ((91, 27, 2301), (91, 8351, 266)), ((157, 119, 3072), (157, 7217, 1088)), ((145, 25, 3317), (145, 6880, 1444)), ((117, 83, 1728), (117, 8241, 320)),
+         ((21, 17, 5643), (17, 17, 576)), ((17, 95, 4032), (17, 8524, 256)), ((71, 39, 4849), (35, 5907, 208)), ((65, 21, 3136), (65, 6049, 256)), ((33, 33, 4168), (33, 8667, 444)),
+         ((81, 21, 2304), (81, 8299, 256)), ((91, 27, 2301), (91, 8351, 266)), ((157, 119, 3136), (157, 7217, 1088)), ((145, 25, 3317), (145, 6880, 1444)), ((117, 83, 1728), (117, 8241, 320)),
          ((633, 23, 1430), (633, 1645, 200)), ((193, 4639, 3136), (193, 4639, 1344)), ((341, 3483, 2729), (341, 3483, 230)), ((163, 6927, 2432), (163, 6927, 256)),
          ((195, 4725, 2409), (195, 4725, 301)), ((397, 6447, 1723), (397, 6447, 250)), ((399, 6691, 2651), (399, 6691, 1430))]
 # Up to 16 rows.
